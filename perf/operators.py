@@ -1,0 +1,337 @@
+"""The operators that answer over a paged cache, and what they must compute.
+
+Once a request's cache is repaired, the target model answers over it: every
+layer appends the keys and values of the new tokens, rotated to their
+positions, to the pages of their sequence, and attends from the rotated
+queries to everything cached.  Three operators, one layer each:
+
+``append``  K and V of the new tokens of a batch of sequences into the pages,
+            keys (and queries) rotated by R_M(p) on the way;
+``attend``  softmax attention of those queries over the pages, grouped heads,
+            causal or over an interval of positions per query, scores
+            optionally capped by a tanh or given a bias by distance;
+``shared``  the same where all sequences of the batch begin with the same
+            pages (one repaired document set, many questions or samples).
+
+A case names an operator, the head layout and ranges of lengths; the lengths
+themselves follow from ``shape``, the values and the order of the pages from
+the seed.  ``q_lo..q_hi`` new tokens per sequence come on top of
+``len_lo..len_hi`` cached ones (of a sequence's own, behind ``shared`` common
+ones).
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+# query heads, KV heads, head_dim of the repository's targets, and of a small fp32 one
+HEADS = {"qwen3b": (16, 2, 128), "llama8b": (32, 8, 128), "tiny": (4, 2, 64)}
+THETA = 1e6
+
+
+def _case(name, op, target, seqs, q, length, shape, dtype="bf16", page=16, **more):
+    heads, kv_heads, head_dim = HEADS[target] if isinstance(target, str) else target
+    c = {"name": name, "op": op, "dtype": dtype, "heads": heads, "kv_heads": kv_heads,
+         "head_dim": head_dim, "page": page, "seqs": seqs, "q_lo": q[0], "q_hi": q[1],
+         "len_lo": length[0], "len_hi": length[1], "shape": shape, "mask": "causal", "cap": 0.0,
+         "bias": False, "shared": 0, "far": 0}
+    c.update(more)
+    return c
+
+
+def listed():
+    return [
+        # one decoding step of a serving batch: 64 sequences, one token each
+        _case("append-64x1", "append", "qwen3b", 64, (1, 1), (100, 4000), 1),
+        # the questions and uncached passages of a ragged batch of an 8B target
+        _case("append-ragged-8b", "append", "llama8b", 6, (300, 4000), (0, 3000), 2),
+        # fp32 pages, odd counts, positions far behind a preamble that is cached elsewhere
+        _case("append-f32-far", "append", "tiny", 3, (7, 301), (0, 90), 3, dtype="f32", page=8,
+              far=1 << 20),
+        # one request decodes over eight repaired passages: latency
+        _case("attend-1x4096", "attend", "qwen3b", 1, (1, 1), (4095, 4095), 4),
+        # a decoding step of a batch whose lengths differ widely
+        _case("attend-64-ragged-8b", "attend", "llama8b", 64, (1, 1), (64, 16000), 5),
+        # few sequences, very long caches
+        _case("attend-4x131072", "attend", "qwen3b", 4, (1, 1), (120000, 131071), 6),
+        # questions of odd lengths over repaired passages
+        _case("attend-questions-8b", "attend", "llama8b", 5, (17, 333), (1177, 8001), 7),
+        # an uncached prompt: as much computing as reading, the longest pass
+        _case("attend-prompt-8b", "attend", "llama8b", 1, (8192, 8192), (4096, 4096), 8, page=64),
+        # capped scores with a bias by distance, each query within an interval of documents
+        _case("attend-capped-documents", "attend", (16, 8, 64), 7, (1, 77), (300, 4001), 9, cap=30.0,
+              bias=True, mask="documents"),
+        # fp32, a bidirectional prefix
+        _case("attend-f32-prefix", "attend", "tiny", 3, (1, 130), (40, 700), 10, dtype="f32",
+              mask="prefix"),
+        # 64 samples of the answer to one request over 16k shared tokens
+        _case("shared-64x16384", "shared", "qwen3b", 64, (1, 1), (1, 500), 11, shared=16384),
+        # questions of a few tokens over one odd-sized set of passages
+        _case("shared-9x1177-8b", "shared", "llama8b", 9, (1, 9), (0, 60), 12, shared=1177),
+    ]
+
+
+def _log(rng, a, b):
+    return int(round(math.exp(rng.uniform(math.log(a), math.log(b)))))
+
+
+def draw(rng):
+    """A case of the listed ranges: one to 64 sequences, one to 8,192 new tokens,
+    none to 131,072 cached ones, groups of one to eight query heads."""
+    op = rng.choice(["append", "attend", "attend", "attend", "shared"])
+    dtype = "f32" if rng.random() < 0.2 else "bf16"
+    kv_heads = rng.choice([1, 2, 3, 4, 8])
+    heads = kv_heads * rng.choice([1, 2, 4, 5, 7, 8])
+    head_dim = rng.choice([64, 128, 128, 128, 96, 256])
+    page = rng.choice([1, 8, 16, 16, 16, 64, 256])
+    seqs = _log(rng, 1, 64)
+    # about 12,000 new tokens and 400 MB of cached keys and values at most
+    decode = rng.random() < 0.5
+    q_hi = 1 if decode else _log(rng, 2, min(8192, 12000 // seqs))
+    q_lo = rng.randint(1, q_hi)
+    budget = (400 << 20) // (2 * kv_heads * head_dim * (4 if dtype == "f32" else 2)) // seqs
+    most = max(1, min(131072, budget, (1 << 32) // (seqs * q_hi * heads * (head_dim // 32))))
+    shape = rng.randrange(1 << 30)
+    more = {}
+    if op == "append":
+        most = min(most, 4096)
+        more["far"] = rng.choice([0, 0, 1, 1 << 20])
+    if op == "attend":
+        more["mask"] = rng.choice(["causal", "causal", "documents", "prefix"])
+        more["cap"] = rng.choice([0.0, 0.0, 15.0, 50.0])
+        more["bias"] = rng.random() < 0.3
+    if op == "shared":
+        more["shared"] = _log(rng, 100, max(100, min(32768, most * seqs // 2)))
+        most = min(most, 1024)
+    len_hi = _log(rng, min(16, most), most)
+    return _case("drawn", op, (heads, kv_heads, head_dim), seqs, (q_lo, q_hi),
+                 (rng.randint(0, len_hi), len_hi), shape, dtype=dtype, page=page, **more)
+
+
+def _lengths(case):
+    """(new tokens, cached tokens including the shared ones) of every sequence."""
+    rng = random.Random(case["shape"])
+    q = [rng.randint(case["q_lo"], case["q_hi"]) for _ in range(case["seqs"])]
+    own_len = [_log(rng, case["len_lo"] + 1, case["len_hi"] + 1) - 1 for _ in range(case["seqs"])]
+    return q, [case["shared"] + n for n in own_len]
+
+
+def _intervals(case, q, total):
+    """Positions [lo, hi) that every query sees, in order of the queries."""
+    rng = random.Random(case["shape"] + 1)
+    lo, hi = [], []
+    for nq, n in zip(q, total):
+        edges = sorted(rng.randrange(n) for _ in range(6))
+        for i in range(nq):
+            p = n - nq + i
+            if case["mask"] == "documents":       # from the start of a document; some see nothing
+                a = rng.choice([e for e in edges if e <= p] or [0])
+                lo.append(a)
+                hi.append(a if rng.random() < 1 / 16 else p + 1)
+            else:                                 # causal, but all of the first two thirds
+                lo.append(0)
+                hi.append(max(p + 1, 2 * n // 3))
+    return lo, hi
+
+
+def prepare(case, seed):
+    q, cached = _lengths(case)
+    total = [a + b for a, b in zip(q, cached)]
+    dt, ps = TORCH[case["dtype"]], case["page"]
+    H, Hkv, d = case["heads"], case["kv_heads"], case["head_dim"]
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    host = random.Random(seed)
+    # the pages that all sequences begin with, then each sequence's own (the rest of a shared
+    # page that ends inside is copied to every sequence, so it counts as its own)
+    n_shared = case["shared"] // ps
+    need = [-(-n // ps) - n_shared for n in total]
+    width = n_shared + max(need)
+    n_blocks = n_shared + sum(need) + 3
+    ids = list(range(n_blocks))
+    host.shuffle(ids)
+    at, rows = n_shared, []
+    for n in need:
+        rows.append(ids[:n_shared] + ids[at:at + n] + [-1] * (width - n_shared - n))
+        at += n
+    pool = torch.empty(1, 2, n_blocks, ps, Hkv, d, dtype=dt, device="cuda").normal_(generator=g)
+    spread = torch.empty(Hkv, d, device="cuda").uniform_(math.log(0.5), math.log(8.0), generator=g).exp()
+    pool[:, 0] *= spread.to(dt)
+    N = sum(q)
+    new = torch.empty(N, H + 2 * Hkv, d, dtype=dt, device="cuda").normal_(generator=g)
+    off = [0]
+    for n in q:
+        off.append(off[-1] + n)
+    st = {"case": dict(case), "q": q, "total": total, "off": off, "pool": pool, "rows": rows,
+          "table": torch.tensor(rows, dtype=torch.int32, device="cuda"),
+          "lens": torch.tensor(total, dtype=torch.int32, device="cuda"),
+          # one fused projection's output: queries, keys and values side by side
+          "qh": new[:, :H], "kh": new[:, H:H + Hkv], "vh": new[:, H + Hkv:],
+          "out": torch.empty(N, H, d, dtype=dt, device="cuda"), "lo": None, "hi": None,
+          "slopes": None, "positions": None}
+    pos = [n - nq + i + case["far"] for nq, n in zip(q, total) for i in range(nq)]
+    st["pos"] = torch.tensor(pos, dtype=torch.int64, device="cuda")
+    if case["far"]:
+        st["positions"] = st["pos"].to(torch.int32)
+    if case["op"] != "append" and case["mask"] != "causal":
+        lo, hi = _intervals(case, q, total)
+        st["lo"] = torch.tensor(lo, dtype=torch.int32, device="cuda")
+        st["hi"] = torch.tensor(hi, dtype=torch.int32, device="cuda")
+    if case["bias"]:
+        st["slopes"] = [2.0 ** (-8.0 * (h + 1) / H) for h in range(H)]
+    if own:
+        from paper_2609_35139_amd.serving import PagedCache
+        st["cache"] = PagedCache(pool)
+        st["seqs"] = st["cache"].sequences(st["table"], st["lens"], off)
+    return st
+
+
+def run(st):
+    c = st["case"]
+    if own:
+        if c["op"] == "append":
+            st["cache"].append(0, st["seqs"], st["kh"], st["vh"], q=st["qh"], q_out=st["out"],
+                               rope={"theta": THETA}, positions=st["positions"])
+            return [st["pool"], st["out"]]
+        st["cache"].attend(0, st["seqs"], st["qh"], out=st["out"], softcap=c["cap"],
+                           slopes=st["slopes"], lo=st["lo"], hi=st["hi"],
+                           shared_len=c["shared"] // c["page"] * c["page"])
+        return [st["out"]]
+    return _plain_append(st) if c["op"] == "append" else _plain_attend(st)
+
+
+def _plain_append(st):
+    c = st["case"]
+    half, ps = c["head_dim"] // 2, c["page"]
+    freq = THETA ** (-torch.arange(half, dtype=torch.float64, device="cuda") / half)
+    ang = st["pos"].to(torch.float64)[:, None] * freq
+    cos, sin = ang.cos().float()[:, None], ang.sin().float()[:, None]
+
+    def rotate(x):
+        a, b = x[..., :half].float(), x[..., half:].float()
+        return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).to(x.dtype)
+
+    slot = st["pos"] - c["far"]
+    seq = torch.repeat_interleave(torch.arange(len(st["q"]), device="cuda"),
+                                  torch.tensor(st["q"], device="cuda"))
+    block = st["table"][seq, slot // ps].long()
+    st["pool"][0, 0, block, slot % ps] = rotate(st["kh"])
+    st["pool"][0, 1, block, slot % ps] = st["vh"]
+    st["out"].copy_(rotate(st["qh"]))
+    return [st["pool"], st["out"]]
+
+
+def _plain_attend(st):
+    c = st["case"]
+    H, Hkv, d = c["heads"], c["kv_heads"], c["head_dim"]
+    G = H // Hkv
+    for s, (nq, n) in enumerate(zip(st["q"], st["total"])):
+        o = st["off"][s]
+        blocks = st["table"][s, :-(-n // c["page"])].long()
+        key = st["pool"][0, 0, blocks].reshape(-1, Hkv, d)[:n]
+        val = st["pool"][0, 1, blocks].reshape(-1, Hkv, d)[:n]
+        j = torch.arange(n, device="cuda")
+        p = torch.arange(n - nq, n, device="cuda")
+        if st["lo"] is None:
+            see = j[None] <= p[:, None]
+        else:
+            see = (j[None] >= st["lo"][o:o + nq, None]) & (j[None] < st["hi"][o:o + nq, None])
+        step = max(1, (1 << 30) // (G * nq * n))
+        for a in range(0, Hkv, step):                     # KV heads at a time
+            b = min(Hkv, a + step)
+            x = st["qh"][o:o + nq, a * G:b * G].float().transpose(0, 1).reshape(b - a, G * nq, d)
+            x = x @ key[:, a:b].float().permute(1, 2, 0).contiguous()
+            x = (x * (1.0 / math.sqrt(d))).view((b - a) * G, nq, n)
+            if c["cap"]:
+                x = c["cap"] * torch.tanh(x / c["cap"])
+            if st["slopes"] is not None:
+                slope = torch.tensor(st["slopes"][a * G:b * G], device="cuda")
+                x = x - slope[:, None, None] * (p[:, None] - j[None]).abs()
+            x = x.masked_fill(~see, -math.inf)
+            top = x.max(2, keepdim=True).values
+            w = (x - torch.where(top > -math.inf, top, torch.zeros_like(top))).exp()
+            w = w / w.sum(2, keepdim=True).clamp_min(1e-38)
+            y = w.view(b - a, G * nq, n) @ val[:, a:b].float().transpose(0, 1).contiguous()
+            st["out"][o:o + nq, a * G:b * G] = y.view(-1, nq, d).transpose(0, 1).to(st["out"].dtype)
+    return [st["out"]]
+
+
+def work(case):
+    """Each new token's q, k, v once in and once out; each cached key and value that some query
+    sees once in (the shared ones once for all), each query in and its output out; 4 d operations
+    for each pair of query head and key."""
+    q, cached = _lengths(case)
+    size = 4 if case["dtype"] == "f32" else 2
+    H, Hkv, d, N = case["heads"], case["kv_heads"], case["head_dim"], sum(q)
+    if case["op"] == "append":
+        return {"bytes": 2 * N * (H + 2 * Hkv) * d * size, "flops": 3 * N * (H + Hkv) * d}
+    total = [a + b for a, b in zip(q, cached)]
+    whole = case["shared"] // case["page"] * case["page"]
+    if case["mask"] == "causal":
+        pairs = sum(nq * (n - nq) + nq * (nq + 1) // 2 for nq, n in zip(q, total))
+        keys = whole + sum(n - whole for n in total)
+    else:
+        lo, hi = _intervals(case, q, total)
+        pairs = sum(b - a for a, b in zip(lo, hi))
+        keys, i = 0, 0
+        for nq in q:
+            seen = [(a, b) for a, b in zip(lo[i:i + nq], hi[i:i + nq]) if b > a]
+            keys += max(b for _, b in seen) - min(a for a, _ in seen) if seen else 0
+            i += nq
+    return {"bytes": size * d * (2 * N * H + 2 * keys * Hkv), "flops": 4 * d * H * pairs}
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    H, Hkv, d, ps = case["heads"], case["kv_heads"], case["head_dim"], case["page"]
+    pool = st["pool"][0].double()
+    if case["op"] == "append":
+        i = torch.arange(d // 2, dtype=torch.float64, device="cuda")
+        # a rotation of the complex numbers x_i + i x_(i + d/2)
+        turn = torch.polar(torch.ones_like(st["pos"], dtype=torch.float64)[:, None].expand(-1, d // 2).contiguous(),
+                           st["pos"].double()[:, None] * torch.exp(-math.log(THETA) * 2 * i / d))
+
+        def spin(x):
+            z = torch.complex(x[..., :d // 2].double(), x[..., d // 2:].double()) * turn[:, None]
+            return torch.cat([z.real, z.imag], -1)
+
+        k = spin(st["kh"])
+        for s in range(case["seqs"]):
+            a, b = st["off"][s], st["off"][s + 1]
+            at = range(st["total"][s] - (b - a), st["total"][s])
+            where = torch.tensor([st["rows"][s][t // ps] * ps + t % ps for t in at], device="cuda")
+            pool[0].view(-1, Hkv, d)[where] = k[a:b]
+            pool[1].view(-1, Hkv, d)[where] = st["vh"][a:b].double()
+        return [pool[None], spin(st["qh"])]
+    if work(case)["flops"] > 4e12:
+        return None
+    out = torch.zeros(sum(st["q"]), H, d, dtype=torch.float64, device="cuda")
+    slopes = torch.tensor(st["slopes"] or [0.0] * H, dtype=torch.float64, device="cuda")
+    for s in range(case["seqs"]):
+        n, nq = st["total"][s], st["q"][s]
+        where = torch.tensor([st["rows"][s][b] for b in range(-(-n // ps))], device="cuda")
+        kv = pool[:, where].flatten(1, 2)[:, :n].transpose(1, 2).contiguous()    # [2][Hkv][n][d]
+        step = max(1, (1 << 28) // (n * H))
+        for a in range(0, nq, step):
+            b = min(nq, a + step)
+            rows = slice(st["off"][s] + a, st["off"][s] + b)
+            x = st["qh"][rows].double().view(b - a, Hkv, -1, d).permute(1, 2, 0, 3)  # [Hkv][G][q][d]
+            z = (x.reshape(Hkv, -1, d) @ kv[0].transpose(1, 2).contiguous()) / d ** 0.5
+            z = z.view(H, b - a, n)
+            if case["cap"]:
+                z = torch.tanh(z / case["cap"]) * case["cap"]
+            here = torch.arange(n - nq + a, n - nq + b, device="cuda").double()[:, None]
+            key = torch.arange(n, device="cuda").double()[None]
+            z = z - slopes[:, None, None] * (here - key).abs()
+            if st["hi"] is None:
+                hidden = key > here
+            else:
+                hidden = (key < st["lo"][rows, None]) | (key >= st["hi"][rows, None])
+            z[:, hidden] = -math.inf
+            prob = torch.exp(z - torch.logsumexp(z, 2, keepdim=True))
+            prob[:, hidden.all(1)] = 0
+            y = prob.view(Hkv, -1, n) @ kv[1]
+            out[rows] = y.view(H, b - a, d).transpose(0, 1)
+    return [out]
