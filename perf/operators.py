@@ -91,9 +91,12 @@ def draw(rng):
     # about 12,000 new tokens and 400 MB of cached keys and values at most
     decode = rng.random() < 0.5
     q_hi = 1 if decode else _log(rng, 2, min(8192, 12000 // seqs))
+    pairs = int(1e12) // (4 * head_dim * heads)   # of a query and a key: about the prompt's work
+    while seqs * q_hi * q_hi > pairs // 2:
+        q_hi //= 2
     q_lo = rng.randint(1, q_hi)
     budget = (400 << 20) // (2 * kv_heads * head_dim * (4 if dtype == "f32" else 2)) // seqs
-    most = max(1, min(131072, budget, (1 << 32) // (seqs * q_hi * heads * (head_dim // 32))))
+    most = max(1, min(131072, budget, pairs // 2 // (seqs * q_hi)))
     shape = rng.randrange(1 << 30)
     more = {}
     if op == "append":
@@ -104,8 +107,8 @@ def draw(rng):
         more["cap"] = rng.choice([0.0, 0.0, 15.0, 50.0])
         more["bias"] = rng.random() < 0.3
     if op == "shared":
-        more["shared"] = _log(rng, 100, max(100, min(32768, most * seqs // 2)))
-        most = min(most, 1024)
+        more["shared"] = _log(rng, 100, max(100, min(32768, most // 2)))
+        most = min(max(1, most // 2), 1024)
     len_hi = _log(rng, min(16, most), most)
     return _case("drawn", op, (heads, kv_heads, head_dim), seqs, (q_lo, q_hi),
                  (rng.randint(0, len_hi), len_hi), shape, dtype=dtype, page=page, **more)
