@@ -461,8 +461,139 @@ CR_API cr_status cr_repair_static(void* kv, const cr_kv_layout* layout,
                                   const void* prepared, uint64_t prepared_bytes, void* stream);
 
 /*
+ * Answering over the cache.  Once a request's cache is repaired, the target
+ * model answers over it: in every layer the new tokens' keys and values are
+ * appended to the pages of their sequence, rotated to their positions
+ * (cr_append_kv), and the rotated queries attend to everything cached
+ * (cr_attend).  Both work on one layer of a paged cache (cr_kv_layout and the
+ * block geometry below, the cache that cr_repair_ex writes with pages or
+ * pages_out) for a batch of sequences.
+ *
+ * cr_sequences: the batch.  Sequence s has q_s new tokens, packed sequence by
+ * sequence: tokens [query_offsets[s], query_offsets[s + 1]) of the call.
+ * Its length kv_lens[s] counts them, so its new token i has cache slot
+ * kv_lens[s] - q_s + i, and slot j lies in block
+ * block_table[s * max_blocks + j / block_size], row j % block_size:
+ *   base + layer*stride_layer + kv*stride_kv + block*stride_block
+ *        + (j % block_size)*stride_token + h*stride_head + i.
+ *  query_offsets: host, n_seqs + 1 entries (first 0, non-decreasing; a
+ *                 sequence may have no new token), or NULL: one token each.
+ *  kv_lens:       device, n_seqs.  Read by the kernels alone, like
+ *                 block_table, so a captured call can be replayed with the
+ *                 lengths and tables of the next step (the offsets stay).
+ *  block_table:   device, n_seqs rows of max_blocks block ids; sequences may
+ *                 share blocks, but a block that a call appends to belongs to
+ *                 one sequence (which of two tokens stays in one row is
+ *                 undefined).  max_blocks * block_size < 2^31 - 256.
+ *  block_size, n_blocks, stride_block: as cr_kv_pages.
+ * The kernels never leave the cache: a length counts as at least 0 and at most
+ * max_blocks * block_size, and a block id outside [0, n_blocks) is no block
+ * (its keys are not seen, tokens appended to it are dropped).
+ *
+ * cr_rows: a [n_tokens][heads][head_dim] operand in device memory, storage
+ * dtype, dim stride 1; strides in elements, multiples of 8, not negative; base
+ * 16-byte aligned.  Query, key and value may lie side by side in one
+ * projection's output.  Rows that are written must not overlap each other.
+ */
+typedef struct {
+    int32_t n_seqs;
+    const int32_t* query_offsets;
+    const int32_t* kv_lens;
+    const int32_t* block_table;
+    int32_t max_blocks;
+    int32_t block_size;
+    int32_t n_blocks;
+    int64_t stride_block;
+} cr_sequences;
+
+typedef struct {
+    void* data;
+    int64_t stride_token, stride_head;
+} cr_rows;
+
+/*
+ * Appends the new tokens of a batch to layer `layer` of a paged cache:
+ *   K[slot] = R(p) k,   V[slot] = v,   q_out = R(p) q
+ * with R the rotation of cr_rope (angles in fp64, products in fp32, rounded
+ * once) and p the token's position.  Rows of the cache that are no new token's
+ * slot keep what they hold.
+ *  k, v:       [n_tokens][n_kv_heads][head_dim].
+ *  q, q_out:   [n_tokens][n_heads][head_dim], or both NULL (n_heads ignored).
+ *              q_out may be q itself (same data and strides); otherwise
+ *              neither it nor the cache may overlap an input.
+ *  rope:       NULL = nothing is rotated, everything is copied as it is.
+ *  positions:  device, n_tokens int32, or NULL: the token's slot.  A cache
+ *              that holds only what follows a preamble kept elsewhere takes
+ *              slot + preamble length.
+ * A new token without a slot (a negative one, one past the table, or one in no
+ * block) is dropped; its query is rotated all the same.
+ * n_tokens == 0 returns CR_OK with nothing enqueued.
+ * Errors: CR_ERR_NULL, CR_ERR_DIMS (dims, layer, heads, rope), CR_ERR_DTYPE,
+ * CR_ERR_OFFSETS (query_offsets, n_seqs), CR_ERR_LAYOUT (strides, alignment,
+ * block geometry), CR_ERR_DEVICE before any enqueue; CR_ERR_LAUNCH.
+ */
+CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t layer,
+                       const cr_sequences* seqs, const cr_rows* k, const cr_rows* v,
+                       const cr_rows* q, const cr_rows* q_out, int32_t n_heads,
+                       const cr_rope* rope, const int32_t* positions, void* stream);
+
+/*
+ * Options of cr_attend.
+ *  scale:      factor of q.k, > 0 (0 = 1 / sqrt(head_dim)).
+ *  softcap:    0, or > 0: scores become softcap * tanh(score / softcap).
+ *  slopes:     NULL, or host, n_heads entries: slopes[h] * |p - j| is taken off
+ *              the score of the query in slot p and the key in slot j.
+ *  lo, hi:     device, n_tokens int32 each, or NULL: query t sees the keys in
+ *              slots [lo[t], hi[t]) of its sequence (within the sequence's
+ *              length).  lo NULL = 0; hi NULL = causal, up to the query's own
+ *              slot.  Documents, a bidirectional prefix, windows.
+ *  shared_len: the first shared_len slots of every sequence are in the same
+ *              blocks (those of sequence 0's row of the table), whose keys are
+ *              then read once for the whole batch; at most max_blocks *
+ *              block_size.  Changes no result but for rounding.  A sequence may
+ *              be shorter.
+ *  lse:        NULL, or device, [n_tokens][n_heads] fp32: the logarithm of the
+ *              sum of exponentials of every row's scores.
+ */
+typedef struct {
+    float scale;
+    float softcap;
+    const float* slopes;
+    const int32_t* lo;
+    const int32_t* hi;
+    int32_t shared_len;
+    float* lse;
+} cr_attend_options;
+
+/*
+ * Attention of the batch's new tokens over layer `layer` of a paged cache that
+ * holds them already:
+ *   out[t, h] = sum_j softmax_j(score(q[t, h], K_j[h / g])) V_j[h / g],
+ *   g = n_heads / n_kv_heads,
+ * over the keys that the query sees.  A query that sees none gets zeros (lse
+ * -inf); what lies in keys and values that it does not see, infinities and
+ * NaN among them, does not matter.  Scores, softmax and sums are fp32; bf16
+ * caches round the probabilities to bf16 for the product with V.
+ *  q, out:    [n_tokens][n_heads][head_dim]; n_heads a multiple of n_kv_heads,
+ *             at most 256.  out must not overlap q or the cache.
+ *  options:   NULL = causal, scale 1 / sqrt(head_dim).
+ *  workspace: device scratch of cr_attend_workspace_bytes for the same
+ *             arguments, 256-byte aligned; contents undefined after the call.
+ *             Calls that may overlap in time need their own.
+ * n_tokens == 0 returns CR_OK with nothing enqueued.
+ * Errors as cr_append_kv; CR_ERR_DIMS also for options outside their ranges,
+ * CR_ERR_WORKSPACE.
+ */
+CR_API cr_status cr_attend_workspace_bytes(const cr_kv_layout* layout, const cr_sequences* seqs,
+                                    int32_t n_heads, int32_t shared_len, uint64_t* bytes);
+CR_API cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t layer,
+                    const cr_sequences* seqs, const cr_rows* q, const cr_rows* out,
+                    int32_t n_heads, const cr_attend_options* options, void* workspace,
+                    uint64_t workspace_bytes, void* stream);
+
+/*
  * Per-launch timing (tracing aid, not needed for repair).  While enabled,
- * cr_repair brackets every kernel launch with HIP events recorded on the
+ * cr_repair, cr_append_kv and cr_attend bracket every kernel launch with HIP events recorded on the
  * call's own stream.  cr_profile_enable(max_launches) creates the events
  * (host-side allocation happens here, never inside cr_repair);
  * max_launches = 0 disables profiling and destroys them.  Launches beyond

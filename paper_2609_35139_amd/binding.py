@@ -32,7 +32,7 @@ EXPORTS = ["cr_version", "cr_status_string", "cr_weights_layout", "cr_prepared_b
            "cr_default_options", "cr_repair_ex", "cr_rotate_workspace_bytes", "cr_rotate_keys",
            "cr_pipeline_create", "cr_pipeline_destroy", "cr_pipeline_staging_bytes",
            "cr_repair_pipelined", "cr_workspace_view", "cr_profile_enable", "cr_profile_read",
-           "cr_repair_static"]
+           "cr_repair_static", "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend"]
 CR_STATIC_SCRATCH_BYTES = 128 << 20
 CR_MASK = {"block_causal": 0, "token_causal": 1, "bidirectional": 2, "block_diagonal": 3}
 CR_APPLY = {"kv": 0, "k": 1, "v": 2}
@@ -79,6 +79,21 @@ class cr_pipeline_item(ctypes.Structure):
                 ("chunk_offsets", POINTER(c_int32)), ("n_chunks", c_int32),
                 ("position_offset", c_int32), ("kv_out", c_void_p),
                 ("layout_out", POINTER(cr_kv_layout)), ("pages_out", POINTER(cr_kv_pages))]
+
+
+class cr_sequences(ctypes.Structure):
+    _fields_ = [("n_seqs", c_int32), ("query_offsets", POINTER(c_int32)), ("kv_lens", c_void_p),
+                ("block_table", c_void_p), ("max_blocks", c_int32), ("block_size", c_int32),
+                ("n_blocks", c_int32), ("stride_block", c_int64)]
+
+
+class cr_rows(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("stride_token", c_int64), ("stride_head", c_int64)]
+
+
+class cr_attend_options(ctypes.Structure):
+    _fields_ = [("scale", c_float), ("softcap", c_float), ("slopes", POINTER(c_float)),
+                ("lo", c_void_p), ("hi", c_void_p), ("shared_len", c_int32), ("lse", c_void_p)]
 
 
 class cr_kernel_stat(ctypes.Structure):
@@ -137,11 +152,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                       P(c_uint64), P(c_int64)]
     lib.cr_profile_enable.argtypes = [c_int32]
     lib.cr_profile_read.argtypes = [P(cr_kernel_stat), c_int32, P(c_int32)]
+    lib.cr_append_kv.argtypes = [c_void_p, P(cr_kv_layout), c_int32, P(cr_sequences), P(cr_rows),
+                                 P(cr_rows), P(cr_rows), P(cr_rows), c_int32, P(cr_rope), c_void_p,
+                                 c_void_p]
+    lib.cr_attend_workspace_bytes.argtypes = [P(cr_kv_layout), P(cr_sequences), c_int32, c_int32,
+                                              P(c_uint64)]
+    lib.cr_attend.argtypes = [c_void_p, P(cr_kv_layout), c_int32, P(cr_sequences), P(cr_rows),
+                              P(cr_rows), c_int32, P(cr_attend_options), c_void_p, c_uint64,
+                              c_void_p]
     for name in ["cr_weights_layout", "cr_prepared_bytes", "cr_prepare_weights",
                  "cr_workspace_bytes", "cr_chunk_schedule", "cr_repair", "cr_repair_ex",
                  "cr_rotate_workspace_bytes", "cr_rotate_keys", "cr_pipeline_create",
                  "cr_pipeline_destroy", "cr_pipeline_staging_bytes", "cr_repair_pipelined",
-                 "cr_workspace_view", "cr_profile_enable", "cr_profile_read", "cr_repair_static"]:
+                 "cr_workspace_view", "cr_profile_enable", "cr_profile_read", "cr_repair_static",
+                 "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend"]:
         getattr(lib, name).restype = c_int32
     _lib = lib
     return lib
@@ -409,6 +433,47 @@ def cr_repair_pipelined(handle: int, items: Sequence[dict], dims: cr_dims, layou
                                       ctypes.byref(o) if o is not None else None, copy_stream,
                                       compute_stream), "cr_repair_pipelined")
     del keep
+
+
+def sequences_struct(n_seqs, kv_lens, block_table, max_blocks, block_size, n_blocks, stride_block,
+                     query_offsets=None):
+    """(cr_sequences, keep-alive): kv_lens and block_table are device addresses,
+    query_offsets a host sequence of n_seqs + 1 or None (one token each)."""
+    off = None
+    q = cr_sequences()
+    if query_offsets is not None:
+        off = np.ascontiguousarray(query_offsets, dtype=np.int32)
+        if off.shape != (n_seqs + 1,):
+            raise ValueError("query_offsets needs one entry more than there are sequences")
+        q.query_offsets = off.ctypes.data_as(POINTER(c_int32))
+    q.n_seqs, q.kv_lens, q.block_table = n_seqs, kv_lens, block_table
+    q.max_blocks, q.block_size, q.n_blocks = max_blocks, block_size, n_blocks
+    q.stride_block = stride_block
+    return q, off
+
+
+def cr_append_kv(kv: int, layout: cr_kv_layout, layer: int, seqs: cr_sequences, k: cr_rows,
+                 v: cr_rows, q: Optional[cr_rows], q_out: Optional[cr_rows], n_heads: int,
+                 rope: Optional[cr_rope], positions: Optional[int],
+                 stream: Optional[int] = None) -> None:
+    _check(load().cr_append_kv(kv, layout, layer, seqs, k, v, q, q_out, n_heads, rope, positions,
+                               stream), "cr_append_kv")
+
+
+def cr_attend_workspace_bytes(layout: cr_kv_layout, seqs: cr_sequences, n_heads: int,
+                              shared_len: int = 0) -> int:
+    b = c_uint64(0)
+    _check(load().cr_attend_workspace_bytes(layout, seqs, n_heads, shared_len, ctypes.byref(b)),
+           "cr_attend_workspace_bytes")
+    return b.value
+
+
+def cr_attend(kv: int, layout: cr_kv_layout, layer: int, seqs: cr_sequences, q: cr_rows,
+              out: cr_rows, n_heads: int, options: Optional[cr_attend_options],
+              workspace: Optional[int], workspace_bytes: int,
+              stream: Optional[int] = None) -> None:
+    _check(load().cr_attend(kv, layout, layer, seqs, q, out, n_heads, options, workspace,
+                            workspace_bytes, stream), "cr_attend")
 
 
 def cr_workspace_view(dims: cr_dims, layout: cr_kv_layout, n_tokens: int,

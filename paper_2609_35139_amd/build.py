@@ -12,11 +12,13 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["api.hip", "gemm.hip", "attention.hip", "rowops.hip"]
-# Per-source code generation options.  The attention kernel's score and
+SOURCES = ["api.hip", "gemm.hip", "attention.hip", "rowops.hip", "serve.hip", "append.hip",
+           "attend_bf16.hip", "attend_f32.hip"]
+# Per-source code generation options.  The attention kernels' score and
 # output accumulators are read by VALU code every key tile; keeping MFMA
 # operands in VGPRs avoids a copy out of the accumulation registers per tile.
-EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+         for src in ("attention.hip", "attend_bf16.hip", "attend_f32.hip")}
 LIB = os.path.join(HERE, "libcacherepair.so")
 ARCH = "gfx950"
 CFLAGS = [

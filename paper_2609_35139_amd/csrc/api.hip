@@ -12,7 +12,9 @@
 #include <vector>
 
 #include "launch.h"
+#include "profile.h"
 #include "rules.h"
+#include "validate.h"
 
 namespace cr {
 LaunchEvents& launch_events() {
@@ -23,30 +25,9 @@ LaunchEvents& launch_events() {
 
 namespace {
 
-using cr::bf16;
-using cr::LaunchEvents;
-using cr::launch_events;
-
-constexpr uint64_t ALIGN = 256;
-inline uint64_t align_up(uint64_t x, uint64_t a = ALIGN) { return (x + a - 1) / a * a; }
-inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-
-struct Arena {
-  uint64_t off = 0;
-  uint64_t take(uint64_t bytes) {
-    const uint64_t o = off;
-    off = align_up(off + bytes);
-    return o;
-  }
-};
-
-inline size_t esize(int dtype) { return dtype == CR_DTYPE_F32 ? 4 : 2; }
+using namespace cr;   // the helpers of validate.h and profile.h
 
 // ------------------------------------------------------------ validation
-cr_status check_dtype(const cr_kv_layout* l) {
-  return (l->dtype == CR_DTYPE_BF16 || l->dtype == CR_DTYPE_F32) ? CR_OK : CR_ERR_DTYPE;
-}
-
 cr_status check_dims(const cr_dims* d, const cr_kv_layout* l) {
   if (!d || !l) return CR_ERR_NULL;
   cr_status st = check_dtype(l);
@@ -68,79 +49,6 @@ cr_status check_dims(const cr_dims* d, const cr_kv_layout* l) {
   return CR_OK;
 }
 
-// Injective index map over (stride, extent) pairs: with the dims sorted by
-// stride, each stride must exceed the largest offset reachable through the
-// dims inside it.  The largest offset must also stay below 2^62 elements, so
-// that no element offset a kernel forms in int64 can overflow.
-struct Dim { int64_t s, e; };
-// At most six (stride, extent) pairs: dim, head, token, (block,) K/V, layer.
-// Fixed capacity, so validating a call allocates nothing.
-struct Dims {
-  Dim d[6];
-  int n = 0;
-  void push_back(Dim x) { d[n++] = x; }
-};
-cr_status check_injective(Dims dims) {
-  std::sort(dims.d, dims.d + dims.n, [](const Dim& a, const Dim& b) { return a.s < b.s; });
-  int64_t reach = 0;  // largest offset reachable by the dims visited so far
-  for (int i = 0; i < dims.n; ++i) {
-    const Dim& x = dims.d[i];
-    if (x.s <= reach) return CR_ERR_LAYOUT;
-    int64_t span;
-    if (__builtin_mul_overflow(x.s, x.e - 1, &span) || __builtin_add_overflow(reach, span, &reach) ||
-        reach >= ((int64_t)1 << 62))
-      return CR_ERR_LAYOUT;
-  }
-  return CR_OK;
-}
-
-cr_status check_layout(const cr_kv_layout* l, int64_t n_tokens) {
-  const int64_t st[4] = {l->stride_layer, l->stride_kv, l->stride_token, l->stride_head};
-  const int64_t ext[4] = {l->n_layers, 2, n_tokens, l->n_kv_heads};
-  Dims dims;
-  dims.push_back({1, l->head_dim});
-  for (int i = 0; i < 4; ++i) {
-    if (st[i] < 0 || st[i] % 8 != 0) return CR_ERR_LAYOUT;
-    if (ext[i] > 1) dims.push_back({st[i], ext[i]});
-  }
-  if (n_tokens == 0) return CR_OK;  // no element is addressed
-  return check_injective(dims);
-}
-
-// Injectivity of a paged layout over (layer, kv, block, row, head, dim) and
-// validity of the host block table for n_tokens tokens.
-cr_status check_pages(const cr_kv_layout* l, const cr_kv_pages* pg, int64_t n_tokens) {
-  const int bs = pg->block_size;
-  if (bs < 1 || bs > 1024 || (bs & (bs - 1)) || pg->n_blocks < 1) return CR_ERR_LAYOUT;
-  if (pg->stride_block < 0 || pg->stride_block % 8) return CR_ERR_LAYOUT;
-  const int64_t st[5] = {l->stride_layer, l->stride_kv, pg->stride_block, l->stride_token,
-                         l->stride_head};
-  const int64_t ext[5] = {l->n_layers, 2, pg->n_blocks, bs, l->n_kv_heads};
-  Dims dims;
-  dims.push_back({1, l->head_dim});
-  for (int i = 0; i < 5; ++i) {
-    if (st[i] < 0 || st[i] % 8 != 0) return CR_ERR_LAYOUT;
-    if (ext[i] > 1) dims.push_back({st[i], ext[i]});
-  }
-  const cr_status inj = check_injective(dims);
-  if (inj != CR_OK) return inj;
-  const int64_t nb = (n_tokens + bs - 1) / bs;
-  if (nb == 0) return CR_OK;
-  if (!pg->block_table) return CR_ERR_NULL;
-  std::vector<int32_t> ids(pg->block_table, pg->block_table + nb);
-  for (int32_t b : ids)
-    if (b < 0 || b >= pg->n_blocks) return CR_ERR_LAYOUT;
-  std::sort(ids.begin(), ids.end());
-  if (std::adjacent_find(ids.begin(), ids.end()) != ids.end()) return CR_ERR_LAYOUT;
-  return CR_OK;
-}
-
-int log2_int(int x) {
-  int s = 0;
-  while ((1 << s) < x) ++s;
-  return s;
-}
-
 cr_status check_offsets(const int32_t* off, int32_t n_chunks, const int32_t* req,
                         int32_t n_req) {
   if (!off) return CR_ERR_NULL;
@@ -156,29 +64,6 @@ cr_status check_offsets(const int32_t* off, int32_t n_chunks, const int32_t* req
   return CR_OK;
 }
 
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// Target rotary encoding: frequencies in fp64 from theta or the caller's
-// table.  Returns CR_ERR_DIMS for a non-finite or non-positive field.
-cr_status key_rope_of(const cr_rope* r, int head_dim, cr::KeyRope* kr) {
-  if (!r || head_dim / 2 > 128) return CR_ERR_DIMS;
-  if (!(r->scale > 0.f) || !std::isfinite(r->scale)) return CR_ERR_DIMS;
-  kr->half = head_dim / 2;
-  kr->scale = r->scale;
-  for (int i = 0; i < kr->half; ++i) {
-    double f;
-    if (r->inv_freq) {
-      f = r->inv_freq[i];
-    } else {
-      if (!(r->theta > 0.0) || !std::isfinite(r->theta)) return CR_ERR_DIMS;
-      f = std::pow(r->theta, -2.0 * i / (double)head_dim);
-    }
-    if (!std::isfinite(f)) return CR_ERR_DIMS;
-    kr->f[i] = f;
-  }
-  return CR_OK;
-}
-
 // Global positions p_t = position_offset[r] + (t - first token of r) must lie
 // in [0, 2^31 - 1).
 cr_status check_positions(const int32_t* off, int32_t n_chunks, const int32_t* req,
@@ -190,19 +75,6 @@ cr_status check_positions(const int32_t* off, int32_t n_chunks, const int32_t* r
     if (o < 0 || o + len >= ((int64_t)1 << 31) - 1) return CR_ERR_OFFSETS;
   }
   return CR_OK;
-}
-
-cr_status check_device() {
-  static std::atomic<int> ok[64];  // per device: 0 unknown, 1 gfx950, -1 not
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return CR_ERR_DEVICE;
-  const int known = dev < 64 ? ok[dev].load(std::memory_order_relaxed) : 0;
-  if (known) return known > 0 ? CR_OK : CR_ERR_DEVICE;
-  hipDeviceProp_t prop;
-  if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return CR_ERR_DEVICE;
-  const bool good = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0;
-  if (dev < 64) ok[dev].store(good ? 1 : -1, std::memory_order_relaxed);
-  return good ? CR_OK : CR_ERR_DEVICE;
 }
 
 // ------------------------------------------------------------- layouts
@@ -352,55 +224,6 @@ Workspace workspace_layout(const cr_dims* d, const cr_kv_layout* l, int64_t N) {
   w.total = a.off;
   return w;
 }
-
-// ------------------------------------------------------------- profiling
-struct Profiler {
-  std::mutex mu;
-  std::vector<hipEvent_t> ev;        // 2 per launch slot
-  std::vector<std::string> cls;      // class of each used slot
-  std::vector<char> valid;           // the slot's events were recorded
-  int used = 0;
-  std::atomic<bool> on{false};       // read without the lock on every launch
-};
-Profiler& prof() {
-  static Profiler p;
-  return p;
-}
-
-// Launch `f` on stream s, bracketed by events when profiling is enabled.
-// While a slot is in use the profiler's lock is held, so a concurrent
-// cr_profile_enable cannot destroy its events; a stage that fails leaves its
-// slot marked invalid (its events may never be recorded).
-template <typename F>
-hipError_t timed(const char* name, hipStream_t s, F&& f) {
-  Profiler& P = prof();
-  if (!P.on) return f();
-  std::unique_lock<std::mutex> g(P.mu);
-  if (!P.on || P.used >= (int)P.ev.size() / 2) {
-    g.unlock();
-    return f();
-  }
-  const int slot = P.used++;
-  P.cls.emplace_back(name);
-  P.valid.push_back(0);
-  const hipEvent_t e0 = P.ev[2 * slot], e1 = P.ev[2 * slot + 1];
-  LaunchEvents& le = launch_events();
-  le.start = e0;
-  le.stop = e1;
-  hipError_t e = f();
-  if (e == hipSuccess && le.start) {   // the stage launched nothing: an empty interval
-    e = hipEventRecord(e0, s);
-    if (e == hipSuccess) e = hipEventRecord(e1, s);
-  }
-  le = LaunchEvents{};
-  P.valid[slot] = e == hipSuccess;
-  return e;
-}
-
-#define CR_TRY(...)                                 \
-  do {                                            \
-    if ((__VA_ARGS__) != hipSuccess) return CR_ERR_LAUNCH; \
-  } while (0)
 
 template <typename T>
 cr_status prepare_impl(const cr_dims* d, const cr_kv_layout* l, const char* blob, char* out,

@@ -1,0 +1,7 @@
+// Attention over a paged cache, f32 storage.
+#include "attend_kernel.h"
+
+namespace cr {
+template hipError_t attend<float>(const AttendArgs&, hipStream_t);
+template hipError_t attend_merge<float>(const AttendArgs&, const AttendArgs&, hipStream_t);
+}  // namespace cr

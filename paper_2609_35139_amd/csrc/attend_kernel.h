@@ -1,0 +1,749 @@
+// Attention from new queries to a paged cache (gfx950 MFMA).
+//
+// Row (t, h) of query t and head h sees the positions j of its sequence with
+// lo(t) <= j < hi(t); hi is t's own position + 1 unless the caller gives it:
+//   x_j = scale * q.k_j;  x_j = cap * tanh(x_j / cap);  x_j -= slope_h |p_t - j|
+//   o = sum_j exp(x_j - m) v_j / l,  l = sum_j exp(x_j - m),  lse = m + log l.
+// A row that sees nothing has o = 0 and lse = -inf.
+//
+// The heads of a group share their keys, so a workgroup's tile packs rows
+// (query, head of the group) of one sequence and one KV head: row r is query
+// r / group.  A tile walks its keys once with a running maximum and sum; where
+// there are few tiles the keys are split among several workgroups, whose
+// (max, sum, unnormalised o) a second kernel joins.  The lengths are known on
+// the device alone (a captured launch is replayed as they grow), so every
+// workgroup derives the split from them, see plan_item.
+//
+// Keys and values are staged in LDS as they lie in the pages (16-byte
+// global->LDS transfers whose addresses come from the block list of the
+// segment, itself in LDS).  Scores are formed transposed, S^T = K Q^T, in
+// 16x16 atoms: a lane holds four consecutive keys of one row, so maximum and
+// sum are register work plus two exchanges, and the probabilities are already
+// the B operand of O^T = V^T P^T.  Its A operand needs four consecutive keys
+// of one dim per lane: for bf16 the LDS reads that transpose 16-bit elements
+// deliver that from the row-major tile.
+#pragma once
+#include "serve.h"
+
+namespace cr {
+
+constexpr int kPlanTile = 64;     // keys per tile of the split's arithmetic
+constexpr int kListPages = 512;   // pages of a segment's block list
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ------------------------------------------------------------ units and rows
+__device__ __forceinline__ int seq_len(const PagedSeqs& p, int s) {
+  const int n = p.lens[s];
+  return min(max(n, 0), p.max_len);
+}
+// largest i with off[i] <= x, i < n
+__device__ __forceinline__ int find_offset(const int* off, int n, int x) {
+  int a = 0, b = n;
+  while (b - a > 1) {
+    const int mid = (a + b) >> 1;
+    if (off[mid] <= x) a = mid; else b = mid;
+  }
+  return a;
+}
+struct Unit {
+  int s, tile;       // sequence and its row tile
+  int tok0, nq;      // the sequence's first query and number of queries
+};
+__device__ __forceinline__ Unit unit_of(const AttendArgs& a, int u) {
+  Unit x;
+  if (a.unit_off) {
+    x.s = find_offset(a.unit_off, a.seqs.n_seqs, u);
+    x.tile = u - a.unit_off[x.s];
+    x.tok0 = a.q_off[x.s];
+    x.nq = a.q_off[x.s + 1] - x.tok0;
+  } else {
+    x.s = u / a.units_per_seq;
+    x.tile = u - x.s * a.units_per_seq;
+    x.tok0 = x.s * a.q_per_seq;
+    x.nq = a.q_per_seq;
+  }
+  return x;
+}
+// One past the last position that a unit's queries may see.
+__device__ __forceinline__ int unit_end(const AttendArgs& a, const Unit& x) {
+  const int n = seq_len(a.seqs, x.s);
+  if (a.hi) return n;
+  const int last = min(((x.tile + 1) * a.rows - 1) / a.group, x.nq - 1);
+  return n - (x.nq - 1 - last);
+}
+__device__ __forceinline__ int unit_tiles(const AttendArgs& a, int u) {
+  return (max(unit_end(a, unit_of(a, u)) - a.key_begin, 0) + kPlanTile - 1) / kPlanTile;
+}
+// Positions [lo, hi) that query i of a sequence (token t) sees in this pass.
+__device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, int i, int t) {
+  int hi = min(a.hi ? a.hi[t] : n - nq + i + 1, n);
+  int lo = a.lo ? max(a.lo[t], 0) : 0;
+  if (a.shared) hi = min(hi, a.shared);
+  else lo = max(lo, a.key_begin);
+  return make_int2(lo, hi);
+}
+
+// ------------------------------------------------------------------- split
+// Item `it` of the split: unit, part, number of the unit's parts, tiles per
+// part, and the unit's first item.  Every unit has at least one part; a part is
+// `chunk` tiles, the mean load of a.slots workgroups, so there are at most
+// a.slots + n_units items.  The same in every wave of every workgroup (the
+// merge asks with a unit instead of an item).
+struct Item { int unit, part, parts, chunk, first; };
+__device__ __forceinline__ int wave_sum_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ Item plan_item(const AttendArgs& a, int it, int unit) {
+  const int lane = threadIdx.x & 63;
+  const int U = a.n_units;
+  const int t0 = lane < U ? unit_tiles(a, lane) : 0;   // the first 64 units stay in registers
+  auto tiles = [&](int u0) {
+    return u0 == 0 ? t0 : (u0 + lane < U ? unit_tiles(a, u0 + lane) : 0);
+  };
+  float total = 0.f;   // (a chunk need not be exact, only the same everywhere)
+  for (int u0 = 0; u0 < U; u0 += 64) {
+    int v = tiles(u0) >> 3;                             // sums of 64 stay below 2^31
+    total += 8.f * (float)wave_sum_i(v) + (float)wave_sum_i(tiles(u0) & 7);
+  }
+  const int chunk = max(a.min_tiles, (int)fminf(total / (float)a.slots + 1.f, 1e9f));
+  Item r{-1, 0, 1, chunk, 0};
+  int base = 0;
+  for (int u0 = 0; u0 < U; u0 += 64) {
+    const int t = tiles(u0);
+    const int n = u0 + lane < U ? max(1, (int)(((int64_t)t + chunk - 1) / chunk)) : 0;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(incl, o);
+      if (lane >= o) incl += x;
+    }
+    const bool mine = unit >= 0 ? u0 + lane == unit : (n > 0 && base + incl > it);
+    const unsigned long long hit = __ballot(mine);
+    if (hit) {
+      const int l = __ffsll(hit) - 1;
+      r.unit = u0 + l;
+      r.parts = __shfl(n, l);
+      r.first = base + __shfl(incl, l) - r.parts;
+      r.part = it - r.first;
+      break;
+    }
+    base += __shfl(incl, 63);
+  }
+  r.unit = __builtin_amdgcn_readfirstlane(r.unit);
+  r.part = __builtin_amdgcn_readfirstlane(r.part);
+  r.parts = __builtin_amdgcn_readfirstlane(r.parts);
+  r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
+  r.first = __builtin_amdgcn_readfirstlane(r.first);
+  return r;
+}
+
+// ------------------------------------------------------------- type specifics
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Rows of RB bytes in 16-byte chunks; chunk c of row r lies in slot
+// c ^ f(r), f periodic in 16 rows, so that the 16 rows of a fragment read and
+// the four rows of a transposing read start in distinct banks.
+template <int RB>
+__device__ __forceinline__ int row_swizzle(int row) {
+  constexpr int CPR = RB / 16;
+  if constexpr (RB >= 256) return row & 15;
+  else return (row / (256 / RB)) & (CPR - 1);
+}
+template <int RB>
+__device__ __forceinline__ int row_offset(int row, int chunk) {
+  return row * RB + ((chunk ^ row_swizzle<RB>(row)) << 4);
+}
+
+// tanh(x): for bf16 through one exponential and a reciprocal (absolute error
+// about 2^-22, far below a bf16 score's own), for fp32 the library's.
+template <typename T> __device__ __forceinline__ float tanh_of(float x);
+template <> __device__ __forceinline__ float tanh_of<float>(float x) { return tanhf(x); }
+template <> __device__ __forceinline__ float tanh_of<bf16>(float x) {
+  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));   // inf for large x: 1 - 0
+  return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+}
+
+// Keys of a PV atom, its V fragment from the row-major tile and the split of a
+// fragment into finite values and indicators of +inf and -inf (NaN: both).
+template <typename T> struct ValueOps;
+template <> struct ValueOps<bf16> {
+  typedef bf16x8 frag;
+  static constexpr int KEYS = 32;       // keys contracted by one atom: two 16-key sub-tiles
+  // lane (g, i): dims d0 + i, keys key0 + 4 g + [0, 4) and key0 + 16 + 4 g + [0, 4).
+  // A transposing read takes 8 bytes per lane: of 16 lanes, lanes 4 r .. 4 r + 3
+  // hold row r's 16 elements and lane i receives element i of the four rows.
+  template <int RB>
+  __device__ __forceinline__ static frag load(const char* tile, int key0, int d0, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    const int row = key0 + 4 * g + (i >> 2);
+    const int byte = (d0 + (i & 3) * 4) * 2;
+    const char* p = tile + row_offset<RB>(row, byte >> 4) + (byte & 15);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * RB));
+    frag r;
+    *reinterpret_cast<s16x4*>(&r) = lo;
+    *(reinterpret_cast<s16x4*>(&r) + 1) = hi;
+    return r;
+  }
+  __device__ __forceinline__ static bool finite(const frag& v) {
+    const u16x8 b = __builtin_bit_cast(u16x8, v);   // (of the whole: an element's cast reads element 0)
+    int bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= (b[e] & 0x7f80) == 0x7f80;
+    return !bad;
+  }
+  __device__ __forceinline__ static void split(const frag& v, frag* f, frag* pos, frag* neg) {
+    const u16x8 bits = __builtin_bit_cast(u16x8, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint16_t b = bits[e];
+      const bool bad = (b & 0x7f80) == 0x7f80, nan = bad && (b & 0x7f);
+      (*f)[e] = bad ? (bf16)0.f : v[e];
+      (*pos)[e] = (bf16)(nan || (bad && !(b & 0x8000)) ? 1.f : 0.f);
+      (*neg)[e] = (bf16)(nan || (bad && (b & 0x8000)) ? 1.f : 0.f);
+    }
+  }
+};
+template <> struct ValueOps<float> {
+  typedef f32x4 frag;
+  static constexpr int KEYS = 16;
+  template <int RB>
+  __device__ __forceinline__ static frag load(const char* tile, int key0, int d0, int lane) {
+    const int d = d0 + (lane & 15), g = lane >> 4;
+    frag r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = key0 + 4 * g + e;
+      r[e] = *reinterpret_cast<const float*>(tile + row_offset<RB>(row, d >> 2) + (d & 3) * 4);
+    }
+    return r;
+  }
+  __device__ __forceinline__ static bool finite(const frag& v) {
+    int bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u;
+    return !bad;
+  }
+  __device__ __forceinline__ static void split(const frag& v, frag* f, frag* pos, frag* neg) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t b = __float_as_uint(v[e]);
+      const bool bad = (b & 0x7f800000u) == 0x7f800000u, nan = bad && (b & 0x7fffffu);
+      (*f)[e] = bad ? 0.f : v[e];
+      (*pos)[e] = nan || (bad && !(b >> 31)) ? 1.f : 0.f;
+      (*neg)[e] = nan || (bad && (b >> 31)) ? 1.f : 0.f;
+    }
+  }
+};
+
+// maximum and sum over the four lanes that hold one row (l, l^16, l^32, l^48)
+__device__ __forceinline__ float row_max(float x) {
+  const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return halves_max(fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return halves_sum(__uint_as_float(v[0]) + __uint_as_float(v[1]));
+}
+
+// ------------------------------------------------------------------ kernel
+// RG * KG waves: KG groups of RG waves walk alternate tiles of KT keys, each
+// with its own ring of STAGES tiles; the RG waves of a group own 16 * NQ rows
+// each.  DM: head_dim (EXACT) or an upper bound of it.
+template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES>
+struct AttendCfg {
+  static constexpr int WAVES = RG * KG, NT = 64 * WAVES, ROWS = 16 * NQ * RG;
+  static constexpr int RB = DM * (int)sizeof(T), CPR = RB / 16, RPW = 1024 / RB;
+  static constexpr int TILE = KT * RB;                    // bytes of a K or V tile
+  static constexpr int ROUNDS = TILE / (RG * 1024);       // transfers per wave and tile
+  static constexpr int RING = STAGES * 2 * TILE;
+  static constexpr int MLD = DM + 4;                      // merge rows, in floats
+  static constexpr int MERGE = KG > 1 ? KG * ROWS * (MLD + 2) * 4 : 0;
+  static constexpr int LDS = KG * RING > MERGE ? KG * RING : MERGE;
+  static_assert(ROUNDS * RG * 1024 == TILE && RPW >= 1 && KT % ValueOps<T>::KEYS == 0, "tile");
+  static_assert(LDS + kListPages * 8 + 64 <= 160 * 1024, "LDS");
+  static_assert(2 * ROUNDS * (STAGES - 1) < 64, "transfers in flight");
+  static_assert(KT <= 128 && KT * KG < kListPages, "bits of a lane's scores, keys of a list");
+};
+
+template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES>
+__global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
+  using C = AttendCfg<T, DM, EXACT, NQ, RG, KG, KT, STAGES>;
+  using MM = Mma16<T>;
+  using VO = ValueOps<T>;
+  using frag = typename MM::frag;
+  constexpr int KPL = MM::KPL, KSTEP = MM::KSTEP;
+  constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KT / 16, PF = KT / VO::KEYS;
+  constexpr int RB = C::RB;
+  __shared__ __align__(1024) char lds[C::LDS];
+  __shared__ __align__(16) int64_t list[kListPages];
+  __shared__ int bad_pages;
+
+  const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = wave / RG, rg = wave % RG;
+  const int D = EXACT ? DM : a.head_dim;
+  const int head = blockIdx.x % a.n_kv;                    // KV head
+  const int item = blockIdx.x / a.n_kv;
+
+  // ---- the item's unit, rows and keys
+  int unit = item, part = 0, parts = 1, chunk = 0, slot = item;
+  if (a.shared) {
+    unit = item / a.splits;
+    part = item - unit * a.splits;
+    chunk = a.split_tiles;
+  } else if (a.slots) {
+    const Item p = plan_item(a, item, -1);
+    if (p.unit < 0) return;
+    unit = p.unit; part = p.part; parts = p.parts; chunk = p.chunk;
+  }
+  Unit x{0, unit, 0, a.n_tokens};
+  if (!a.shared) x = unit_of(a, unit);
+  const int row0 = x.tile * C::ROWS, n_rows = min(C::ROWS, x.nq * a.group - row0);
+  const int seq_n = a.shared ? 0 : seq_len(a.seqs, x.s);
+  // query, position and interval of row r of the unit
+  struct Row { int t, g, p, lo, hi; };
+  auto row_of = [&](int r) {
+    Row w;
+    const int i = (row0 + r) / a.group;
+    w.g = row0 + r - i * a.group;
+    w.t = x.tok0 + i;
+    int n = seq_n, nq = x.nq, qi = i;
+    if (a.shared) {
+      const int s = a.q_off ? find_offset(a.q_off, a.seqs.n_seqs, i) : i / a.q_per_seq;
+      const int o = a.q_off ? a.q_off[s] : s * a.q_per_seq;
+      nq = a.q_off ? a.q_off[s + 1] - o : a.q_per_seq;
+      n = seq_len(a.seqs, s);
+      qi = i - o;
+    }
+    w.p = n - nq + qi;
+    const int2 iv = interval_of(a, n, nq, qi, w.t);
+    w.lo = iv.x;
+    w.hi = iv.y;
+    return w;
+  };
+  // the keys that any row sees
+  int kb = INT_MAX, ke = INT_MIN;
+  for (int r = lane; r < C::ROWS; r += 64)
+    if (r < n_rows) {
+      const Row w = row_of(r);
+      if (w.lo < w.hi) { kb = min(kb, w.lo); ke = max(ke, w.hi); }
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    kb = min(kb, __shfl_xor(kb, o));
+    ke = max(ke, __shfl_xor(ke, o));
+  }
+  if (chunk) {
+    const int64_t b = (int64_t)a.key_begin + (int64_t)part * chunk * kPlanTile;
+    kb = (int)max((int64_t)kb, b);
+    // (the last part of a planned unit takes whatever is left)
+    if (a.shared || part + 1 < parts) ke = (int)min((int64_t)ke, b + (int64_t)chunk * kPlanTile);
+  }
+  kb = __builtin_amdgcn_readfirstlane(kb);
+  ke = __builtin_amdgcn_readfirstlane(ke);
+
+  // ---- this lane's rows
+  Row rw[NQ];
+  bool rvalid[NQ];
+  frag qf[NQ][QF];
+  float slope[NQ];
+  int wlo = INT_MIN, whi = INT_MAX;      // window that every row of the wave sees
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = (rg * NQ + n) * 16 + c16;
+    rvalid[n] = r < n_rows;
+    rw[n] = Row{0, 0, 0, INT_MIN, INT_MAX};
+    if (rvalid[n]) {
+      rw[n] = row_of(r);
+      wlo = max(wlo, rw[n].lo);
+      whi = min(whi, rw[n].hi);
+    }
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)rw[n].t * a.q_token +
+                  (int64_t)(head * a.group + rw[n].g) * a.q_head;
+#pragma unroll
+    for (int kk = 0; kk < QF; ++kk)
+      qf[n][kk] = rvalid[n] && (EXACT || kk * KSTEP < D)
+                      ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
+    slope[n] = a.bias ? a.slopes_log2[head * a.group + rw[n].g] : 0.f;
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    wlo = max(wlo, __shfl_xor(wlo, o));
+    whi = min(whi, __shfl_xor(whi, o));
+  }
+  wlo = __builtin_amdgcn_readfirstlane(wlo);
+  whi = __builtin_amdgcn_readfirstlane(whi);
+  const bool idle = rg * NQ * 16 >= n_rows;     // no row: the wave only stages
+
+  f32x4 oacc[NQ][DT];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m[n] = -INFINITY;
+    l[n] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) oacc[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const bool general = a.cap_log2 > 0.f || a.bias;
+  const float cc = general ? 1.f : a.scale_log2;
+
+  const char* kbase = static_cast<const char*>(a.k) + (int64_t)head * a.seqs.head * sizeof(T);
+  const char* vbase = static_cast<const char*>(a.v) + (int64_t)head * a.seqs.head * sizeof(T);
+  char* ring = lds + kg * C::RING;
+  const int shift = a.seqs.shift, page_mask = (1 << shift) - 1;
+  const int* table = a.seqs.table + (int64_t)x.s * a.seqs.max_blocks;
+  constexpr int STEP = KT * KG;
+  const int64_t seg_most = ((int64_t)(kListPages - 1) << shift) / STEP * STEP;
+
+  for (int64_t seg64 = kb; seg64 < ke; seg64 += seg_most) {
+    // ---- a segment: its block list, then its tiles through the ring
+    const int seg = (int)seg64, seg_end = (int)min(seg64 + seg_most, (int64_t)ke);
+    const int p0 = seg >> shift, np = ((seg_end - 1) >> shift) - p0 + 1;
+    __syncthreads();                       // the last segment's list and ring are idle
+    if (tid == 0) bad_pages = 0;
+    __syncthreads();
+    for (int i = tid; i < np; i += C::NT) {
+      const int id = table[p0 + i];
+      const bool ok = id >= 0 && id < a.seqs.n_blocks;
+      list[i] = ok ? (int64_t)id * a.seqs.block : -1;
+      if (!ok) bad_pages = 1;
+    }
+    __syncthreads();
+    const bool seg_bad = __builtin_amdgcn_readfirstlane(bad_pages) != 0;
+    const int tiles = (seg_end - seg + KT - 1) / KT;
+    const int iters = (tiles + KG - 1) / KG, mine = (tiles - kg + KG - 1) / KG;
+
+    auto issue = [&](int i, int st) {      // tile i of this group into ring slot st
+      const int k0 = seg + (i * KG + kg) * KT;
+      int64_t src[C::ROUNDS];
+#pragma unroll
+      for (int r = 0; r < C::ROUNDS; ++r) {
+        const int row = (r * RG + rg) * C::RPW + lane / C::CPR;
+        int ch = (lane % C::CPR) ^ row_swizzle<RB>(row);
+        if (!EXACT && ch * 16 >= D * (int)sizeof(T)) ch = 0;
+        const int key = min(k0 + row, seg_end - 1);      // never past the last key seen
+        const int64_t off = max(list[(key >> shift) - p0], (int64_t)0);
+        src[r] = (off + (int64_t)(key & page_mask) * a.seqs.token) * (int)sizeof(T) + ch * 16;
+      }
+      char* base = ring + st * 2 * C::TILE;
+#pragma unroll
+      for (int r = 0; r < C::ROUNDS; ++r) dma16(kbase + src[r], base + (r * RG + rg) * 1024);
+#pragma unroll
+      for (int r = 0; r < C::ROUNDS; ++r)
+        dma16(vbase + src[r], base + C::TILE + (r * RG + rg) * 1024);
+    };
+
+    auto compute = [&](int i, int st) {
+      const char* kt = ring + st * 2 * C::TILE;
+      const char* vt = kt + C::TILE;
+      const int k0 = seg + (i * KG + kg) * KT;
+      // S^T: sub-tile t, row block n: keys k0 + 16 t + 4 g + [0, 4) of row c16
+      f32x4 s[NQ][ST];
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < QF; ++kk) {
+          if (!EXACT && kk * KSTEP >= D) break;
+          const int byte = (kk * KSTEP + g * KPL) * (int)sizeof(T);
+          const frag kf = *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + c16, byte >> 4));
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
+        }
+      }
+      if (general) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int t = 0; t < ST; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float v = a.cap_log2 > 0.f ? a.cap_log2 * tanh_of<T>(s[n][t][e] * a.scale_over_cap)
+                                         : s[n][t][e] * a.scale_log2;
+              const int key = k0 + t * 16 + 4 * g + e;
+              v -= slope[n] * fabsf((float)(rw[n].p - key));
+              s[n][t][e] = v;
+            }
+      }
+      // masked tiles: not wholly inside every row's window, or with keys past
+      // the segment, or over a block that is none
+      const bool masked = seg_bad || k0 < wlo || k0 + KT > whi || k0 + KT > seg_end;
+      uint32_t see[NQ] = {};     // visible bits of this lane's scores (bit t * 4 + e)
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int t = 0; t < ST; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = k0 + t * 16 + 4 * g + e;
+              bool ok = key >= rw[n].lo && key < rw[n].hi && key < seg_end;
+              if (seg_bad && ok) ok = list[(key >> shift) - p0] >= 0;
+              if (ok) see[n] |= 1u << (t * 4 + e);
+              else s[n][t][e] = -INFINITY;
+            }
+      }
+      // running maximum: raised only when a score exceeds it by 2^8 (softmax
+      // does not depend on the reference; p and l stay far inside fp32)
+      frag pf[NQ][PF];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < ST; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][t][e]);
+        mx = row_max(mx) * cc;
+        const bool raise = mx > m[n] + 8.f;     // row by row: no row's rounding depends on another
+        if (__any(raise)) {
+          const float mn = raise ? mx : m[n];
+          const float alpha = raise ? __builtin_amdgcn_exp2f(m[n] - mn) : 1.f;
+          l[n] *= alpha;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) oacc[n][d] *= alpha;
+          m[n] = mn;
+        }
+        const float ref = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+        for (int f = 0; f < PF; ++f) {
+          float pv[KPL];
+#pragma unroll
+          for (int e = 0; e < KPL; ++e)
+            pv[e] = __builtin_amdgcn_exp2f(
+                __builtin_fmaf(s[n][f * (KPL / 4) + e / 4][e % 4], cc, -ref));
+          pf[n][f] = pack_frag(pv, (frag*)nullptr);
+          l[n] = frag_sum(pf[n][f], l[n]);
+        }
+      }
+      // O^T += V^T P^T.  A value that is not finite must not reach a row that
+      // does not see its key (0 * inf): where a tile is masked and has such
+      // values, they are taken out and added as what they do to the rows
+      // that see them.
+      bool odd = false;
+      if (masked) {
+        int bad = 0;
+#pragma unroll
+        for (int f = 0; f < PF; ++f)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            if (!EXACT && d * 16 >= D) break;
+            // (read by the whole wave: a transposing read crosses lanes)
+            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+            bad |= !VO::finite(vf);
+          }
+        odd = __any(bad);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int f = 0; f < PF; ++f)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            if (!EXACT && d * 16 >= D) break;
+            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          }
+      } else {
+        const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < PF; ++f) {
+          frag one[NQ];
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            float b[KPL];
+#pragma unroll
+            for (int e = 0; e < KPL; ++e) b[e] = (see[n] >> (f * KPL + e)) & 1 ? 1.f : 0.f;
+            one[n] = pack_frag(b, (frag*)nullptr);
+          }
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            if (!EXACT && d * 16 >= D) break;
+            frag fin, pos, neg;
+            VO::split(VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane), &fin, &pos, &neg);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+              oacc[n][d] = MM::mma(fin, pf[n][f], oacc[n][d]);
+              const f32x4 cp = MM::mma(pos, one[n], zero), cn = MM::mma(neg, one[n], zero);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (cp[e] > 0.f) oacc[n][d][e] += INFINITY;
+                if (cn[e] > 0.f) oacc[n][d][e] -= INFINITY;
+              }
+            }
+          }
+        }
+      }
+    };
+
+#pragma unroll
+    for (int st = 0; st < STAGES - 1; ++st)
+      if (mine > 0) issue(min(st, mine - 1), st);
+    int st = 0;
+    for (int i = 0; i < iters; ++i) {
+      // every iteration issues one tile (past the last one, a copy of it into a
+      // slot nobody reads again), so tile i has landed once STAGES - 2 later
+      // ones remain in flight
+      wait_vmcnt<(STAGES - 2) * 2 * C::ROUNDS>();
+      if (RG > 1) {   // ... in every wave's part, and the slot refilled below is idle
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (i < mine) {
+        const int fill = st == 0 ? STAGES - 1 : st - 1;
+        issue(min(i + STAGES - 1, mine - 1), fill);
+        if (!idle) compute(i, st);
+      }
+      st = st + 1 == STAGES ? 0 : st + 1;
+    }
+    wait_vmcnt<0>();
+  }
+
+  // ---- join the groups, write the result or the partial one
+  float lt[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) lt[n] = row_sum(l[n]);
+  const bool partial = a.always_partial || parts > 1;
+  const int64_t prow = ((int64_t)slot * a.n_kv + head) * C::ROWS;
+  if constexpr (KG == 1) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      if (!rvalid[n]) continue;
+      const int r = (rg * NQ + n) * 16 + c16;
+      const float inv = lt[n] == 0.f ? 0.f : 1.f / lt[n];
+      T* op = static_cast<T*>(a.o) + (int64_t)rw[n].t * a.o_token +
+              (int64_t)(head * a.group + rw[n].g) * a.o_head;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        if (!EXACT && d * 16 >= D) break;
+        if (partial) {
+          *reinterpret_cast<f32x4*>(a.part_o + (prow + r) * D + d * 16 + 4 * g) = oacc[n][d];
+        } else {
+          T w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(oacc[n][d][e] * inv);
+          if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint2*>(op + d * 16 + 4 * g) = *reinterpret_cast<const uint2*>(w);
+          else
+            *reinterpret_cast<uint4*>(op + d * 16 + 4 * g) = *reinterpret_cast<const uint4*>(w);
+        }
+      }
+      if (g == 0) {
+        if (partial) a.part_ml[prow + r] = make_float2(m[n], lt[n]);
+        else if (a.lse)
+          a.lse[(int64_t)rw[n].t * a.n_kv * a.group + head * a.group + rw[n].g] =
+              lt[n] == 0.f ? -INFINITY : (m[n] + __log2f(lt[n])) / kLog2e;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------- merge
+// One workgroup per (query, head): its waves share the row's partial results,
+// those of the pass over the shared keys (pre) and those of its own unit.
+template <typename T>
+__global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendArgs pre) {
+  __shared__ float part[4][256 + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
+  const int n_heads = a.n_kv * a.group;
+  const int t = blockIdx.x / n_heads, h = blockIdx.x - t * n_heads;
+  const int head = h / a.group, g = h - head * a.group;
+  int s, i, unit;
+  if (a.unit_off) {
+    s = find_offset(a.q_off, a.seqs.n_seqs, t);
+    i = t - a.q_off[s];
+    unit = a.unit_off[s];
+  } else {
+    s = t / a.q_per_seq;
+    i = t - s * a.q_per_seq;
+    unit = s * a.units_per_seq;
+  }
+  const int tile = (i * a.group + g) / a.rows, row = i * a.group + g - tile * a.rows;
+  unit += tile;
+  const Item it = plan_item(a, -1, unit);
+  if (it.unit < 0 || (it.parts == 1 && !a.always_partial)) return;   // written already
+  const int n_pre = pre.shared ? pre.splits : 0, P = n_pre + it.parts;
+  const int prow = t * a.group + g;      // the row in the tiles over all sequences
+  const int ptile = pre.shared ? prow / pre.rows : 0;
+  auto index = [&](int j, const float2** ml) -> const float* {
+    const bool p = j < n_pre;
+    const AttendArgs& x = p ? pre : a;
+    const int64_t item = p ? (int64_t)ptile * n_pre + j : it.first + (j - n_pre);
+    const int64_t r = (item * a.n_kv + head) * x.rows + (p ? prow - ptile * pre.rows : row);
+    *ml = x.part_ml + r;
+    return x.part_o + r * D;
+  };
+  float m = -INFINITY;
+  for (int j = lane; j < P; j += 64) {
+    const float2* ml;
+    index(j, &ml);
+    if (ml->y != 0.f) m = fmaxf(m, ml->x);      // (a NaN sum counts, its maximum may be -inf)
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int j = wave; j < P; j += 4) {
+    const float2* ml;
+    const float* po = index(j, &ml);
+    const float2 v = *ml;
+    if (v.y == 0.f) continue;                   // saw nothing
+    const float w = __builtin_amdgcn_exp2f((v.x == -INFINITY ? 0.f : v.x) - ref);
+    l += w * v.y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (lane + 64 * k < D) o[k] += w * po[lane + 64 * k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = o[k];
+  if (lane == 0) part[wave][256] = l;
+  __syncthreads();
+  l = (part[0][256] + part[1][256]) + (part[2][256] + part[3][256]);
+  const int d = threadIdx.x;
+  if (d < D) {
+    const float v = (part[0][d] + part[1][d]) + (part[2][d] + part[3][d]);
+    static_cast<T*>(a.o)[(int64_t)t * a.o_token + (int64_t)h * a.o_head + d] =
+        from_f32<T>(l == 0.f ? 0.f : v / l);
+  }
+  if (d == 0 && a.lse)
+    a.lse[(int64_t)t * n_heads + h] = l == 0.f ? -INFINITY : (m + __log2f(l)) / kLog2e;
+}
+
+template <typename T>
+hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, hipStream_t s) {
+  const int64_t rows = (int64_t)a.n_tokens * a.n_kv * a.group;
+  CR_LAUNCH((attend_merge_kernel<T>), dim3((unsigned)rows), dim3(256), 0, s, a, pre);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ launch
+template <typename T, int DM, bool EXACT>
+hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
+  constexpr int KT = sizeof(T) == 2 ? (DM > 128 ? 32 : 64) : (DM > 128 ? 16 : 32);
+  constexpr int NQ = attend_rows(sizeof(T), DM) / 64;
+  if (a.rows != 64 * NQ) return hipErrorInvalidValue;
+  CR_LAUNCH((attend_kernel<T, DM, EXACT, NQ, 4, 1, KT, 2>), dim3((unsigned)(items * a.n_kv)),
+            dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attend(const AttendArgs& a, hipStream_t s) {
+  const int64_t items = a.shared ? (int64_t)a.n_units * a.splits
+                                 : (int64_t)a.n_units + (a.slots ? a.slots : 0);
+  if (items * a.n_kv >= (int64_t)1 << 31) return hipErrorInvalidValue;
+  switch (a.head_dim) {
+    case 64: return attend_as<T, 64, true>(a, items, s);
+    case 128: return attend_as<T, 128, true>(a, items, s);
+    case 256: return attend_as<T, 256, true>(a, items, s);
+    default: return attend_as<T, 256, false>(a, items, s);
+  }
+}
+
+}  // namespace cr

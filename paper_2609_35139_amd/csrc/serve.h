@@ -1,0 +1,84 @@
+// Launchers of the kernels that answer over a paged cache (internal to the
+// library): appending rotated keys and values, and attention over the pages.
+#pragma once
+#include <stdint.h>
+
+#include "launch.h"
+
+namespace cr {
+
+constexpr int kMaxQueryHeads = 256;
+
+// One layer of a paged cache and the sequences in it.  Token t of sequence s
+// lies in block table[s * max_blocks + (t >> shift)], row t & (2^shift - 1).
+// lens and table are device memory that only the kernels read: a length is
+// clamped to [0, max_len] and a block outside [0, n_blocks) is no block.
+struct PagedSeqs {
+  int64_t token, head, block;       // strides in elements
+  int shift, n_blocks, max_blocks, max_len, n_seqs;
+  const int *table, *lens;
+};
+
+// ---- append: K (rotated) and V of the new tokens into their pages, and the
+// rotated queries.  New token i of sequence s has slot lens[s] - q_s + i.
+struct AppendArgs {
+  PagedSeqs seqs;
+  void *k_cache, *v_cache;          // this layer's keys and values
+  const void *k, *v, *q;            // q null: no queries
+  void* q_out;
+  int64_t k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head;
+  int n_tokens, n_kv, n_heads, head_dim;
+  const int* positions;             // device, null: the slot
+  int rotate;                       // 0: copied as they are
+};
+template <typename T>
+hipError_t append_kv(const AppendArgs& a, const KeyRope& kr, const int32_t* offsets,
+                     hipStream_t s);
+
+// ---- attention.  A unit is a tile of `rows` (query, head of the group) rows
+// of one sequence and one KV head; see attend_kernel.h.
+struct AttendArgs {
+  PagedSeqs seqs;
+  const void *k, *v;                // this layer's keys and values
+  const void* q;
+  int64_t q_token, q_head, o_token, o_head;
+  void* o;
+  float* lse;                       // [n_tokens][n_heads] or null
+  int n_tokens, n_kv, group, head_dim;
+  // device offsets of the sequences' queries and units, or null where every
+  // sequence has q_per_seq queries and units_per_seq units
+  const int *q_off, *unit_off;
+  int q_per_seq, units_per_seq, n_units, rows;
+  const int *lo, *hi;               // device interval of every query, or null
+  float scale_log2;                 // score scale * log2(e)
+  float cap_log2, scale_over_cap;   // cap * log2(e) (0: no cap), scale / cap
+  int bias;                         // slopes are used
+  float slopes_log2[kMaxQueryHeads];
+  // keys of this pass: [key_begin, ...) of every sequence, or, with shared > 0,
+  // [0, shared) of sequence 0's pages for the rows of all sequences
+  int key_begin, shared;
+  // splits of the keys: planned on the device from the lengths (slots > 0:
+  // about that many items per KV head, at least min_tiles 64-key tiles each),
+  // or fixed (shared: `splits` of split_tiles tiles), or none
+  int slots, min_tiles, splits, split_tiles;
+  int always_partial;               // write partial results for the merge
+  float* part_o;                    // [item][kv head][rows][head_dim]
+  float2* part_ml;                  // [item][kv head][rows] (max, sum)
+};
+// Rows of a unit: 128, or 64 where the accumulators of wide fp32 heads fill the
+// registers (head dims without a kernel of their own run in that of 256).
+constexpr bool attend_exact(int head_dim) {
+  return head_dim == 64 || head_dim == 128 || head_dim == 256;
+}
+constexpr int attend_rows(int element_bytes, int head_dim) {
+  return element_bytes == 4 && (head_dim > 128 || !attend_exact(head_dim)) ? 64 : 128;
+}
+template <typename T>
+hipError_t attend(const AttendArgs& a, hipStream_t s);
+
+// Joins the partial results of a planned pass and, with pre.shared > 0, those
+// of the pass over the shared keys.
+template <typename T>
+hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, hipStream_t s);
+
+}  // namespace cr

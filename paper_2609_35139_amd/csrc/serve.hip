@@ -1,0 +1,360 @@
+// C ABI of answering over a paged cache: validation, the split of the work and
+// the kernel sequence of cr_append_kv and cr_attend.  See include/cacherepair.h.
+#include "../../include/cacherepair.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "profile.h"
+#include "rules.h"
+#include "serve.h"
+#include "validate.h"
+
+namespace {
+
+using namespace cr;   // the helpers of validate.h and profile.h
+
+constexpr int64_t kMostTokens = ((int64_t)1 << 31) - 256;
+
+// The batch as the host sees it.
+struct Batch {
+  int64_t n_tokens = 0;
+  int64_t most = 0;              // queries of the longest sequence
+  const int32_t* off = nullptr;  // null: every sequence has n_tokens / n_seqs queries
+};
+
+cr_status check_cache(const cr_kv_layout* l) {
+  if (l->n_layers < 1 || l->n_kv_heads < 1 || l->head_dim < 32 || l->head_dim > 256 ||
+      l->head_dim % 32)
+    return CR_ERR_DIMS;
+  return check_dtype(l);
+}
+
+// The offsets and the table's extent (no device memory is read).
+cr_status check_batch(const cr_sequences* q, Batch* b) {
+  if (q->n_seqs < 1) return CR_ERR_OFFSETS;
+  if (!q->query_offsets) {
+    b->n_tokens = q->n_seqs;
+    b->most = 1;
+  } else {
+    const int32_t* o = q->query_offsets;
+    if (o[0] != 0) return CR_ERR_OFFSETS;
+    bool same = true;
+    for (int s = 0; s < q->n_seqs; ++s) {
+      if (o[s + 1] < o[s]) return CR_ERR_OFFSETS;
+      b->most = std::max<int64_t>(b->most, (int64_t)o[s + 1] - o[s]);
+      same = same && o[s + 1] - o[s] == o[1];
+    }
+    b->n_tokens = o[q->n_seqs];
+    if (!same) b->off = o;
+  }
+  if (b->n_tokens >= kMostTokens) return CR_ERR_DIMS;
+  if (q->block_size < 1 || q->block_size > 1024 || (q->block_size & (q->block_size - 1)) ||
+      q->max_blocks < 1 || (int64_t)q->max_blocks * q->block_size >= kMostTokens)
+    return CR_ERR_LAYOUT;
+  return CR_OK;
+}
+
+// A [n][heads][head_dim] operand; written ones must not overlap themselves.
+cr_status check_rows(const cr_rows* r, int64_t n, int64_t heads, int64_t head_dim, bool written) {
+  if (!r->data && n > 0) return CR_ERR_NULL;
+  if (!aligned(r->data, 16)) return CR_ERR_LAYOUT;
+  const int64_t st[2] = {r->stride_token, r->stride_head}, ext[2] = {n, heads};
+  Dims dims;
+  dims.push_back({1, head_dim});
+  if (n == 0) return CR_OK;   // no element is addressed
+  int64_t reach = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (st[i] < 0 || st[i] % 8) return CR_ERR_LAYOUT;
+    int64_t span;
+    if (__builtin_mul_overflow(st[i], ext[i] - 1, &span) ||
+        __builtin_add_overflow(reach, span, &reach) || reach >= (int64_t)1 << 62)
+      return CR_ERR_LAYOUT;
+    if (ext[i] > 1) dims.push_back({st[i], ext[i]});
+  }
+  return written ? check_injective(dims) : CR_OK;
+}
+
+PagedSeqs paged(const cr_kv_layout* l, const cr_sequences* q) {
+  PagedSeqs p{};
+  p.token = l->stride_token;
+  p.head = l->stride_head;
+  p.block = q->stride_block;
+  p.shift = log2_int(q->block_size);
+  p.n_blocks = q->n_blocks;
+  p.max_blocks = q->max_blocks;
+  p.max_len = q->max_blocks * q->block_size;
+  p.n_seqs = q->n_seqs;
+  p.table = q->block_table;
+  p.lens = q->kv_lens;
+  return p;
+}
+
+// Address of component c (0 K, 1 V) of a layer.
+const char* component(const void* kv, const cr_kv_layout* l, int layer, int c) {
+  return static_cast<const char*>(kv) +
+         ((int64_t)layer * l->stride_layer + (int64_t)c * l->stride_kv) * (int64_t)esize(l->dtype);
+}
+
+// ------------------------------------------------------------- attention
+// How one cr_attend call is cut up; a function of what the host knows, so the
+// workspace can be sized ahead of the lengths.
+struct Plan {
+  int rows = 0;                  // rows of a unit
+  int64_t units = 0;             // of the pass over each sequence's own keys
+  int slots = 0, min_tiles = 0;  // its split (slots 0: none)
+  int64_t own_items = 0;         // partial results of that pass, per KV head
+  int64_t pre_units = 0;         // units of the pass over the shared keys, its split
+  int splits = 0, split_tiles = 0;
+  uint64_t tables = 0, own_ml = 0, own_o = 0, pre_ml = 0, pre_o = 0, total = 0;
+};
+
+Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, int n_heads,
+                 int shared) {
+  Plan p;
+  const int G = n_heads / l->n_kv_heads, D = l->head_dim, H = l->n_kv_heads;
+  p.rows = attend_rows((int)esize(l->dtype), D);
+  auto tiles = [&](int64_t n) { return ceil_div(n * G, p.rows); };
+  if (b.off) {
+    for (int s = 0; s < q->n_seqs; ++s) p.units += tiles(b.off[s + 1] - b.off[s]);
+  } else {
+    p.units = q->n_seqs * tiles(b.most);
+  }
+  Arena a;
+  if (b.off) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
+  // split the keys unless the units fill the chip by themselves
+  if (p.units * H < 512) {
+    p.slots = (int)std::max<int64_t>(1, 512 / H);
+    p.min_tiles = 4;
+    // one part holds all keys there can be
+    if ((int64_t)q->max_blocks * q->block_size <= p.min_tiles * 64) p.slots = 0;
+  }
+  if (p.slots && shared > 0) {
+    p.pre_units = tiles(b.n_tokens);
+    const int64_t key_tiles = ceil_div(shared, 64);
+    const int64_t want = std::max<int64_t>(1, 512 / (p.pre_units * H));
+    p.split_tiles = (int)std::max<int64_t>(p.min_tiles, ceil_div(key_tiles, want));
+    p.splits = (int)ceil_div(key_tiles, p.split_tiles);
+  }
+  p.own_items = p.slots ? p.units + p.slots : 0;
+  const uint64_t own = (uint64_t)p.own_items * H * p.rows;
+  const uint64_t pre = (uint64_t)p.pre_units * p.splits * H * p.rows;
+  p.own_ml = a.take(own * 8);
+  p.own_o = a.take(own * D * 4);
+  p.pre_ml = a.take(pre * 8);
+  p.pre_o = a.take(pre * D * 4);
+  p.total = a.off;
+  return p;
+}
+
+cr_status check_attend(const cr_kv_layout* l, const cr_sequences* q, int n_heads, int shared,
+                       Batch* b) {
+  cr_status st = check_cache(l);
+  if (st != CR_OK) return st;
+  st = check_batch(q, b);
+  if (st != CR_OK) return st;
+  if (n_heads < 1 || n_heads > kMaxQueryHeads || n_heads % l->n_kv_heads) return CR_ERR_DIMS;
+  if (b->n_tokens * n_heads >= kMostTokens) return CR_ERR_DIMS;
+  if (shared < 0 || shared > q->max_blocks * q->block_size) return CR_ERR_DIMS;
+  return CR_OK;
+}
+
+template <typename T>
+cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr_sequences* q,
+                      const Batch& b, const Plan& p, const cr_rows* qr, const cr_rows* out,
+                      int n_heads, const cr_attend_options& o, char* ws, hipStream_t s) {
+  AttendArgs a{};
+  a.seqs = paged(l, q);
+  a.k = component(kv, l, layer, 0);
+  a.v = component(kv, l, layer, 1);
+  a.q = qr->data;
+  a.q_token = qr->stride_token;
+  a.q_head = qr->stride_head;
+  a.o = out->data;
+  a.o_token = out->stride_token;
+  a.o_head = out->stride_head;
+  a.lse = o.lse;
+  a.n_tokens = (int)b.n_tokens;
+  a.n_kv = l->n_kv_heads;
+  a.group = n_heads / l->n_kv_heads;
+  a.head_dim = l->head_dim;
+  a.rows = p.rows;
+  a.n_units = (int)p.units;
+  a.lo = o.lo;
+  a.hi = o.hi;
+  const double scale = o.scale > 0.f ? o.scale : 1.0 / std::sqrt((double)l->head_dim);
+  const double log2e = 1.4426950408889634;
+  a.scale_log2 = (float)(scale * log2e);
+  if (o.softcap > 0.f) {
+    a.cap_log2 = (float)(o.softcap * log2e);
+    a.scale_over_cap = (float)(scale / o.softcap);
+  }
+  if (o.slopes) {
+    a.bias = 1;
+    for (int h = 0; h < n_heads; ++h) a.slopes_log2[h] = (float)(o.slopes[h] * log2e);
+  }
+  if (b.off) {
+    // the sequences' first queries and first units, for the kernels
+    const int n = q->n_seqs + 1;
+    int* dev = reinterpret_cast<int*>(ws + p.tables);
+    CR_TRY(timed("attend_table", s, [&] {
+      int32_t buf[512];
+      int64_t unit = 0;
+      for (int i0 = 0; i0 < 2 * n; i0 += 512) {
+        const int m = std::min(512, 2 * n - i0);
+        for (int i = i0; i < i0 + m; ++i) {
+          if (i > n) unit += ceil_div((int64_t)(b.off[i - n] - b.off[i - n - 1]) * a.group, p.rows);
+          buf[i - i0] = i < n ? b.off[i] : (int32_t)unit;
+        }
+        const hipError_t e = copy_table(buf, m, dev + i0, s);
+        if (e != hipSuccess) return e;
+      }
+      return hipSuccess; }));
+    a.q_off = dev;
+    a.unit_off = dev + q->n_seqs + 1;
+  } else {
+    a.q_per_seq = (int)b.most;
+    a.units_per_seq = (int)ceil_div(b.most * a.group, p.rows);
+  }
+  a.slots = p.slots;
+  a.min_tiles = p.min_tiles;
+  a.part_ml = reinterpret_cast<float2*>(ws + p.own_ml);
+  a.part_o = reinterpret_cast<float*>(ws + p.own_o);
+  AttendArgs pre{};
+  if (p.pre_units) {
+    pre = a;
+    pre.shared = o.shared_len;
+    pre.n_units = (int)p.pre_units;
+    pre.slots = 0;
+    pre.splits = p.splits;
+    pre.split_tiles = p.split_tiles;
+    pre.always_partial = 1;
+    pre.part_ml = reinterpret_cast<float2*>(ws + p.pre_ml);
+    pre.part_o = reinterpret_cast<float*>(ws + p.pre_o);
+    a.key_begin = o.shared_len;
+    a.always_partial = 1;
+    CR_TRY(timed("attend_shared", s, [&] { return attend<T>(pre, s); }));
+  }
+  CR_TRY(timed("attend", s, [&] { return attend<T>(a, s); }));
+  if (p.slots) CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, pre, s); }));
+  return CR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t layer,
+                       const cr_sequences* seqs, const cr_rows* k, const cr_rows* v,
+                       const cr_rows* q, const cr_rows* q_out, int32_t n_heads,
+                       const cr_rope* rope, const int32_t* positions, void* stream) {
+  if (!kv || !layout || !seqs || !k || !v || !seqs->kv_lens || !seqs->block_table)
+    return CR_ERR_NULL;
+  if (!q != !q_out) return CR_ERR_NULL;
+  cr_status st = check_cache(layout);
+  if (st != CR_OK) return st;
+  Batch b;
+  st = check_batch(seqs, &b);
+  if (st != CR_OK) return st;
+  if (layer < 0 || layer >= layout->n_layers) return CR_ERR_DIMS;
+  if (q && (n_heads < 1 || n_heads > (1 << 16))) return CR_ERR_DIMS;
+  if (layout->n_kv_heads > (1 << 16)) return CR_ERR_DIMS;
+  st = check_page_strides(layout, seqs->block_size, seqs->n_blocks, seqs->stride_block);
+  if (st != CR_OK) return st;
+  if (!aligned(kv, 16)) return CR_ERR_LAYOUT;
+  KeyRope kr{};
+  kr.half = layout->head_dim / 2;
+  if (rope) {
+    st = key_rope_of(rope, layout->head_dim, &kr);
+    if (st != CR_OK) return st;
+  }
+  const int64_t H = layout->n_kv_heads, D = layout->head_dim;
+  if ((st = check_rows(k, b.n_tokens, H, D, false)) != CR_OK) return st;
+  if ((st = check_rows(v, b.n_tokens, H, D, false)) != CR_OK) return st;
+  if (q) {
+    if ((st = check_rows(q, b.n_tokens, n_heads, D, false)) != CR_OK) return st;
+    if ((st = check_rows(q_out, b.n_tokens, n_heads, D, true)) != CR_OK) return st;
+    // in place only element on element
+    if (q->data == q_out->data &&
+        (q->stride_token != q_out->stride_token || q->stride_head != q_out->stride_head))
+      return CR_ERR_LAYOUT;
+  }
+  // (a launch of at most 2^31 workgroups)
+  if ((double)b.n_tokens * (H + (q ? n_heads : 0)) * (D / 8) >= 256.0 * 2147483647.0)
+    return CR_ERR_DIMS;
+  if (b.n_tokens == 0) return CR_OK;
+  st = check_device();
+  if (st != CR_OK) return st;
+  AppendArgs a{};
+  a.seqs = paged(layout, seqs);
+  a.k_cache = const_cast<char*>(component(kv, layout, layer, 0));
+  a.v_cache = const_cast<char*>(component(kv, layout, layer, 1));
+  a.k = k->data; a.k_token = k->stride_token; a.k_head = k->stride_head;
+  a.v = v->data; a.v_token = v->stride_token; a.v_head = v->stride_head;
+  if (q) {
+    a.q = q->data; a.q_token = q->stride_token; a.q_head = q->stride_head;
+    a.q_out = q_out->data; a.o_token = q_out->stride_token; a.o_head = q_out->stride_head;
+    a.n_heads = n_heads;
+  }
+  a.n_tokens = (int)b.n_tokens;
+  a.n_kv = layout->n_kv_heads;
+  a.head_dim = layout->head_dim;
+  a.positions = positions;
+  a.rotate = rope != nullptr;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  CR_TRY(timed("append_kv", s, [&] {
+    return layout->dtype == CR_DTYPE_BF16 ? append_kv<bf16>(a, kr, b.off, s)
+                                          : append_kv<float>(a, kr, b.off, s); }));
+  return CR_OK;
+}
+
+cr_status cr_attend_workspace_bytes(const cr_kv_layout* layout, const cr_sequences* seqs,
+                                    int32_t n_heads, int32_t shared_len, uint64_t* bytes) {
+  if (!layout || !seqs || !bytes) return CR_ERR_NULL;
+  Batch b;
+  const cr_status st = check_attend(layout, seqs, n_heads, shared_len, &b);
+  if (st != CR_OK) return st;
+  *bytes = b.n_tokens ? attend_plan(layout, seqs, b, n_heads, shared_len).total : 0;
+  return CR_OK;
+}
+
+cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t layer,
+                    const cr_sequences* seqs, const cr_rows* q, const cr_rows* out,
+                    int32_t n_heads, const cr_attend_options* options, void* workspace,
+                    uint64_t workspace_bytes, void* stream) {
+  if (!kv || !layout || !seqs || !q || !out || !seqs->kv_lens || !seqs->block_table)
+    return CR_ERR_NULL;
+  const cr_attend_options o = options ? *options : cr_attend_options{};
+  Batch b;
+  cr_status st = check_attend(layout, seqs, n_heads, o.shared_len, &b);
+  if (st != CR_OK) return st;
+  if (layer < 0 || layer >= layout->n_layers) return CR_ERR_DIMS;
+  if (!(o.scale >= 0.f) || !std::isfinite(o.scale) || !(o.softcap >= 0.f) ||
+      !std::isfinite(o.softcap))
+    return CR_ERR_DIMS;
+  for (int h = 0; o.slopes && h < n_heads; ++h)
+    if (!std::isfinite(o.slopes[h])) return CR_ERR_DIMS;
+  st = check_page_strides(layout, seqs->block_size, seqs->n_blocks, seqs->stride_block);
+  if (st != CR_OK) return st;
+  if (!aligned(kv, 16)) return CR_ERR_LAYOUT;
+  const int64_t D = layout->head_dim;
+  if ((st = check_rows(q, b.n_tokens, n_heads, D, false)) != CR_OK) return st;
+  if ((st = check_rows(out, b.n_tokens, n_heads, D, true)) != CR_OK) return st;
+  if (q->data == out->data) return CR_ERR_LAYOUT;
+  if (b.n_tokens == 0) return CR_OK;
+  const Plan p = attend_plan(layout, seqs, b, n_heads, o.shared_len);
+  if (p.units * layout->n_kv_heads >= kMostTokens) return CR_ERR_DIMS;
+  if (p.total) {
+    if (!workspace) return CR_ERR_NULL;
+    if (workspace_bytes < p.total || !aligned(workspace, ALIGN)) return CR_ERR_WORKSPACE;
+  }
+  st = check_device();
+  if (st != CR_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  return layout->dtype == CR_DTYPE_BF16
+             ? attend_impl<bf16>(kv, layout, layer, seqs, b, p, q, out, n_heads, o, ws, s)
+             : attend_impl<float>(kv, layout, layer, seqs, b, p, q, out, n_heads, o, ws, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,182 @@
+"""Torch-side marshalling of answering over a paged cache (``cr_append_kv``,
+``cr_attend``): device buffers and streams only, like :mod:`repairer`.
+
+:class:`PagedCache` wraps the block pool that a paged repair writes
+(``binding.paged_layout``); :meth:`PagedCache.sequences` describes a batch and
+is reused by every layer (and, as the lengths and the table are read on the
+device, by every replay of a captured step)::
+
+    cache = PagedCache(pool)                        # [L][2][n_blocks][block_size][H][d_h]
+    step = cache.sequences(block_table, kv_lens)    # one new token per sequence
+    for layer in range(L):
+        cache.append(layer, step, k, v, q=q, q_out=q, rope={"theta": 1e6})
+        o = cache.attend(layer, step, q)
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import binding as B
+
+_DTYPE = {torch.bfloat16: B.CR_DTYPE_BF16, torch.float32: B.CR_DTYPE_F32}
+
+
+class Sequences:
+    """A batch of sequences of a :class:`PagedCache` (cr_sequences)."""
+
+    def __init__(self, cache: "PagedCache", block_table: torch.Tensor, kv_lens: torch.Tensor,
+                 query_offsets: Optional[Sequence[int]]):
+        for t, dims, name in ((block_table, 2, "block_table"), (kv_lens, 1, "kv_lens")):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
+                raise TypeError(f"{name} must be a contiguous {dims}-d int32 tensor")
+            if t.device != cache.pool.device:
+                raise ValueError(f"{name} must be on the cache's device")
+        n = kv_lens.shape[0]
+        if block_table.shape[0] != n:
+            raise ValueError("block_table needs one row per sequence")
+        self.block_table, self.kv_lens = block_table, kv_lens        # keeps them alive
+        self.struct, self._offsets = B.sequences_struct(
+            n, kv_lens.data_ptr(), block_table.data_ptr(), block_table.shape[1], cache.block_size,
+            cache.n_blocks, cache.stride_block, query_offsets)
+        self.n_tokens = n if query_offsets is None else int(self._offsets[-1])
+        self.workspace_bytes = {}                                    # by (heads, shared_len)
+
+
+class PagedCache:
+    """Block pool [n_layers][2][n_blocks][block_size][n_kv_heads][head_dim]
+    (any strides that cr_kv_layout and stride_block can describe)."""
+
+    def __init__(self, pool: torch.Tensor):
+        if pool.dim() != 6 or pool.shape[1] != 2 or pool.dtype not in _DTYPE:
+            raise TypeError("pool must be a bf16 or fp32 [L][2][n_blocks][block_size][H][d_h] tensor")
+        if not pool.is_cuda or pool.stride(5) != 1:
+            raise ValueError("pool must be device memory whose last dimension is contiguous")
+        self.pool = pool
+        L, _, self.n_blocks, self.block_size, H, d = pool.shape
+        # (the stride of a dimension of one element addresses nothing)
+        st = [x if n > 1 else 0 for x, n in zip(pool.stride(), pool.shape)]
+        self.stride_block = st[2]
+        self.layout = B.cr_kv_layout(L, H, d, _DTYPE[pool.dtype], st[0], st[1], st[3], st[4])
+        self.n_kv_heads, self.head_dim = H, d
+
+    def sequences(self, block_table: torch.Tensor, kv_lens: torch.Tensor,
+                  query_offsets: Optional[Sequence[int]] = None) -> Sequences:
+        """block_table: device int32 [n_seqs][max_blocks]; kv_lens: device int32
+        [n_seqs], the new tokens included; query_offsets: host offsets of each
+        sequence's new tokens, or None for one each."""
+        return Sequences(self, block_table, kv_lens, query_offsets)
+
+    def _rows(self, t: torch.Tensor, n: int, heads: Optional[int], name: str) -> B.cr_rows:
+        if t.dtype != self.pool.dtype or t.device != self.pool.device:
+            raise TypeError(f"{name} must have the cache's dtype and device")
+        if t.dim() != 3 or t.shape[0] != n or t.shape[2] != self.head_dim or \
+                (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected "
+                             f"({n}, {heads or 'heads'}, {self.head_dim})")
+        st = t.stride()
+        if st[2] != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+        return B.cr_rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if t.shape[1] > 1 else 0)
+
+    def _index(self, t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.device != self.pool.device or t.shape != (n,) or \
+                not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous int32 [{n}] tensor on the cache's device")
+        return t.data_ptr()
+
+    def _enter(self, stream: Optional[torch.cuda.Stream]):
+        """The cache's device and the call's stream as torch's current ones: the
+        library launches on the current device, and a workspace belongs to the
+        stream that uses it."""
+        dev = self.pool.device
+        if stream is None:
+            return torch.cuda.device(dev)
+        if stream.device != dev:
+            raise ValueError("the stream must be on the cache's device")
+        return torch.cuda.stream(stream)
+
+    def append(self, layer: int, seqs: Sequences, k: torch.Tensor, v: torch.Tensor,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               rope: Optional[dict] = None, positions: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+        """K <- R(p) k and V <- v in the new tokens' slots, q_out <- R(p) q
+        (cr_append_kv).  k, v: [n_tokens, n_kv_heads, head_dim]; q, q_out:
+        [n_tokens, n_heads, head_dim] (q_out None: a new tensor); rope: as
+        Repairer.rotate_keys, or None; positions: device int32, or None for the
+        slots.  Returns q_out."""
+        n = seqs.n_tokens
+        kr, vr = self._rows(k, n, self.n_kv_heads, "k"), self._rows(v, n, self.n_kv_heads, "v")
+        pos = self._index(positions, n, "positions")
+        rs, keep = (None, None) if rope is None else B.rope_struct(**rope)
+        if rs is not None and keep is not None and len(keep) != self.head_dim // 2:
+            raise ValueError("inv_freq needs head_dim / 2 entries")
+        with self._enter(stream):
+            qr = qo = None
+            if q is not None:
+                qr = self._rows(q, n, None, "q")
+                if q_out is None:
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                qo = self._rows(q_out, n, q.shape[1], "q_out")
+            B.cr_append_kv(self.pool.data_ptr(), self.layout, layer, seqs.struct, kr, vr, qr, qo,
+                           0 if q is None else q.shape[1], rs, pos,
+                           torch.cuda.current_stream().cuda_stream)
+        return q_out
+
+    def workspace(self, seqs: Sequences, n_heads: int, shared_len: int = 0) -> torch.Tensor:
+        """Device scratch for :meth:`attend` with these arguments."""
+        return torch.empty(max(self._workspace_bytes(seqs, n_heads, shared_len), 256),
+                           dtype=torch.uint8, device=self.pool.device)
+
+    def _workspace_bytes(self, seqs: Sequences, n_heads: int, shared_len: int) -> int:
+        n = seqs.workspace_bytes.get((n_heads, shared_len))
+        if n is None:
+            n = B.cr_attend_workspace_bytes(self.layout, seqs.struct, n_heads, shared_len)
+            seqs.workspace_bytes[n_heads, shared_len] = n
+        return n
+
+    def attend(self, layer: int, seqs: Sequences, q: torch.Tensor,
+               out: Optional[torch.Tensor] = None, scale: float = 0.0, softcap: float = 0.0,
+               slopes: Optional[Sequence[float]] = None, lo: Optional[torch.Tensor] = None,
+               hi: Optional[torch.Tensor] = None, shared_len: int = 0,
+               lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Attention of the new tokens' queries over the pages (cr_attend): out
+        [n_tokens, n_heads, head_dim] (None: a new tensor).  The options are
+        those of cr_attend_options; slopes is a host sequence, lo, hi (int32)
+        and lse (fp32 [n_tokens, n_heads]) are device tensors."""
+        n, heads = seqs.n_tokens, q.shape[1]
+        qr = self._rows(q, n, None, "q")
+        o = B.cr_attend_options(scale, softcap)
+        if slopes is not None:
+            sl = np.ascontiguousarray(slopes, dtype=np.float32)
+            if sl.shape != (heads,):
+                raise ValueError("slopes needs one entry per query head")
+            o.slopes = sl.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
+        o.lo, o.hi = self._index(lo, n, "lo"), self._index(hi, n, "hi")
+        o.shared_len = shared_len
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or \
+                    lse.device != q.device:
+                raise TypeError(f"lse must be a contiguous fp32 [{n}, {heads}] tensor")
+            o.lse = lse.data_ptr()
+        with self._enter(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            orows = self._rows(out, n, heads, "out")
+            need = self._workspace_bytes(seqs, heads, shared_len)
+            ws = workspace
+            if ws is not None and ws.device != self.pool.device:
+                raise ValueError("workspace must be on the cache's device")
+            if ws is None and need:
+                ws = torch.empty(need, dtype=torch.uint8, device=self.pool.device)
+            B.cr_attend(self.pool.data_ptr(), self.layout, layer, seqs.struct, qr, orows, heads, o,
+                        None if ws is None else ws.data_ptr(),
+                        0 if ws is None else ws.numel() * ws.element_size(),
+                        torch.cuda.current_stream().cuda_stream)
+        return out

@@ -1,0 +1,374 @@
+"""cr_append_kv and cr_attend on the GPU against their definitions in 64 bits
+(tests/serving_helpers.py), with bounds derived there from the roundings."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from serving_helpers import TORCH, Batch, append_oracle, assert_within, attend_oracle
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_35139_amd import binding
+    binding.load()
+
+
+# ------------------------------------------------------------------- append
+APPEND = {
+    "decode": dict(dtype="bf16", heads=16, kv_heads=2, d=128, bs=16, q=[1] * 5, lens=[1, 16, 17, 250, 33]),
+    "ragged": dict(dtype="bf16", heads=6, kv_heads=3, d=64, bs=8, q=[0, 5, 1, 40], lens=[9, 5, 30, 41]),
+    "f32": dict(dtype="f32", heads=4, kv_heads=4, d=96, bs=1, q=[3, 0, 2], lens=[3, 0, 9]),
+    "wide": dict(dtype="bf16", heads=2, kv_heads=1, d=256, bs=1024, q=[33], lens=[1100]),
+    "narrow": dict(dtype="f32", heads=5, kv_heads=1, d=32, bs=4, q=[7, 7], lens=[7, 50]),
+    # lengths that leave new tokens without a slot
+    "short": dict(dtype="bf16", heads=2, kv_heads=2, d=64, bs=4, q=[5, 2, 1], lens=[3, -2, 0]),
+}
+
+
+@pytest.mark.parametrize("name", APPEND)
+@pytest.mark.parametrize("far", [None, (1 << 20) + 7, -9])
+def test_append(name, far):
+    b = Batch(L=2, seed=len(name), fill=7.5, **APPEND[name])
+    cache, seqs, q, k, v = b.cuda()
+    pos = None
+    if far is not None:
+        pos = [far + 3 * i for i in range(b.N)]
+    got = cache.append(1, seqs, k, v, q=q, rope=dict(theta=1e6, scale=1.25),
+                       positions=None if pos is None else torch.tensor(pos, dtype=torch.int32).cuda())
+    pool, qo, ep, eq = append_oracle(b, 1, scale=1.25, positions=pos)
+    assert_within(cache.pool, pool, ep, "cache")        # what no token was appended to: exactly
+    assert_within(got, qo, eq, "queries")
+
+
+def test_append_copies_without_rope_and_in_place():
+    b = Batch(L=1, seed=4, **APPEND["ragged"])
+    cache, seqs, q, k, v = b.cuda()
+    k[0, 0, 0] = float("nan")
+    b.kh[0, 0, 0] = float("nan")
+    out = cache.append(0, seqs, k, v, q=q)
+    pool, _, ep, _ = append_oracle(b, 0, rotate=False)
+    assert_within(cache.pool, pool, ep * 0, "cache")
+    assert torch.equal(out, q)
+    cache.append(0, seqs, k, v)                          # no queries
+    ref = cache.append(0, seqs, k, v, q=q, rope=dict(theta=1e4))
+    same = q.clone()
+    assert cache.append(0, seqs, k, v, q=same, q_out=same, rope=dict(theta=1e4)) is same
+    assert torch.equal(same, ref)
+
+
+def test_append_frequency_table_and_many_sequences():
+    """300 sequences of zero to two tokens (more than one launch's table), the
+    model's own frequencies."""
+    q = [i % 3 for i in range(300)]
+    b = Batch("bf16", 4, 2, 64, 4, q, [n + i % 7 for i, n in enumerate(q)], seed=9)
+    cache, seqs, qh, k, v = b.cuda()
+    f = [1e4 ** (-i / 32) / (1 + i % 2) for i in range(32)]
+    got = cache.append(0, seqs, k, v, q=qh, rope=dict(inv_freq=f))
+    pos = torch.tensor([j for _, j in b.slots()], dtype=torch.float64)
+    ang = pos[:, None, None] * torch.tensor(f, dtype=torch.float32).double()
+    u, w = b.qh[..., :32].double(), b.qh[..., 32:].double()
+    ref = torch.cat([u * ang.cos() - w * ang.sin(), w * ang.cos() + u * ang.sin()], -1)
+    size = torch.cat([u.abs() + w.abs()] * 2, -1)
+    assert_within(got, ref, 2.0 ** -20 * size + 2.0 ** -8 * ref.abs(), "queries")
+
+
+def test_append_drops_tokens_of_no_block():
+    b = Batch("bf16", 2, 2, 64, 4, [6, 6], [10, 12], seed=5, fill=7.5)
+    b.table[0, 1], b.table[1, 2] = -1, b.n_blocks       # slots 4-7, slots 8-11
+    cache, seqs, q, k, v = b.cuda()
+    got = cache.append(0, seqs, k, v, q=q, rope=dict(theta=1e6))
+    pool, qo, ep, eq = append_oracle(b, 0)
+    assert_within(cache.pool, pool, ep, "cache")
+    assert_within(got, qo, eq, "queries")
+
+
+# ------------------------------------------------------------------- attend
+def _check(b, layer=0, shared=0, what="", **opt):
+    """attend against the oracle, twice to the same bits."""
+    cache, seqs, q, _, _ = b.cuda()
+    dev = {k: torch.tensor(v, dtype=torch.int32).cuda() if k in ("lo", "hi") else v
+           for k, v in opt.items()}
+    lse = torch.empty(b.N, b.heads, device="cuda")
+    out = cache.attend(layer, seqs, q, lse=lse, shared_len=shared, **dev)
+    again = cache.attend(layer, seqs, q, shared_len=shared, **dev)
+    ref, rl, tol, ltol = attend_oracle(b, layer, **opt)
+    assert_within(out, ref, tol, what + "out")
+    assert_within(lse, rl, ltol, what + "lse")
+    assert torch.equal(out.view(torch.int16 if b.dtype == "bf16" else torch.int32),
+                       again.view(torch.int16 if b.dtype == "bf16" else torch.int32))
+    return out
+
+
+ATTEND = {
+    "decode": dict(dtype="bf16", heads=16, kv_heads=2, d=128, bs=16, q=[1] * 8,
+                   lens=[1, 2, 63, 64, 65, 300, 1000, 17]),
+    "decode-f32": dict(dtype="f32", heads=4, kv_heads=2, d=128, bs=16, q=[1] * 4, lens=[1, 31, 129, 700]),
+    "ragged": dict(dtype="bf16", heads=12, kv_heads=4, d=64, bs=8, q=[0, 1, 17, 130, 5],
+                   lens=[4, 200, 17, 300, 700]),
+    "ragged-f32": dict(dtype="f32", heads=6, kv_heads=2, d=64, bs=4, q=[3, 0, 41], lens=[3, 5, 150]),
+    "one-token": dict(dtype="bf16", heads=2, kv_heads=2, d=64, bs=1, q=[1], lens=[1]),
+    "many-heads": dict(dtype="bf16", heads=40, kv_heads=1, d=64, bs=16, q=[1, 4], lens=[90, 260]),
+    "group-of-7": dict(dtype="bf16", heads=28, kv_heads=4, d=128, bs=16, q=[1, 9, 1], lens=[70, 80, 500]),
+    "prompt": dict(dtype="bf16", heads=4, kv_heads=2, d=128, bs=64, q=[333], lens=[333]),
+    "long": dict(dtype="bf16", heads=2, kv_heads=1, d=128, bs=16, q=[1], lens=[20001]),
+    "long-pages-of-1": dict(dtype="bf16", heads=2, kv_heads=1, d=64, bs=1, q=[2], lens=[2500]),
+    "pages-of-1024": dict(dtype="bf16", heads=2, kv_heads=1, d=64, bs=1024, q=[1, 1], lens=[1025, 3000]),
+    "d32": dict(dtype="bf16", heads=4, kv_heads=2, d=32, bs=16, q=[1, 20], lens=[100, 77]),
+    "d96": dict(dtype="bf16", heads=4, kv_heads=2, d=96, bs=16, q=[1, 20], lens=[100, 277]),
+    "d160": dict(dtype="bf16", heads=4, kv_heads=2, d=160, bs=16, q=[1, 20], lens=[100, 77]),
+    "d224-f32": dict(dtype="f32", heads=4, kv_heads=2, d=224, bs=16, q=[1, 20], lens=[100, 77]),
+    "d192-f32": dict(dtype="f32", heads=2, kv_heads=2, d=192, bs=2, q=[70], lens=[90]),
+    "d256": dict(dtype="bf16", heads=4, kv_heads=1, d=256, bs=16, q=[1, 50], lens=[400, 77]),
+    "d256-f32": dict(dtype="f32", heads=4, kv_heads=1, d=256, bs=16, q=[1, 30], lens=[300, 77]),
+    # lengths that leave queries without a key of their own
+    "short": dict(dtype="bf16", heads=4, kv_heads=2, d=64, bs=4, q=[5, 2, 1, 3], lens=[3, -2, 0, 40]),
+}
+
+
+@pytest.mark.parametrize("name", ATTEND)
+def test_attend_causal(name):
+    # rows of the cache in no sequence's slots hold NaN: they are never seen
+    _check(Batch(L=2, seed=len(name), fill=float("nan"), table_slack=1, **ATTEND[name]), layer=1)
+
+
+@pytest.mark.parametrize("name", ["decode", "ragged", "ragged-f32", "group-of-7", "d96", "d256-f32", "short"])
+@pytest.mark.parametrize("kind", ["capped", "bias", "capped-bias-documents", "windows", "all"])
+def test_attend_options(name, kind):
+    b = Batch(seed=3 + len(kind), **ATTEND[name])
+    rng = np.random.default_rng(7)
+    p = np.array([j for _, j in b.slots()])
+    n = np.repeat(np.maximum(b.lens, 0), b.q)
+    slopes = [2.0 ** (-8.0 * (h + 1) / b.heads) for h in range(b.heads)]
+    opt = {}
+    if "capped" in kind:
+        opt["softcap"] = 5.0
+    if "bias" in kind:
+        opt["slopes"] = slopes
+    if "documents" in kind:                       # every third query sees nothing
+        opt["lo"] = rng.integers(-3, np.maximum(p, 0) + 1)
+        opt["hi"] = np.where(np.arange(b.N) % 3 == 0, opt["lo"], p + 1)
+    if kind == "windows":                         # the 20 keys before, none of the later ones
+        opt["lo"] = p - 20
+    if kind == "all":                             # hi beyond the length, a scale of its own
+        opt["hi"] = n + 1000
+        opt["scale"] = 0.3
+    _check(b, **opt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_of_hidden_keys_do_not_matter(dtype):
+    """Infinities and NaN in keys that some rows of a tile see and others do
+    not: a padded batch, documents of another query."""
+    b = Batch(dtype, 4, 2, 64, 8, [40, 3], [60, 3], seed=21)
+    slot = {(s, j): t for t, (s, j) in enumerate(b.slots())}
+    hidden = {}
+    for j, kv, x in [(33, 1, float("inf")), (45, 1, float("nan")), (50, 1, -float("inf")),
+                     (52, 0, float("nan")), (58, 0, float("inf"))]:
+        at = b.row(0, j)
+        b.pool[0, kv, at[0], at[1], 1, 5] = x
+        hidden[j] = x
+    out = _check(b)
+    first = slot[(0, 33)]
+    assert torch.isfinite(out[:first]).all()      # rows before the first odd value: finite
+    assert torch.isfinite(out[:, :2]).all()       # the other KV head never
+    assert torch.isnan(out[slot[(0, 46)], 2:, 5]).all() and torch.isinf(out[slot[(0, 40)], 2:, 5]).all()
+    lo = np.zeros(b.N, int)
+    lo[:40] = 59
+    hi = np.full(b.N, 60)
+    hi[5] = 0
+    out = _check(b, lo=lo, hi=hi)                 # every query sees one key, one sees none
+    assert torch.isfinite(out).all() and (out[5] == 0).all()
+
+
+def test_blocks_that_are_none_are_not_seen():
+    b = Batch("bf16", 4, 2, 64, 4, [1, 30], [200, 90], seed=22)
+    b.table[0, 3], b.table[0, 20], b.table[1, 2], b.table[1, 22] = -1, b.n_blocks, 1 << 30, -(1 << 31)
+    _check(b)
+    b.table[:] = -1
+    out = _check(b)
+    assert (out == 0).all()
+
+
+def test_length_beyond_the_table_counts_as_the_table():
+    b = Batch("bf16", 4, 2, 64, 4, [1, 2], [41, 16], seed=23)
+    cache, _, q, _, _ = b.cuda()
+    lens = torch.tensor([1 << 30, 16], dtype=torch.int32).cuda()
+    seqs = cache.sequences(b.table.cuda(), lens, b.off)
+    b.lens = [44, 16]
+    out = cache.attend(0, seqs, q)
+    ref, _, tol, _ = attend_oracle(b, 0)
+    assert_within(out, ref, tol, "out")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("shared,q,lens", [
+    (64, [1] * 6, [64, 65, 100, 2, 700, 128]),        # a sequence that ends inside the prefix
+    (1100, [1, 3, 0, 20], [1101, 1180, 1100, 1500]),
+    (999, [2, 2], [1200, 1003]),                      # ends inside a page
+])
+def test_shared_prefix(dtype, d, shared, q, lens):
+    b = Batch(dtype, 8, 2, d, 16, q, lens, seed=31, shared=-(-shared // 16) * 16)
+    plain = _check(b)
+    out = _check(b, shared=shared, what="shared ")
+    assert (out.float() - plain.float()).abs().max() < (2.0 ** -6 if dtype == "bf16" else 1e-5)
+    p = np.array([j for _, j in b.slots()])
+    _check(b, shared=shared, lo=p - 300, hi=np.where(p % 4 == 1, 0, p + 1), softcap=8.0,
+           slopes=[0.01 * h for h in range(8)])
+
+
+def test_pool_of_other_strides_and_strided_rows():
+    """Block-major pool with K and V and layers inside a block; queries and
+    results with strides of their own; only the result's rows are written."""
+    b = Batch("bf16", 4, 2, 64, 8, [9, 1], [50, 30], L=3, seed=41)
+    from paper_2609_35139_amd.serving import PagedCache
+    pool = torch.empty(b.n_blocks, 3, 2, 2, 8, 64 + 8, dtype=torch.bfloat16, device="cuda")
+    view = pool[..., :64].permute(1, 2, 0, 4, 3, 5)     # [L][2][n_blocks][bs][H][d]
+    view.copy_(b.pool.cuda())
+    cache = PagedCache(view)
+    seqs = cache.sequences(b.table.cuda(), torch.tensor(b.lens, dtype=torch.int32).cuda(), b.off)
+    out = torch.full((4, b.N + 2, 80), 3.0, dtype=torch.bfloat16, device="cuda")
+    o = out[:, 1:-1, 8:72].permute(1, 0, 2)
+    q = b.qh.permute(1, 0, 2).contiguous().cuda().permute(1, 0, 2)
+    cache.attend(2, seqs, q, out=o)
+    ref, _, tol, _ = attend_oracle(b, 2)
+    assert_within(o, ref, tol, "out")
+    o.fill_(3.0)
+    assert (out == 3.0).all()
+    k, v = b.kh.cuda().expand(-1, 2, -1), b.vh[:, :1].cuda().expand(-1, 2, -1)   # one value for both heads
+    b.vh = b.vh[:, :1].expand(-1, 2, -1)
+    cache.append(0, seqs, k, v, rope=dict(theta=1e6))
+    p, _, ep, _ = append_oracle(b, 0)
+    assert_within(view, p, ep, "cache")
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond 2^32 elements of a pool of 9.7 GB."""
+    from paper_2609_35139_amd.serving import PagedCache
+    b = Batch("bf16", 4, 2, 128, 16, [1, 5], [40, 90], seed=43)
+    far = 600_000
+    pool = torch.empty(1, 2, far + b.n_blocks, 16, 2, 128, dtype=torch.bfloat16, device="cuda")
+    pool[:, :, far:] = b.pool.cuda()
+    cache = PagedCache(pool)
+    table = torch.where(b.table >= 0, b.table + far, b.table).cuda()
+    seqs = cache.sequences(table, torch.tensor(b.lens, dtype=torch.int32).cuda(), b.off)
+    q = cache.append(0, seqs, b.kh.cuda(), b.vh.cuda(), q=b.qh.cuda(), rope=dict(theta=1e6))
+    p, qo, ep, eq = append_oracle(b, 0)
+    assert_within(pool[:, :, far:], p, ep, "cache")
+    assert_within(q, qo, eq, "queries")
+    out = cache.attend(0, seqs, q)
+    ref, _, tol, _ = attend_oracle(b, 0, pool=pool[:, :, far:].cpu(), q=q.cpu())
+    assert_within(out, ref, tol, "out")
+
+
+# ---------------------------------------------------------------- in a program
+def test_decode_steps_in_a_captured_graph_on_another_stream():
+    """A captured step (append, attend, two layers) replayed while lengths,
+    tables and inputs move on, against the same step run eagerly and against
+    the definition; two graphs share one workspace, in turn."""
+    from paper_2609_35139_amd.serving import PagedCache
+    b = Batch("bf16", 8, 2, 64, 4, [1] * 3, [90, 700, 5], L=2, seed=51, spare=40)
+    table = torch.full((3, 190), -1, dtype=torch.int32)
+    table[:, :b.table.shape[1]] = b.table
+    free = [i for i in range(b.n_blocks) if i not in set(b.table.flatten().tolist())]
+    for s, n in enumerate(b.lens):                       # room for the steps to come
+        have = -(-n // 4)
+        table[s, have:have + 4] = torch.tensor([free.pop() for _ in range(4)])
+    b.table = table
+    side = torch.cuda.Stream()
+    dt, rope = torch.bfloat16, dict(theta=1e6)
+
+    def world():
+        cache = PagedCache(b.pool.cuda())
+        lens = torch.tensor([n - 1 for n in b.lens], dtype=torch.int32).cuda()
+        new = torch.zeros(2, 3, 12, 64, dtype=dt, device="cuda")
+        return cache, lens, cache.sequences(table.cuda(), lens), new, torch.zeros(2, 3, 8, 64, dtype=dt, device="cuda")
+
+    def step(w, ws, stream):
+        cache, lens, seqs, new, out = w
+        for layer in range(2):
+            q, k, v = new[layer, :, :8], new[layer, :, 8:10], new[layer, :, 10:]
+            q = cache.append(layer, seqs, k, v, q=q, rope=rope, stream=stream)
+            cache.attend(layer, seqs, q, out=out[layer], workspace=ws, stream=stream)
+
+    eager, a = world(), world()
+    ws = a[0].workspace(a[2], 8)
+    side.wait_stream(torch.cuda.current_stream())
+    a[1].add_(1)
+    step(a, ws, side)                                    # warm-up, over slots written again below
+    side.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step(a, ws, side)
+        graphs.append(g)
+    a[1].sub_(1)
+    gen = torch.Generator().manual_seed(5)
+    for i in range(5):
+        x = torch.randn(2, 3, 12, 64, generator=gen).to(dt)
+        for w in (eager, a):
+            w[1].add_(1)
+            w[3].copy_(x)
+        torch.cuda.synchronize()
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(eager, None, None)
+        assert torch.equal(a[4], eager[4]) and torch.equal(a[0].pool, eager[0].pool)
+        b.lens = eager[1].tolist()
+        q = eager[0].append(1, eager[2], x[1, :, 8:10].cuda(), x[1, :, 10:].cuda(), q=x[1, :, :8].cuda(), rope=rope)
+        ref, _, tol, _ = attend_oracle(b, 1, pool=eager[0].pool.cpu(), q=q.cpu())
+        assert_within(a[4][1], ref, tol, f"step {i}")
+
+
+def test_repaired_cache_is_answered_over():
+    """Repair into pages with the keys placed, append a question, attend with
+    the documents shared by two questions: the whole path of a request."""
+    import workloads as W
+    from helpers import repairer_for, small_workload, to_device
+    from paper_2609_35139_amd import binding as B
+    from paper_2609_35139_amd.serving import PagedCache
+    w = small_workload(((70, 61, 29),), dtype="bf16", L=2, H=2, dh=64, E=128, d_c=64, d_b=128,
+                       n_heads=2, d_seg=8, ffn_mult=4)
+    inp = W.make_inputs(w)
+    rep = repairer_for(w, inp.weights)
+    bs, doc = 16, 160
+    q = [5, 12]
+    b = Batch("bf16", 4, 2, 64, bs, q, [doc + n for n in q], L=2, seed=61, shared=doc)
+    cache, seqs, qh, k, v = b.cuda()
+    lay, sB = B.paged_layout(2, 2, 64, b.n_blocks, bs, B.CR_DTYPE_BF16)
+    kv, emb = to_device(w, inp.kv), to_device(w, inp.token_embeds)
+    pages = dict(block_size=bs, n_blocks=b.n_blocks, stride_block=sB, block_table=b.table[0, :doc // bs])
+    rep.repair(kv, w.chunk_offsets, w.request_chunks, emb,
+               options=B.Options(global_rope=dict(theta=1e6), kv_out=cache.pool.data_ptr(),
+                                 layout_out=lay, pages_out=pages))
+    before = cache.pool.cpu()
+    b.pool = before
+    assert not torch.equal(before[:, :, b.table[0, 0]], Batch("bf16", 4, 2, 64, bs, q, b.lens, L=2, seed=61, shared=doc).pool[:, :, b.table[0, 0]])
+    for layer in range(2):
+        b.pool = cache.pool.cpu()
+        qr = cache.append(layer, seqs, k, v, q=qh, rope=dict(theta=1e6))
+        pool, qo, ep, eq = append_oracle(b, layer)
+        assert_within(cache.pool, pool, ep, "cache")
+        out = cache.attend(layer, seqs, qr, shared_len=doc)
+        ref, _, tol, _ = attend_oracle(b, layer, pool=cache.pool.cpu(), q=qr.cpu())
+        assert_within(out, ref, tol, f"layer {layer}")
+
+
+def test_profile_names_the_launches():
+    from paper_2609_35139_amd import binding as B
+    b = Batch(seed=1, **ATTEND["decode"])
+    cache, seqs, q, k, v = b.cuda()
+    B.cr_profile_enable(16)
+    try:
+        cache.append(0, seqs, k, v, q=q, rope=dict(theta=1e6))
+        cache.attend(0, seqs, q)
+        stats = {r["name"]: r["launches"] for r in B.cr_profile_read()}
+    finally:
+        B.cr_profile_enable(0)
+    assert stats["append_kv"] == 1 and stats["attend"] == 1
