@@ -640,6 +640,56 @@ __global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
               lt[n] == 0.f ? -INFINITY : (m[n] + __log2f(lt[n])) / kLog2e;
       }
     }
+  } else {
+    // the groups' (max, sum, o) through LDS, then 8 dims of a row per thread
+    float* mo = reinterpret_cast<float*>(lds);
+    float2* ml = reinterpret_cast<float2*>(mo + KG * C::ROWS * C::MLD);
+    __syncthreads();                       // every ring is idle
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const int r = kg * C::ROWS + (rg * NQ + n) * 16 + c16;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (EXACT || d * 16 < D)
+          *reinterpret_cast<f32x4*>(mo + r * C::MLD + d * 16 + 4 * g) = oacc[n][d];
+      if (g == 0) ml[r] = make_float2(m[n], lt[n]);
+    }
+    __syncthreads();
+    const int per_row = D / 8;
+    for (int idx = tid; idx < n_rows * per_row; idx += C::NT) {
+      const int r = idx / per_row, d0 = (idx - r * per_row) * 8;
+      float mx = -INFINITY, sum = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KG; ++k) mx = fmaxf(mx, ml[k * C::ROWS + r].x);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int k = 0; k < KG; ++k) {
+        const float2 w = ml[k * C::ROWS + r];
+        if (w.y == 0.f) continue;          // saw nothing (a NaN sum counts)
+        const float f = __builtin_amdgcn_exp2f((w.x == -INFINITY ? 0.f : w.x) - ref);
+        sum += f * w.y;
+        const float* x = mo + (k * C::ROWS + r) * C::MLD + d0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += f * x[e];
+      }
+      if (partial) {
+        float* po = a.part_o + (prow + r) * D + d0;
+        *reinterpret_cast<f32x4*>(po) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(po + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        if (d0 == 0) a.part_ml[prow + r] = make_float2(mx, sum);
+        continue;
+      }
+      const int i = (row0 + r) / a.group, hd = head * a.group + row0 + r - i * a.group;
+      const int64_t t = x.tok0 + i;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= inv;
+      Vec8<T> o8;
+      o8.from_float(v);
+      o8.store(static_cast<T*>(a.o) + t * a.o_token + (int64_t)hd * a.o_head + d0);
+      if (d0 == 0 && a.lse)
+        a.lse[t * a.n_kv * a.group + hd] = sum == 0.f ? -INFINITY : (mx + __log2f(sum)) / kLog2e;
+    }
   }
 }
 
@@ -725,11 +775,21 @@ hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, hipStream_t 
 // ------------------------------------------------------------------ launch
 template <typename T, int DM, bool EXACT>
 hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
-  constexpr int KT = sizeof(T) == 2 ? (DM > 128 ? 32 : 64) : (DM > 128 ? 16 : 32);
-  constexpr int NQ = attend_rows(sizeof(T), DM) / 64;
-  if (a.rows != 64 * NQ) return hipErrorInvalidValue;
-  CR_LAUNCH((attend_kernel<T, DM, EXACT, NQ, 4, 1, KT, 2>), dim3((unsigned)(items * a.n_kv)),
-            dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(items * a.n_kv));
+  constexpr int WIDE = attend_rows(sizeof(T), DM), KEYS = ValueOps<T>::KEYS;
+  // 16 rows (the heads of a group for one new token): bound by reading the
+  // keys.  Two waves with a ring of two 16 KB tiles of their own each (32 KB
+  // for wide heads), two workgroups to a CU.
+  constexpr int NARROW = 64 * 128 / (DM * (int)sizeof(T));
+  constexpr int KN = NARROW < KEYS ? KEYS : NARROW;
+  constexpr int KW = sizeof(T) == 2 ? (DM > 128 ? 32 : 64) : (DM > 128 ? 16 : 32);
+  if (a.rows == 16) {
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a);
+  } else if (a.rows == WIDE) {
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2>), grid, dim3(256), 0, s, a);
+  } else {
+    return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 

@@ -100,7 +100,7 @@ const char* component(const void* kv, const cr_kv_layout* l, int layer, int c) {
 // How one cr_attend call is cut up; a function of what the host knows, so the
 // workspace can be sized ahead of the lengths.
 struct Plan {
-  int rows = 0;                  // rows of a unit
+  int rows = 0, pre_rows = 0;    // rows of a unit of either pass
   int64_t units = 0;             // of the pass over each sequence's own keys
   int slots = 0, min_tiles = 0;  // its split (slots 0: none)
   int64_t own_items = 0;         // partial results of that pass, per KV head
@@ -113,7 +113,9 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
                  int shared) {
   Plan p;
   const int G = n_heads / l->n_kv_heads, D = l->head_dim, H = l->n_kv_heads;
-  p.rows = attend_rows((int)esize(l->dtype), D);
+  const int wide = attend_rows((int)esize(l->dtype), D);
+  p.rows = b.most * G <= 16 ? 16 : wide;
+  p.pre_rows = b.n_tokens * G <= 16 ? 16 : wide;
   auto tiles = [&](int64_t n) { return ceil_div(n * G, p.rows); };
   if (b.off) {
     for (int s = 0; s < q->n_seqs; ++s) p.units += tiles(b.off[s + 1] - b.off[s]);
@@ -123,14 +125,14 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   Arena a;
   if (b.off) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
   // split the keys unless the units fill the chip by themselves
-  if (p.units * H < 512) {
-    p.slots = (int)std::max<int64_t>(1, 512 / H);
+  if (p.units * H < (p.rows == 16 ? 8192 : 512)) {
+    p.slots = (int)std::max<int64_t>(1, (p.rows == 16 ? 1024 : 512) / H);
     p.min_tiles = 4;
     // one part holds all keys there can be
     if ((int64_t)q->max_blocks * q->block_size <= p.min_tiles * 64) p.slots = 0;
   }
   if (p.slots && shared > 0) {
-    p.pre_units = tiles(b.n_tokens);
+    p.pre_units = ceil_div(b.n_tokens * G, p.pre_rows);
     const int64_t key_tiles = ceil_div(shared, 64);
     const int64_t want = std::max<int64_t>(1, 512 / (p.pre_units * H));
     p.split_tiles = (int)std::max<int64_t>(p.min_tiles, ceil_div(key_tiles, want));
@@ -138,7 +140,7 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   }
   p.own_items = p.slots ? p.units + p.slots : 0;
   const uint64_t own = (uint64_t)p.own_items * H * p.rows;
-  const uint64_t pre = (uint64_t)p.pre_units * p.splits * H * p.rows;
+  const uint64_t pre = (uint64_t)p.pre_units * p.splits * H * p.pre_rows;
   p.own_ml = a.take(own * 8);
   p.own_o = a.take(own * D * 4);
   p.pre_ml = a.take(pre * 8);
@@ -224,6 +226,7 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
   if (p.pre_units) {
     pre = a;
     pre.shared = o.shared_len;
+    pre.rows = p.pre_rows;
     pre.n_units = (int)p.pre_units;
     pre.slots = 0;
     pre.splits = p.splits;
