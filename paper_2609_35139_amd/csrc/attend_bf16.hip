@@ -3,5 +3,5 @@
 
 namespace cr {
 template hipError_t attend<bf16>(const AttendArgs&, hipStream_t);
-template hipError_t attend_merge<bf16>(const AttendArgs&, const AttendArgs&, hipStream_t);
+template hipError_t attend_merge<bf16>(const AttendArgs&, const AttendArgs&, int, hipStream_t);
 }  // namespace cr

@@ -3,5 +3,5 @@
 
 namespace cr {
 template hipError_t attend<float>(const AttendArgs&, hipStream_t);
-template hipError_t attend_merge<float>(const AttendArgs&, const AttendArgs&, hipStream_t);
+template hipError_t attend_merge<float>(const AttendArgs&, const AttendArgs&, int, hipStream_t);
 }  // namespace cr

@@ -694,81 +694,121 @@ __global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
 }
 
 // ------------------------------------------------------------------- merge
-// One workgroup per (query, head): its waves share the row's partial results,
-// those of the pass over the shared keys (pre) and those of its own unit.
-template <typename T>
-__global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendArgs pre) {
-  __shared__ float part[4][256 + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
-  const int n_heads = a.n_kv * a.group;
-  const int t = blockIdx.x / n_heads, h = blockIdx.x - t * n_heads;
-  const int head = h / a.group, g = h - head * a.group;
-  int s, i, unit;
-  if (a.unit_off) {
-    s = find_offset(a.q_off, a.seqs.n_seqs, t);
-    i = t - a.q_off[s];
-    unit = a.unit_off[s];
-  } else {
-    s = t / a.q_per_seq;
-    i = t - s * a.q_per_seq;
-    unit = s * a.units_per_seq;
-  }
-  const int tile = (i * a.group + g) / a.rows, row = i * a.group + g - tile * a.rows;
-  unit += tile;
+// Joins a row's partial results, those of the pass over the shared keys (pre)
+// and those of its own unit: o = sum_j 2^(m_j - m) o_j / sum_j 2^(m_j - m) l_j.
+// A workgroup takes RPW rows of one unit and KV head; 256 / RPW threads share
+// a row, 4 dims each, the others taking every (STREAMS)-th part.  The weights
+// go through LDS first, so that the loads of o depend on nothing.
+constexpr int kMergeParts = 512;   // weights held at a time
+template <typename T, int RPW>
+__global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendArgs pre,
+                                                           int row_blocks) {
+  __shared__ float wts[RPW][kMergeParts / RPW];
+  __shared__ __align__(16) float sums[256 * 4];
+  __shared__ float lsum[256];
+  constexpr int TPR = 256 / RPW, CHUNK = kMergeParts / RPW;
+  const int D = a.head_dim, tpd = D / 4;                  // threads per part
+  const int rb = blockIdx.x % row_blocks;
+  const int head = blockIdx.x / row_blocks % a.n_kv, unit = blockIdx.x / row_blocks / a.n_kv;
+  const Unit x = unit_of(a, unit);
+  const int row0 = x.tile * a.rows, n_rows = min(a.rows, x.nq * a.group - row0);
+  if (rb * RPW >= n_rows) return;
   const Item it = plan_item(a, -1, unit);
-  if (it.unit < 0 || (it.parts == 1 && !a.always_partial)) return;   // written already
+  if (it.parts == 1 && !a.always_partial) return;         // written already
+  const int rl = threadIdx.x / TPR, tr = threadIdx.x % TPR;
+  const int r = rb * RPW + rl;
+  const bool valid = r < n_rows;
+  const int rr = valid ? r : n_rows - 1;                  // (a row of its own for every thread)
+  const int i = (row0 + rr) / a.group, g = row0 + rr - i * a.group;
+  const int t = x.tok0 + i, h = head * a.group + g;
   const int n_pre = pre.shared ? pre.splits : 0, P = n_pre + it.parts;
-  const int prow = t * a.group + g;      // the row in the tiles over all sequences
-  const int ptile = pre.shared ? prow / pre.rows : 0;
-  auto index = [&](int j, const float2** ml) -> const float* {
-    const bool p = j < n_pre;
-    const AttendArgs& x = p ? pre : a;
-    const int64_t item = p ? (int64_t)ptile * n_pre + j : it.first + (j - n_pre);
-    const int64_t r = (item * a.n_kv + head) * x.rows + (p ? prow - ptile * pre.rows : row);
-    *ml = x.part_ml + r;
-    return x.part_o + r * D;
+  // part j: row index into the partial results of its pass
+  const int prow = t * a.group + g, ptile = pre.shared ? prow / pre.rows : 0;
+  const int64_t pre_at = ((int64_t)ptile * n_pre * a.n_kv + head) * pre.rows + prow - ptile * pre.rows;
+  const int64_t own_at = ((int64_t)it.first * a.n_kv + head) * a.rows + rr;
+  const int64_t pre_step = (int64_t)a.n_kv * pre.rows, own_step = (int64_t)a.n_kv * a.rows;
+  auto ml_of = [&](int j) {
+    return j < n_pre ? pre.part_ml[pre_at + j * pre_step] : a.part_ml[own_at + (j - n_pre) * own_step];
   };
+  auto o_of = [&](int j) {
+    return j < n_pre ? pre.part_o + (pre_at + j * pre_step) * D
+                     : a.part_o + (own_at + (j - n_pre) * own_step) * D;
+  };
+  // maximum over the row's parts (a part that saw nothing has sum 0; a NaN sum
+  // counts, its maximum may be -inf)
   float m = -INFINITY;
-  for (int j = lane; j < P; j += 64) {
-    const float2* ml;
-    index(j, &ml);
-    if (ml->y != 0.f) m = fmaxf(m, ml->x);      // (a NaN sum counts, its maximum may be -inf)
+  for (int j = tr; j < P; j += TPR) {
+    const float2 v = ml_of(j);
+    if (v.y != 0.f) m = fmaxf(m, v.x);
   }
+  constexpr int SH = TPR < 64 ? TPR : 64;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  for (int o = SH / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) lsum[threadIdx.x / 64] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(lsum[0], lsum[1]), fmaxf(lsum[2], lsum[3]));
+    __syncthreads();
+  }
   const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int j = wave; j < P; j += 4) {
-    const float2* ml;
-    const float* po = index(j, &ml);
-    const float2 v = *ml;
-    if (v.y == 0.f) continue;                   // saw nothing
-    const float w = __builtin_amdgcn_exp2f((v.x == -INFINITY ? 0.f : v.x) - ref);
-    l += w * v.y;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 64 * k < D) o[k] += w * po[lane + 64 * k];
+  const int streams = TPR / tpd, sj = tr / tpd, d0 = (tr - sj * tpd) * 4;
+  const bool active = sj < streams;
+  float l = 0.f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < P; j0 += CHUNK) {
+    const int n = min(CHUNK, P - j0);
+    __syncthreads();
+    for (int j = tr; j < n; j += TPR) {
+      const float2 v = ml_of(j0 + j);
+      const float w = v.y == 0.f ? 0.f
+                                 : __builtin_amdgcn_exp2f((v.x == -INFINITY ? 0.f : v.x) - ref);
+      wts[rl][j] = w;
+      l += w * v.y;
+    }
+    __syncthreads();
+    if (active) {
+#pragma unroll 8
+      for (int j = sj; j < n; j += streams)
+        o += wts[rl][j] * *reinterpret_cast<const f32x4*>(o_of(j0 + j) + d0);
+    }
   }
+  // sums over the row's threads, in a fixed order
+  *reinterpret_cast<f32x4*>(sums + threadIdx.x * 4) = o;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = o[k];
-  if (lane == 0) part[wave][256] = l;
+  for (int k = SH / 2; k > 0; k >>= 1) l += __shfl_xor(l, k);
+  lsum[threadIdx.x] = l;
   __syncthreads();
-  l = (part[0][256] + part[1][256]) + (part[2][256] + part[3][256]);
-  const int d = threadIdx.x;
-  if (d < D) {
-    const float v = (part[0][d] + part[1][d]) + (part[2][d] + part[3][d]);
-    static_cast<T*>(a.o)[(int64_t)t * a.o_token + (int64_t)h * a.o_head + d] =
-        from_f32<T>(l == 0.f ? 0.f : v / l);
-  }
-  if (d == 0 && a.lse)
-    a.lse[(int64_t)t * n_heads + h] = l == 0.f ? -INFINITY : (m + __log2f(l)) / kLog2e;
+  if (TPR > 64) l = (lsum[0] + lsum[64]) + (lsum[128] + lsum[192]);
+  if (!valid || sj != 0) return;
+  for (int k = 1; k < streams; ++k)
+    o += *reinterpret_cast<const f32x4*>(sums + (threadIdx.x + k * tpd) * 4);
+  T* op = static_cast<T*>(a.o) + (int64_t)t * a.o_token + (int64_t)h * a.o_head + d0;
+  T w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(l == 0.f ? 0.f : o[e] / l);
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(op) = *reinterpret_cast<const uint2*>(w);
+  else
+    *reinterpret_cast<uint4*>(op) = *reinterpret_cast<const uint4*>(w);
+  if (d0 == 0 && a.lse)
+    a.lse[(int64_t)t * a.n_kv * a.group + h] =
+        l == 0.f ? -INFINITY : (m + __log2f(l)) / kLog2e;
 }
 
 template <typename T>
-hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, hipStream_t s) {
-  const int64_t rows = (int64_t)a.n_tokens * a.n_kv * a.group;
-  CR_LAUNCH((attend_merge_kernel<T>), dim3((unsigned)rows), dim3(256), 0, s, a, pre);
+hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, int most_rows, hipStream_t s) {
+  // one row per workgroup while there are few (their parts are many), else as
+  // many as leave a row's dims to one wave's threads
+  const int rows = most_rows < a.rows ? most_rows : a.rows;
+  const int64_t tiles = (int64_t)a.n_units * a.n_kv;
+  if (tiles * rows <= 4096) {
+    CR_LAUNCH((attend_merge_kernel<T, 1>), dim3((unsigned)(tiles * rows)), dim3(256), 0, s, a, pre,
+              rows);
+  } else {
+    const int blocks = (rows + 3) / 4;
+    CR_LAUNCH((attend_merge_kernel<T, 4>), dim3((unsigned)(tiles * blocks)), dim3(256), 0, s, a,
+              pre, blocks);
+  }
   return hipGetLastError();
 }
 

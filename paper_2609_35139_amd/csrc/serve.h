@@ -77,8 +77,8 @@ template <typename T>
 hipError_t attend(const AttendArgs& a, hipStream_t s);
 
 // Joins the partial results of a planned pass and, with pre.shared > 0, those
-// of the pass over the shared keys.
+// of the pass over the shared keys.  most_rows: rows of the longest sequence.
 template <typename T>
-hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, hipStream_t s);
+hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, int most_rows, hipStream_t s);
 
 }  // namespace cr

@@ -239,7 +239,10 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
     CR_TRY(timed("attend_shared", s, [&] { return attend<T>(pre, s); }));
   }
   CR_TRY(timed("attend", s, [&] { return attend<T>(a, s); }));
-  if (p.slots) CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, pre, s); }));
+  if (p.slots) {
+    const int most_rows = (int)std::min<int64_t>(b.most * a.group, p.rows);
+    CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, pre, most_rows, s); }));
+  }
   return CR_OK;
 }
 

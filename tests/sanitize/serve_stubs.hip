@@ -16,7 +16,7 @@ hipError_t append_kv(const AppendArgs&, const KeyRope&, const int32_t*, hipStrea
 template <typename T>
 hipError_t attend(const AttendArgs&, hipStream_t) { return hipErrorInvalidValue; }
 template <typename T>
-hipError_t attend_merge(const AttendArgs&, const AttendArgs&, hipStream_t) {
+hipError_t attend_merge(const AttendArgs&, const AttendArgs&, int, hipStream_t) {
   return hipErrorInvalidValue;
 }
 
@@ -24,7 +24,7 @@ hipError_t attend_merge(const AttendArgs&, const AttendArgs&, hipStream_t) {
   template hipError_t append_kv<T>(const AppendArgs&, const KeyRope&, const int32_t*,        \
                                    hipStream_t);                                             \
   template hipError_t attend<T>(const AttendArgs&, hipStream_t);                             \
-  template hipError_t attend_merge<T>(const AttendArgs&, const AttendArgs&, hipStream_t);
+  template hipError_t attend_merge<T>(const AttendArgs&, const AttendArgs&, int, hipStream_t);
 STUBS(bf16)
 STUBS(float)
 #undef STUBS
