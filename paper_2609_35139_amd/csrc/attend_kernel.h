@@ -30,6 +30,7 @@ namespace cr {
 constexpr int kPlanTile = 64;     // keys per tile of the split's arithmetic
 constexpr int kListPages = 512;   // pages of a segment's block list
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kMostSum = 16777216.f;   // 2^24: a lane's share of a tile's probabilities
 
 // ------------------------------------------------------------ units and rows
 __device__ __forceinline__ int seq_len(const PagedSeqs& p, int s) {
@@ -167,8 +168,8 @@ template <> __device__ __forceinline__ float tanh_of<bf16>(float x) {
   return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
 }
 
-// Keys of a PV atom, its V fragment from the row-major tile and the split of a
-// fragment into finite values and indicators of +inf and -inf (NaN: both).
+// Keys of a PV atom, its V fragment from the row-major tile, and a fragment's
+// finite values and indicators of the others.
 template <typename T> struct ValueOps;
 template <> struct ValueOps<bf16> {
   typedef bf16x8 frag;
@@ -196,16 +197,21 @@ template <> struct ValueOps<bf16> {
     for (int e = 0; e < 8; ++e) bad |= (b[e] & 0x7f80) == 0x7f80;
     return !bad;
   }
-  __device__ __forceinline__ static void split(const frag& v, frag* f, frag* pos, frag* neg) {
-    const u16x8 bits = __builtin_bit_cast(u16x8, v);
+  __device__ __forceinline__ static frag finite_part(const frag& v) {
+    const u16x8 b = __builtin_bit_cast(u16x8, v);
+    u16x8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint16_t b = bits[e];
-      const bool bad = (b & 0x7f80) == 0x7f80, nan = bad && (b & 0x7f);
-      (*f)[e] = bad ? (bf16)0.f : v[e];
-      (*pos)[e] = (bf16)(nan || (bad && !(b & 0x8000)) ? 1.f : 0.f);
-      (*neg)[e] = (bf16)(nan || (bad && (b & 0x8000)) ? 1.f : 0.f);
-    }
+    for (int e = 0; e < 8; ++e) r[e] = (b[e] & 0x7f80) == 0x7f80 ? 0 : b[e];
+    return __builtin_bit_cast(frag, r);
+  }
+  // 1 where the value is infinite with this sign (0 +, 1 -) or NaN
+  __device__ __forceinline__ static frag odd_part(const frag& v, int sign) {
+    const u16x8 b = __builtin_bit_cast(u16x8, v);
+    u16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      r[e] = (b[e] & 0x7fff) > 0x7f80 || b[e] == (sign ? 0xff80 : 0x7f80) ? 0x3f80 : 0;
+    return __builtin_bit_cast(frag, r);
   }
 };
 template <> struct ValueOps<float> {
@@ -228,15 +234,20 @@ template <> struct ValueOps<float> {
     for (int e = 0; e < 4; ++e) bad |= (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u;
     return !bad;
   }
-  __device__ __forceinline__ static void split(const frag& v, frag* f, frag* pos, frag* neg) {
+  __device__ __forceinline__ static frag finite_part(const frag& v) {
+    frag r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u ? 0.f : v[e];
+    return r;
+  }
+  __device__ __forceinline__ static frag odd_part(const frag& v, int sign) {
+    frag r;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t b = __float_as_uint(v[e]);
-      const bool bad = (b & 0x7f800000u) == 0x7f800000u, nan = bad && (b & 0x7fffffu);
-      (*f)[e] = bad ? 0.f : v[e];
-      (*pos)[e] = nan || (bad && !(b >> 31)) ? 1.f : 0.f;
-      (*neg)[e] = nan || (bad && (b >> 31)) ? 1.f : 0.f;
+      r[e] = (b & 0x7fffffffu) > 0x7f800000u || b == (sign ? 0xff800000u : 0x7f800000u) ? 1.f : 0.f;
     }
+    return r;
   }
 };
 
@@ -270,14 +281,16 @@ struct AttendCfg {
   static_assert(KT <= 128 && KT * KG < kListPages, "bits of a lane's scores, keys of a list");
 };
 
-template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES>
-__global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
+template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES, int OCC = 1>
+__global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a) {
   using C = AttendCfg<T, DM, EXACT, NQ, RG, KG, KT, STAGES>;
   using MM = Mma16<T>;
   using VO = ValueOps<T>;
   using frag = typename MM::frag;
   constexpr int KPL = MM::KPL, KSTEP = MM::KSTEP;
-  constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KT / 16, PF = KT / VO::KEYS;
+  // a wave works on KS keys of a tile at a time
+  constexpr int KS = VO::KEYS;
+  constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
   __shared__ __align__(1024) char lds[C::LDS];
   __shared__ __align__(16) int64_t list[kListPages];
@@ -438,10 +451,57 @@ __global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
         dma16(vbase + src[r], base + C::TILE + (r * RG + rg) * 1024);
     };
 
-    auto compute = [&](int i, int st) {
-      const char* kt = ring + st * 2 * C::TILE;
-      const char* vt = kt + C::TILE;
-      const int k0 = seg + (i * KG + kg) * KT;
+    // K fragment (sub-tile t, step kk) of a tile
+    auto key_frag = [&](const char* kt, int t, int kk) {
+      const int byte = (kk * KSTEP + g * KPL) * (int)sizeof(T);
+      return *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + c16, byte >> 4));
+    };
+    // a score's value in exp2 units, before the mask, where it is not just scaled
+    auto transform = [&](float v, int n, int key) {
+      v = a.cap_log2 > 0.f ? a.cap_log2 * tanh_of<T>(v * a.scale_over_cap) : v * a.scale_log2;
+      return v - slope[n] * fabsf((float)(rw[n].p - key));
+    };
+    // probabilities of row block n against its reference, packed, and their sum
+    auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF]) {
+      float ts = 0.f;
+#pragma unroll
+      for (int f = 0; f < PF; ++f) {
+        float pv[KPL];
+#pragma unroll
+        for (int e = 0; e < KPL; ++e)
+          pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f * (KPL / 4) + e / 4][e % 4], cc, -ref));
+        pf[f] = pack_frag(pv, (frag*)nullptr);
+        ts = frag_sum(pf[f], ts);
+      }
+      return ts;
+    };
+    // The reference of a row is not its running maximum: it stays where it is
+    // while a tile's probabilities sum to at most 2^24 (softmax does not depend
+    // on it, and o and l stay far inside fp32), so most tiles need no maximum.
+    // `raise`: rows that take the exact maximum of this tile, all four lanes of
+    // a row alike; no row's rounding depends on another row.
+    auto new_reference = [&](const f32x4 (&s)[ST], int n, bool raise) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < ST; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
+      mx = row_max(mx) * cc;
+      const float mn = raise ? fmaxf(m[n], mx) : m[n];
+      const float alpha = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
+      l[n] *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) oacc[n][d] *= alpha;
+      m[n] = mn;
+    };
+    auto reference = [&](int n) { return m[n] == -INFINITY ? 0.f : m[n]; };
+    auto any_in_row = [&](bool x) {      // over the four lanes of a row
+      const auto v = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
+      return halves_or((int)(v[0] | v[1])) != 0;
+    };
+
+    // KS keys that every row of the wave sees.
+    auto whole = [&](const char* kt, const char* vt, int k0) {
       // S^T: sub-tile t, row block n: keys k0 + 16 t + 4 g + [0, 4) of row c16
       f32x4 s[NQ][ST];
 #pragma unroll
@@ -451,8 +511,7 @@ __global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int kk = 0; kk < QF; ++kk) {
           if (!EXACT && kk * KSTEP >= D) break;
-          const int byte = (kk * KSTEP + g * KPL) * (int)sizeof(T);
-          const frag kf = *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + c16, byte >> 4));
+          const frag kf = key_frag(kt, t, kk);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
         }
@@ -463,121 +522,124 @@ __global__ __launch_bounds__(64 * RG * KG) void attend_kernel(AttendArgs a) {
 #pragma unroll
           for (int t = 0; t < ST; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float v = a.cap_log2 > 0.f ? a.cap_log2 * tanh_of<T>(s[n][t][e] * a.scale_over_cap)
-                                         : s[n][t][e] * a.scale_log2;
-              const int key = k0 + t * 16 + 4 * g + e;
-              v -= slope[n] * fabsf((float)(rw[n].p - key));
-              s[n][t][e] = v;
-            }
+            for (int e = 0; e < 4; ++e) s[n][t][e] = transform(s[n][t][e], n, k0 + t * 16 + 4 * g + e);
       }
-      // masked tiles: not wholly inside every row's window, or with keys past
-      // the segment, or over a block that is none
-      const bool masked = seg_bad || k0 < wlo || k0 + KT > whi || k0 + KT > seg_end;
-      uint32_t see[NQ] = {};     // visible bits of this lane's scores (bit t * 4 + e)
-      if (masked) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int t = 0; t < ST; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int key = k0 + t * 16 + 4 * g + e;
-              bool ok = key >= rw[n].lo && key < rw[n].hi && key < seg_end;
-              if (seg_bad && ok) ok = list[(key >> shift) - p0] >= 0;
-              if (ok) see[n] |= 1u << (t * 4 + e);
-              else s[n][t][e] = -INFINITY;
-            }
-      }
-      // running maximum: raised only when a score exceeds it by 2^8 (softmax
-      // does not depend on the reference; p and l stay far inside fp32)
       frag pf[NQ][PF];
+      float ts[NQ];
+      bool raise = false;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        float mx = -INFINITY;
+        ts[n] = probs(s[n], reference(n), pf[n]);
+        raise = raise || m[n] == -INFINITY || !(ts[n] <= kMostSum);
+      }
+      if (__any(raise)) {
 #pragma unroll
-        for (int t = 0; t < ST; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][t][e]);
-        mx = row_max(mx) * cc;
-        const bool raise = mx > m[n] + 8.f;     // row by row: no row's rounding depends on another
-        if (__any(raise)) {
-          const float mn = raise ? mx : m[n];
-          const float alpha = raise ? __builtin_amdgcn_exp2f(m[n] - mn) : 1.f;
-          l[n] *= alpha;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) oacc[n][d] *= alpha;
-          m[n] = mn;
-        }
-        const float ref = m[n] == -INFINITY ? 0.f : m[n];
-#pragma unroll
-        for (int f = 0; f < PF; ++f) {
-          float pv[KPL];
-#pragma unroll
-          for (int e = 0; e < KPL; ++e)
-            pv[e] = __builtin_amdgcn_exp2f(
-                __builtin_fmaf(s[n][f * (KPL / 4) + e / 4][e % 4], cc, -ref));
-          pf[n][f] = pack_frag(pv, (frag*)nullptr);
-          l[n] = frag_sum(pf[n][f], l[n]);
+        for (int n = 0; n < NQ; ++n) {
+          const bool up = any_in_row(m[n] == -INFINITY || !(ts[n] <= kMostSum));
+          new_reference(s[n], n, up);
+          ts[n] = probs(s[n], reference(n), pf[n]);
         }
       }
-      // O^T += V^T P^T.  A value that is not finite must not reach a row that
-      // does not see its key (0 * inf): where a tile is masked and has such
-      // values, they are taken out and added as what they do to the rows
-      // that see them.
-      bool odd = false;
-      if (masked) {
-        int bad = 0;
 #pragma unroll
-        for (int f = 0; f < PF; ++f)
+      for (int n = 0; n < NQ; ++n) l[n] += ts[n];
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            if (!EXACT && d * 16 >= D) break;
-            // (read by the whole wave: a transposing read crosses lanes)
-            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-            bad |= !VO::finite(vf);
+      for (int f = 0; f < PF; ++f)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          if (!EXACT && d * 16 >= D) break;
+          const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+        }
+    };
+
+    // Any other KS keys, one row block at a time: keys that a row does not see,
+    // keys past the segment, blocks that are none.
+    auto masked = [&](const char* kt, const char* vt, int k0) {
+      // a value that is not finite must not reach a row that does not see its
+      // key (0 * inf): such values are taken out, and added as what they do to
+      // the rows that see them
+      int bad = 0;
+#pragma unroll
+      for (int f = 0; f < PF; ++f)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          if (!EXACT && d * 16 >= D) break;
+          // (read by the whole wave: a transposing read crosses lanes)
+          const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+          bad |= !VO::finite(vf);
+        }
+      const bool odd = __any(bad);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        f32x4 s[ST];
+        uint32_t see = 0;          // visible bits of this lane's scores (bit t * 4 + e)
+#pragma unroll
+        for (int t = 0; t < ST; ++t) {
+          s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < QF; ++kk) {
+            if (!EXACT && kk * KSTEP >= D) break;
+            s[t] = MM::mma(key_frag(kt, t, kk), qf[n][kk], s[t]);
           }
-        odd = __any(bad);
-      }
-      if (!odd) {
 #pragma unroll
-        for (int f = 0; f < PF; ++f)
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            if (!EXACT && d * 16 >= D) break;
-            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          for (int e = 0; e < 4; ++e) {
+            const int key = k0 + t * 16 + 4 * g + e;
+            if (general) s[t][e] = transform(s[t][e], n, key);
+            bool ok = key >= rw[n].lo && key < rw[n].hi && key < seg_end;
+            if (seg_bad && ok) ok = list[(key >> shift) - p0] >= 0;
+            if (ok) see |= 1u << (t * 4 + e);
+            else s[t][e] = -INFINITY;
           }
-      } else {
-        const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+        }
+        frag pf[PF];
+        float ts = probs(s, reference(n), pf);
+        const bool up = any_in_row(m[n] == -INFINITY || !(ts <= kMostSum));
+        if (__any(up)) {
+          new_reference(s, n, up);
+          ts = probs(s, reference(n), pf);
+        }
+        l[n] += ts;
 #pragma unroll
         for (int f = 0; f < PF; ++f) {
-          frag one[NQ];
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            float b[KPL];
-#pragma unroll
-            for (int e = 0; e < KPL; ++e) b[e] = (see[n] >> (f * KPL + e)) & 1 ? 1.f : 0.f;
-            one[n] = pack_frag(b, (frag*)nullptr);
-          }
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             if (!EXACT && d * 16 >= D) break;
-            frag fin, pos, neg;
-            VO::split(VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane), &fin, &pos, &neg);
+            frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+            if (odd) vf = VO::finite_part(vf);
+            oacc[n][d] = MM::mma(vf, pf[f], oacc[n][d]);
+          }
+        }
+        if (!odd) continue;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-              oacc[n][d] = MM::mma(fin, pf[n][f], oacc[n][d]);
-              const f32x4 cp = MM::mma(pos, one[n], zero), cn = MM::mma(neg, one[n], zero);
+        for (int f = 0; f < PF; ++f) {
+          float b[KPL];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if (cp[e] > 0.f) oacc[n][d][e] += INFINITY;
-                if (cn[e] > 0.f) oacc[n][d][e] -= INFINITY;
-              }
+          for (int e = 0; e < KPL; ++e) b[e] = (see >> (f * KPL + e)) & 1 ? 1.f : 0.f;
+          const frag one = pack_frag(b, (frag*)nullptr);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            if (!EXACT && d * 16 >= D) break;
+            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+#pragma unroll
+            for (int sign = 0; sign < 2; ++sign) {
+              const f32x4 c = MM::mma(VO::odd_part(vf, sign), one, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (c[e] > 0.f) oacc[n][d][e] += sign ? -INFINITY : INFINITY;
             }
           }
         }
+      }
+    };
+
+    auto compute = [&](int i, int st) {
+      const char* kt = ring + st * 2 * C::TILE;
+      const char* vt = kt + C::TILE;
+      int k0 = seg + (i * KG + kg) * KT;
+      for (int h = 0; h < KT / KS; ++h, k0 += KS, kt += KS * RB, vt += KS * RB) {
+        if (!seg_bad && k0 >= wlo && k0 + KS <= whi && k0 + KS <= seg_end) whole(kt, vt, k0);
+        else if (k0 < seg_end) masked(kt, vt, k0);
       }
     };
 
@@ -816,7 +878,8 @@ hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, int most_row
 template <typename T, int DM, bool EXACT>
 hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
   const dim3 grid((unsigned)(items * a.n_kv));
-  constexpr int WIDE = attend_rows(sizeof(T), DM), KEYS = ValueOps<T>::KEYS;
+  constexpr int WIDE = attend_rows(sizeof(T), DM, EXACT), KEYS = ValueOps<T>::KEYS;
+  constexpr int OCC = sizeof(T) == 2 && DM <= 128 ? 2 : 1;   // workgroups to a CU that the registers allow
   // 16 rows (the heads of a group for one new token): bound by reading the
   // keys.  Two waves with a ring of two 16 KB tiles of their own each (32 KB
   // for wide heads), two workgroups to a CU.
@@ -826,7 +889,7 @@ hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
   if (a.rows == 16) {
     CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2>), grid, dim3(256), 0, s, a);
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a);
   } else {
     return hipErrorInvalidValue;
   }
@@ -842,6 +905,8 @@ hipError_t attend(const AttendArgs& a, hipStream_t s) {
     case 64: return attend_as<T, 64, true>(a, items, s);
     case 128: return attend_as<T, 128, true>(a, items, s);
     case 256: return attend_as<T, 256, true>(a, items, s);
+    case 32:
+    case 96: return attend_as<T, 128, false>(a, items, s);
     default: return attend_as<T, 256, false>(a, items, s);
   }
 }

@@ -65,13 +65,10 @@ struct AttendArgs {
   float* part_o;                    // [item][kv head][rows][head_dim]
   float2* part_ml;                  // [item][kv head][rows] (max, sum)
 };
-// Rows of a unit: 128, or 64 where the accumulators of wide fp32 heads fill the
-// registers (head dims without a kernel of their own run in that of 256).
-constexpr bool attend_exact(int head_dim) {
-  return head_dim == 64 || head_dim == 128 || head_dim == 256;
-}
-constexpr int attend_rows(int element_bytes, int head_dim) {
-  return element_bytes == 4 && (head_dim > 128 || !attend_exact(head_dim)) ? 64 : 128;
+// Rows of a wide unit: 128, or 64 where the accumulators of heads over 128 fill
+// the registers (exact: the kernel is compiled for the very head_dim).
+constexpr int attend_rows(int element_bytes, int head_dim, bool exact) {
+  return head_dim > 128 && (element_bytes == 4 || !exact) ? 64 : 128;
 }
 template <typename T>
 hipError_t attend(const AttendArgs& a, hipStream_t s);

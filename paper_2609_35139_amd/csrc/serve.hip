@@ -113,7 +113,7 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
                  int shared) {
   Plan p;
   const int G = n_heads / l->n_kv_heads, D = l->head_dim, H = l->n_kv_heads;
-  const int wide = attend_rows((int)esize(l->dtype), D);
+  const int wide = attend_rows((int)esize(l->dtype), D, D == 256);
   p.rows = b.most * G <= 16 ? 16 : wide;
   p.pre_rows = b.n_tokens * G <= 16 ? 16 : wide;
   auto tiles = [&](int64_t n) { return ceil_div(n * G, p.rows); };
