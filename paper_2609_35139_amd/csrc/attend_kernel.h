@@ -292,9 +292,12 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   constexpr int KS = VO::KEYS;
   constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
-  __shared__ __align__(1024) char lds[C::LDS];
-  __shared__ __align__(16) int64_t list[kListPages];
-  __shared__ int bad_pages;
+  // rings (later the merge area), the block list, the list's flag: one array,
+  // since the compiler waits for every transfer in flight before it reads LDS
+  // where it tells several apart
+  __shared__ __align__(1024) char lds[C::LDS + kListPages * 8 + 16];
+  int64_t* const list = reinterpret_cast<int64_t*>(lds + C::LDS);
+  int* const bad_pages = reinterpret_cast<int*>(list + kListPages);
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -418,16 +421,16 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     const int seg = (int)seg64, seg_end = (int)min(seg64 + seg_most, (int64_t)ke);
     const int p0 = seg >> shift, np = ((seg_end - 1) >> shift) - p0 + 1;
     __syncthreads();                       // the last segment's list and ring are idle
-    if (tid == 0) bad_pages = 0;
+    if (tid == 0) *bad_pages = 0;
     __syncthreads();
     for (int i = tid; i < np; i += C::NT) {
       const int id = table[p0 + i];
       const bool ok = id >= 0 && id < a.seqs.n_blocks;
       list[i] = ok ? (int64_t)id * a.seqs.block : -1;
-      if (!ok) bad_pages = 1;
+      if (!ok) *bad_pages = 1;
     }
     __syncthreads();
-    const bool seg_bad = __builtin_amdgcn_readfirstlane(bad_pages) != 0;
+    const bool seg_bad = __builtin_amdgcn_readfirstlane(*bad_pages) != 0;
     const int tiles = (seg_end - seg + KT - 1) / KT;
     const int iters = (tiles + KG - 1) / KG, mine = (tiles - kg + KG - 1) / KG;
 
@@ -478,16 +481,17 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     // The reference of a row is not its running maximum: it stays where it is
     // while a tile's probabilities sum to at most 2^24 (softmax does not depend
     // on it, and o and l stay far inside fp32), so most tiles need no maximum.
-    // `raise`: rows that take the exact maximum of this tile, all four lanes of
-    // a row alike; no row's rounding depends on another row.
-    auto new_reference = [&](const f32x4 (&s)[ST], int n, bool raise) {
+    // Rows that need it take the exact maximum of this tile, all four lanes of a
+    // row alike; no row's rounding depends on another row.
+    auto new_reference = [&](const f32x4 (&s)[ST], int n) {
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < ST; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
       mx = row_max(mx) * cc;
-      const float mn = raise ? fmaxf(m[n], mx) : m[n];
+      const float mn = fmaxf(m[n], mx);
+      // (nothing to scale before the first key; -inf - -inf is avoided)
       const float alpha = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
       l[n] *= alpha;
 #pragma unroll
@@ -498,6 +502,15 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     auto any_in_row = [&](bool x) {      // over the four lanes of a row
       const auto v = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
       return halves_or((int)(v[0] | v[1])) != 0;
+    };
+
+    auto weigh = [&](const f32x4 (&s)[ST], int n, frag (&pf)[PF]) {
+      float ts = probs(s, reference(n), pf);
+      if (any_in_row(m[n] == -INFINITY || !(ts <= kMostSum))) {
+        new_reference(s, n);
+        ts = probs(s, reference(n), pf);
+      }
+      return ts;
     };
 
     // KS keys that every row of the wave sees.
@@ -525,23 +538,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
             for (int e = 0; e < 4; ++e) s[n][t][e] = transform(s[n][t][e], n, k0 + t * 16 + 4 * g + e);
       }
       frag pf[NQ][PF];
-      float ts[NQ];
-      bool raise = false;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        ts[n] = probs(s[n], reference(n), pf[n]);
-        raise = raise || m[n] == -INFINITY || !(ts[n] <= kMostSum);
-      }
-      if (__any(raise)) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          const bool up = any_in_row(m[n] == -INFINITY || !(ts[n] <= kMostSum));
-          new_reference(s[n], n, up);
-          ts[n] = probs(s[n], reference(n), pf[n]);
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) l[n] += ts[n];
+      for (int n = 0; n < NQ; ++n) l[n] += weigh(s[n], n, pf[n]);
 #pragma unroll
       for (int f = 0; f < PF; ++f)
 #pragma unroll
@@ -593,13 +591,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
           }
         }
         frag pf[PF];
-        float ts = probs(s, reference(n), pf);
-        const bool up = any_in_row(m[n] == -INFINITY || !(ts <= kMostSum));
-        if (__any(up)) {
-          new_reference(s, n, up);
-          ts = probs(s, reference(n), pf);
-        }
-        l[n] += ts;
+        l[n] += weigh(s, n, pf);
 #pragma unroll
         for (int f = 0; f < PF; ++f) {
 #pragma unroll
