@@ -485,7 +485,8 @@ CR_API cr_status cr_repair_static(void* kv, const cr_kv_layout* layout,
  *                 share blocks, but a block that a call appends to belongs to
  *                 one sequence (which of two tokens stays in one row is
  *                 undefined).  max_blocks * block_size < 2^31 - 256.
- *  block_size, n_blocks, stride_block: as cr_kv_pages.
+ *  block_size, n_blocks, stride_block: as cr_kv_pages; rows of a block (the
+ *                 layout's stride_token) less than 4 GiB apart.
  * The kernels never leave the cache: a length counts as at least 0 and at most
  * max_blocks * block_size, and a block id outside [0, n_blocks) is no block
  * (its keys are not seen, tokens appended to it are dropped).

@@ -23,6 +23,9 @@
 // of one dim per lane: for bf16 the LDS reads that transpose 16-bit elements
 // deliver that from the row-major tile.
 #pragma once
+#include <climits>
+#include <type_traits>
+
 #include "serve.h"
 
 namespace cr {
@@ -276,7 +279,8 @@ struct AttendCfg {
   static constexpr int MERGE = KG > 1 ? KG * ROWS * (MLD + 2) * 4 : 0;
   static constexpr int LDS = KG * RING > MERGE ? KG * RING : MERGE;
   static_assert(ROUNDS * RG * 1024 == TILE && RPW >= 1 && KT % ValueOps<T>::KEYS == 0, "tile");
-  static_assert(LDS + kListPages * 8 + 64 <= 160 * 1024, "LDS");
+  static constexpr int BYTES = LDS + kListPages * 8 + kListPages / 8 + ROWS * 16;
+  static_assert(BYTES <= 160 * 1024 && ROWS <= NT, "LDS");
   static_assert(2 * ROUNDS * (STAGES - 1) < 64, "transfers in flight");
   static_assert(KT <= 128 && KT * KG < kListPages, "bits of a lane's scores, keys of a list");
 };
@@ -292,12 +296,14 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   constexpr int KS = VO::KEYS;
   constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
-  // rings (later the merge area), the block list, the list's flag: one array,
-  // since the compiler waits for every transfer in flight before it reads LDS
-  // where it tells several apart
-  __shared__ __align__(1024) char lds[C::LDS + kListPages * 8 + 16];
-  int64_t* const list = reinterpret_cast<int64_t*>(lds + C::LDS);
-  int* const bad_pages = reinterpret_cast<int*>(list + kListPages);
+  // rings (later the merge area), the segment's block list (addresses of the
+  // blocks' keys), the bits of those that are no block, and of every row (lo,
+  // hi, p, slope): one array, since the compiler waits for every transfer in
+  // flight before it reads LDS where it tells several apart
+  __shared__ __align__(1024) char lds[C::BYTES];
+  uint64_t* const list = reinterpret_cast<uint64_t*>(lds + C::LDS);
+  uint32_t* const none = reinterpret_cast<uint32_t*>(list + kListPages);
+  int4* const info = reinterpret_cast<int4*>(none + kListPages / 32);
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -321,34 +327,32 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   if (!a.shared) x = unit_of(a, unit);
   const int row0 = x.tile * C::ROWS, n_rows = min(C::ROWS, x.nq * a.group - row0);
   const int seq_n = a.shared ? 0 : seq_len(a.seqs, x.s);
-  // query, position and interval of row r of the unit
-  struct Row { int t, g, p, lo, hi; };
-  auto row_of = [&](int r) {
-    Row w;
-    const int i = (row0 + r) / a.group;
-    w.g = row0 + r - i * a.group;
-    w.t = x.tok0 + i;
-    int n = seq_n, nq = x.nq, qi = i;
-    if (a.shared) {
-      const int s = a.q_off ? find_offset(a.q_off, a.seqs.n_seqs, i) : i / a.q_per_seq;
-      const int o = a.q_off ? a.q_off[s] : s * a.q_per_seq;
-      nq = a.q_off ? a.q_off[s + 1] - o : a.q_per_seq;
-      n = seq_len(a.seqs, s);
-      qi = i - o;
+  // position and interval of every row of the unit, and the keys that any row
+  // sees (a row past the last one sees everything: it masks nothing)
+  if (tid < C::ROWS) {
+    int4 w{INT_MIN, INT_MAX, 0, 0};
+    if (tid < n_rows) {
+      const int i = (row0 + tid) / a.group;
+      int n = seq_n, nq = x.nq, qi = i;
+      if (a.shared) {
+        const int s = a.q_off ? find_offset(a.q_off, a.seqs.n_seqs, i) : i / a.q_per_seq;
+        const int o = a.q_off ? a.q_off[s] : s * a.q_per_seq;
+        nq = a.q_off ? a.q_off[s + 1] - o : a.q_per_seq;
+        n = seq_len(a.seqs, s);
+        qi = i - o;
+      }
+      const int2 iv = interval_of(a, n, nq, qi, x.tok0 + i);
+      const float slope = a.bias ? a.slopes_log2[head * a.group + row0 + tid - i * a.group] : 0.f;
+      w = int4{iv.x, iv.y, n - nq + qi, __float_as_int(slope)};
     }
-    w.p = n - nq + qi;
-    const int2 iv = interval_of(a, n, nq, qi, w.t);
-    w.lo = iv.x;
-    w.hi = iv.y;
-    return w;
-  };
-  // the keys that any row sees
+    info[tid] = w;
+  }
+  __syncthreads();
   int kb = INT_MAX, ke = INT_MIN;
-  for (int r = lane; r < C::ROWS; r += 64)
-    if (r < n_rows) {
-      const Row w = row_of(r);
-      if (w.lo < w.hi) { kb = min(kb, w.lo); ke = max(ke, w.hi); }
-    }
+  for (int r = lane; r < n_rows; r += 64) {
+    const int lo = info[r].x, hi = info[r].y;
+    if (lo < hi) { kb = min(kb, lo); ke = max(ke, hi); }
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     kb = min(kb, __shfl_xor(kb, o));
@@ -364,28 +368,20 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   ke = __builtin_amdgcn_readfirstlane(ke);
 
   // ---- this lane's rows
-  Row rw[NQ];
-  bool rvalid[NQ];
   frag qf[NQ][QF];
-  float slope[NQ];
   int wlo = INT_MIN, whi = INT_MAX;      // window that every row of the wave sees
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int r = (rg * NQ + n) * 16 + c16;
-    rvalid[n] = r < n_rows;
-    rw[n] = Row{0, 0, 0, INT_MIN, INT_MAX};
-    if (rvalid[n]) {
-      rw[n] = row_of(r);
-      wlo = max(wlo, rw[n].lo);
-      whi = min(whi, rw[n].hi);
-    }
-    const T* qp = static_cast<const T*>(a.q) + (int64_t)rw[n].t * a.q_token +
-                  (int64_t)(head * a.group + rw[n].g) * a.q_head;
+    wlo = max(wlo, info[r].x);
+    whi = min(whi, info[r].y);
+    const int i = (row0 + min(r, n_rows - 1)) / a.group;
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(x.tok0 + i) * a.q_token +
+                  (int64_t)(head * a.group + row0 + min(r, n_rows - 1) - i * a.group) * a.q_head;
 #pragma unroll
     for (int kk = 0; kk < QF; ++kk)
-      qf[n][kk] = rvalid[n] && (EXACT || kk * KSTEP < D)
+      qf[n][kk] = r < n_rows && (EXACT || kk * KSTEP < D)
                       ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
-    slope[n] = a.bias ? a.slopes_log2[head * a.group + rw[n].g] : 0.f;
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
@@ -409,7 +405,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   const float cc = general ? 1.f : a.scale_log2;
 
   const char* kbase = static_cast<const char*>(a.k) + (int64_t)head * a.seqs.head * sizeof(T);
-  const char* vbase = static_cast<const char*>(a.v) + (int64_t)head * a.seqs.head * sizeof(T);
+  const uint64_t to_values = (uint64_t)a.v - (uint64_t)a.k;
+  const uint32_t token_bytes = (uint32_t)(a.seqs.token * (int64_t)sizeof(T));   // (32 bits: checked on the host)
   char* ring = lds + kg * C::RING;
   const int shift = a.seqs.shift, page_mask = (1 << shift) - 1;
   const int* table = a.seqs.table + (int64_t)x.s * a.seqs.max_blocks;
@@ -421,37 +418,37 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     const int seg = (int)seg64, seg_end = (int)min(seg64 + seg_most, (int64_t)ke);
     const int p0 = seg >> shift, np = ((seg_end - 1) >> shift) - p0 + 1;
     __syncthreads();                       // the last segment's list and ring are idle
-    if (tid == 0) *bad_pages = 0;
+    if (tid < kListPages / 32) none[tid] = 0;
     __syncthreads();
+    int bad = 0;
     for (int i = tid; i < np; i += C::NT) {
       const int id = table[p0 + i];
       const bool ok = id >= 0 && id < a.seqs.n_blocks;
-      list[i] = ok ? (int64_t)id * a.seqs.block : -1;
-      if (!ok) *bad_pages = 1;
+      list[i] = (uint64_t)kbase + (ok ? (int64_t)id * a.seqs.block * (int64_t)sizeof(T) : 0);
+      if (!ok) { atomicOr(none + i / 32, 1u << (i % 32)); bad = 1; }
     }
-    __syncthreads();
-    const bool seg_bad = __builtin_amdgcn_readfirstlane(*bad_pages) != 0;
+    const bool seg_bad = __syncthreads_or(bad) != 0;
     const int tiles = (seg_end - seg + KT - 1) / KT;
     const int iters = (tiles + KG - 1) / KG, mine = (tiles - kg + KG - 1) / KG;
 
     auto issue = [&](int i, int st) {      // tile i of this group into ring slot st
       const int k0 = seg + (i * KG + kg) * KT;
-      int64_t src[C::ROUNDS];
+      uint64_t src[C::ROUNDS];
 #pragma unroll
       for (int r = 0; r < C::ROUNDS; ++r) {
         const int row = (r * RG + rg) * C::RPW + lane / C::CPR;
         int ch = (lane % C::CPR) ^ row_swizzle<RB>(row);
         if (!EXACT && ch * 16 >= D * (int)sizeof(T)) ch = 0;
         const int key = min(k0 + row, seg_end - 1);      // never past the last key seen
-        const int64_t off = max(list[(key >> shift) - p0], (int64_t)0);
-        src[r] = (off + (int64_t)(key & page_mask) * a.seqs.token) * (int)sizeof(T) + ch * 16;
+        src[r] = list[(key >> shift) - p0] + (uint64_t)(uint32_t)(key & page_mask) * token_bytes + ch * 16;
       }
       char* base = ring + st * 2 * C::TILE;
 #pragma unroll
-      for (int r = 0; r < C::ROUNDS; ++r) dma16(kbase + src[r], base + (r * RG + rg) * 1024);
+      for (int r = 0; r < C::ROUNDS; ++r)
+        dma16(reinterpret_cast<const char*>(src[r]), base + (r * RG + rg) * 1024);
 #pragma unroll
       for (int r = 0; r < C::ROUNDS; ++r)
-        dma16(vbase + src[r], base + C::TILE + (r * RG + rg) * 1024);
+        dma16(reinterpret_cast<const char*>(src[r] + to_values), base + C::TILE + (r * RG + rg) * 1024);
     };
 
     // K fragment (sub-tile t, step kk) of a tile
@@ -459,10 +456,24 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       const int byte = (kk * KSTEP + g * KPL) * (int)sizeof(T);
       return *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + c16, byte >> 4));
     };
-    // a score's value in exp2 units, before the mask, where it is not just scaled
-    auto transform = [&](float v, int n, int key) {
-      v = a.cap_log2 > 0.f ? a.cap_log2 * tanh_of<T>(v * a.scale_over_cap) : v * a.scale_log2;
-      return v - slope[n] * fabsf((float)(rw[n].p - key));
+    // scores of row block n in exp2 units, before the mask, where they are not
+    // just scaled
+    auto transform = [&](f32x4 (&s)[ST], int n, int k0) {
+      if (a.cap_log2 > 0.f) {
+#pragma unroll
+        for (int t = 0; t < ST; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][e] = a.cap_log2 * tanh_of<T>(s[t][e] * a.scale_over_cap);
+      } else {
+#pragma unroll
+        for (int t = 0; t < ST; ++t) s[t] *= a.scale_log2;
+      }
+      const int4 w = info[(rg * NQ + n) * 16 + c16];
+#pragma unroll
+      for (int t = 0; t < ST; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[t][e] -= __int_as_float(w.w) * fabsf((float)(w.z - (k0 + t * 16 + 4 * g + e)));
     };
     // probabilities of row block n against its reference, packed, and their sum
     auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF]) {
@@ -483,14 +494,14 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     // on it, and o and l stay far inside fp32), so most tiles need no maximum.
     // Rows that need it take the exact maximum of this tile, all four lanes of a
     // row alike; no row's rounding depends on another row.
-    auto new_reference = [&](const f32x4 (&s)[ST], int n) {
+    auto new_reference = [&](const f32x4 (&s)[ST], int n, bool raise) {
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < ST; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
       mx = row_max(mx) * cc;
-      const float mn = fmaxf(m[n], mx);
+      const float mn = raise ? fmaxf(m[n], mx) : m[n];
       // (nothing to scale before the first key; -inf - -inf is avoided)
       const float alpha = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
       l[n] *= alpha;
@@ -506,15 +517,16 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 
     auto weigh = [&](const f32x4 (&s)[ST], int n, frag (&pf)[PF]) {
       float ts = probs(s, reference(n), pf);
-      if (any_in_row(m[n] == -INFINITY || !(ts <= kMostSum))) {
-        new_reference(s, n);
+      const bool over = m[n] == -INFINITY || !(ts <= kMostSum);
+      if (__any(over)) {
+        new_reference(s, n, any_in_row(over));
         ts = probs(s, reference(n), pf);
       }
       return ts;
     };
 
     // KS keys that every row of the wave sees.
-    auto whole = [&](const char* kt, const char* vt, int k0) {
+    auto whole = [&](auto other, const char* kt, const char* vt, int k0) {
       // S^T: sub-tile t, row block n: keys k0 + 16 t + 4 g + [0, 4) of row c16
       f32x4 s[NQ][ST];
 #pragma unroll
@@ -529,13 +541,9 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
           for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
         }
       }
-      if (general) {
+      if constexpr (decltype(other)::value) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int t = 0; t < ST; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][t][e] = transform(s[n][t][e], n, k0 + t * 16 + 4 * g + e);
+        for (int n = 0; n < NQ; ++n) transform(s[n], n, k0);
       }
       frag pf[NQ][PF];
 #pragma unroll
@@ -571,7 +579,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         f32x4 s[ST];
-        uint32_t see = 0;          // visible bits of this lane's scores (bit t * 4 + e)
 #pragma unroll
         for (int t = 0; t < ST; ++t) {
           s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -580,16 +587,23 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
             if (!EXACT && kk * KSTEP >= D) break;
             s[t] = MM::mma(key_frag(kt, t, kk), qf[n][kk], s[t]);
           }
+        }
+        if (general) transform(s, n, k0);
+        const int4 w = info[(rg * NQ + n) * 16 + c16];
+        uint32_t see = 0;          // visible bits of this lane's scores (bit t * 4 + e)
+#pragma unroll
+        for (int t = 0; t < ST; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = k0 + t * 16 + 4 * g + e;
-            if (general) s[t][e] = transform(s[t][e], n, key);
-            bool ok = key >= rw[n].lo && key < rw[n].hi && key < seg_end;
-            if (seg_bad && ok) ok = list[(key >> shift) - p0] >= 0;
+            bool ok = key >= w.x && key < min(w.y, seg_end);
+            if (seg_bad && ok) {
+              const int pg = (key >> shift) - p0;
+              ok = !((none[pg / 32] >> (pg % 32)) & 1);
+            }
             if (ok) see |= 1u << (t * 4 + e);
             else s[t][e] = -INFINITY;
           }
-        }
         frag pf[PF];
         l[n] += weigh(s, n, pf);
 #pragma unroll
@@ -625,21 +639,18 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       }
     };
 
-    auto compute = [&](int i, int st) {
-      const char* kt = ring + st * 2 * C::TILE;
-      const char* vt = kt + C::TILE;
-      int k0 = seg + (i * KG + kg) * KT;
-      for (int h = 0; h < KT / KS; ++h, k0 += KS, kt += KS * RB, vt += KS * RB) {
-        if (!seg_bad && k0 >= wlo && k0 + KS <= whi && k0 + KS <= seg_end) whole(kt, vt, k0);
-        else if (k0 < seg_end) masked(kt, vt, k0);
-      }
+    // ---- the segment's tiles: those before the window that every row of the
+    // wave sees, those inside it, those after it.  Loops of their own, so that
+    // the accumulators keep their registers through the one that counts; the
+    // waves of a group may be in different ones, but each passes one barrier
+    // per tile.
+    auto first_key = [&](int i) { return seg + (i * KG + kg) * KT; };
+    auto inside = [&](int i) {
+      const int k0 = first_key(i);
+      return !seg_bad && k0 >= wlo && k0 + KT <= min(whi, seg_end);
     };
-
-#pragma unroll
-    for (int st = 0; st < STAGES - 1; ++st)
-      if (mine > 0) issue(min(st, mine - 1), st);
-    int st = 0;
-    for (int i = 0; i < iters; ++i) {
+    int i = 0, st = 0;
+    auto turn = [&](auto&& work) {
       // every iteration issues one tile (past the last one, a copy of it into a
       // slot nobody reads again), so tile i has landed once STAGES - 2 later
       // ones remain in flight
@@ -649,11 +660,37 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
         asm volatile("" ::: "memory");
       }
       if (i < mine) {
-        const int fill = st == 0 ? STAGES - 1 : st - 1;
-        issue(min(i + STAGES - 1, mine - 1), fill);
-        if (!idle) compute(i, st);
+        issue(min(i + STAGES - 1, mine - 1), st == 0 ? STAGES - 1 : st - 1);
+        const char* kt = ring + st * 2 * C::TILE;
+        if (!idle) work(kt, kt + C::TILE, first_key(i));
       }
       st = st + 1 == STAGES ? 0 : st + 1;
+      ++i;
+    };
+    auto parts_of = [&](auto&& work) {       // a tile, KS keys at a time
+      return [&, work](const char* kt, const char* vt, int k0) {
+#pragma unroll
+        for (int h = 0; h < KT / KS; ++h)
+          work(kt + h * KS * RB, vt + h * KS * RB, k0 + h * KS);
+      };
+    };
+#pragma unroll
+    for (int p = 0; p < STAGES - 1; ++p)
+      if (mine > 0) issue(min(p, mine - 1), p);
+    for (int pass = 0; pass < 2; ++pass) {
+      while (i < iters && (pass == 1 || !inside(i)))
+        turn([&](const char* kt, const char* vt, int k0) {
+          for (int h = 0; h < KT / KS && k0 < seg_end; ++h, k0 += KS)
+            masked(kt + h * KS * RB, vt + h * KS * RB, k0);
+        });
+      if (general)
+        while (i < iters && inside(i))
+          turn(parts_of([&](const char* kt, const char* vt, int k0) {
+            whole(std::true_type{}, kt, vt, k0); }));
+      else
+        while (i < iters && inside(i))
+          turn(parts_of([&](const char* kt, const char* vt, int k0) {
+            whole(std::false_type{}, kt, vt, k0); }));
     }
     wait_vmcnt<0>();
   }
@@ -665,13 +702,17 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   const bool partial = a.always_partial || parts > 1;
   const int64_t prow = ((int64_t)slot * a.n_kv + head) * C::ROWS;
   if constexpr (KG == 1) {
+    // (what depends on the lane is formed anew, not kept in registers till here)
+    int le = threadIdx.x & 63;
+    asm volatile("" : "+v"(le));
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      if (!rvalid[n]) continue;
-      const int r = (rg * NQ + n) * 16 + c16;
+      const int g = le >> 4, r = (rg * NQ + n) * 16 + (le & 15);
+      if (r >= n_rows) continue;
       const float inv = lt[n] == 0.f ? 0.f : 1.f / lt[n];
-      T* op = static_cast<T*>(a.o) + (int64_t)rw[n].t * a.o_token +
-              (int64_t)(head * a.group + rw[n].g) * a.o_head;
+      const int i = (row0 + r) / a.group, hd = head * a.group + row0 + r - i * a.group;
+      const int64_t t = x.tok0 + i;
+      T* op = static_cast<T*>(a.o) + t * a.o_token + (int64_t)hd * a.o_head;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         if (!EXACT && d * 16 >= D) break;
@@ -690,7 +731,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       if (g == 0) {
         if (partial) a.part_ml[prow + r] = make_float2(m[n], lt[n]);
         else if (a.lse)
-          a.lse[(int64_t)rw[n].t * a.n_kv * a.group + head * a.group + rw[n].g] =
+          a.lse[t * a.n_kv * a.group + hd] =
               lt[n] == 0.f ? -INFINITY : (m[n] + __log2f(lt[n])) / kLog2e;
       }
     }

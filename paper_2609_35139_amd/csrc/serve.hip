@@ -75,6 +75,15 @@ cr_status check_rows(const cr_rows* r, int64_t n, int64_t heads, int64_t head_di
   return written ? check_injective(dims) : CR_OK;
 }
 
+// The block geometry; the kernels take the bytes between a block's rows in 32 bits.
+cr_status check_blocks(const cr_kv_layout* l, const cr_sequences* q) {
+  const cr_status st = check_page_strides(l, q->block_size, q->n_blocks, q->stride_block);
+  if (st != CR_OK) return st;
+  if (q->block_size > 1 && l->stride_token >= ((int64_t)1 << 32) / (int64_t)esize(l->dtype))
+    return CR_ERR_LAYOUT;
+  return CR_OK;
+}
+
 PagedSeqs paged(const cr_kv_layout* l, const cr_sequences* q) {
   PagedSeqs p{};
   p.token = l->stride_token;
@@ -265,7 +274,7 @@ cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t layer,
   if (layer < 0 || layer >= layout->n_layers) return CR_ERR_DIMS;
   if (q && (n_heads < 1 || n_heads > (1 << 16))) return CR_ERR_DIMS;
   if (layout->n_kv_heads > (1 << 16)) return CR_ERR_DIMS;
-  st = check_page_strides(layout, seqs->block_size, seqs->n_blocks, seqs->stride_block);
+  st = check_blocks(layout, seqs);
   if (st != CR_OK) return st;
   if (!aligned(kv, 16)) return CR_ERR_LAYOUT;
   KeyRope kr{};
@@ -340,7 +349,7 @@ cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t layer,
     return CR_ERR_DIMS;
   for (int h = 0; o.slopes && h < n_heads; ++h)
     if (!std::isfinite(o.slopes[h])) return CR_ERR_DIMS;
-  st = check_page_strides(layout, seqs->block_size, seqs->n_blocks, seqs->stride_block);
+  st = check_blocks(layout, seqs);
   if (st != CR_OK) return st;
   if (!aligned(kv, 16)) return CR_ERR_LAYOUT;
   const int64_t D = layout->head_dim;
