@@ -279,7 +279,7 @@ struct AttendCfg {
   static constexpr int MERGE = KG > 1 ? KG * ROWS * (MLD + 2) * 4 : 0;
   static constexpr int LDS = KG * RING > MERGE ? KG * RING : MERGE;
   static_assert(ROUNDS * RG * 1024 == TILE && RPW >= 1 && KT % ValueOps<T>::KEYS == 0, "tile");
-  static constexpr int BYTES = LDS + kListPages * 8 + kListPages / 8 + ROWS * 16;
+  static constexpr int BYTES = LDS + kListPages * 8 + kListPages / 8 + 16 + ROWS * 16;
   static_assert(BYTES <= 160 * 1024 && ROWS <= NT, "LDS");
   static_assert(2 * ROUNDS * (STAGES - 1) < 64, "transfers in flight");
   static_assert(KT <= 128 && KT * KG < kListPages, "bits of a lane's scores, keys of a list");
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   __shared__ __align__(1024) char lds[C::BYTES];
   uint64_t* const list = reinterpret_cast<uint64_t*>(lds + C::LDS);
   uint32_t* const none = reinterpret_cast<uint32_t*>(list + kListPages);
-  int4* const info = reinterpret_cast<int4*>(none + kListPages / 32);
+  int4* const info = reinterpret_cast<int4*>(none + kListPages / 32 + 4);
 
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -390,6 +390,12 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   }
   wlo = __builtin_amdgcn_readfirstlane(wlo);
   whi = __builtin_amdgcn_readfirstlane(whi);
+  // (waited for here: a load still pending at the loops' entry would have every
+  // turn of them wait for all transfers in flight)
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int kk = 0; kk < QF; ++kk) asm volatile("" : "+v"(qf[n][kk]));
   const bool idle = rg * NQ * 16 >= n_rows;     // no row: the wave only stages
 
   f32x4 oacc[NQ][DT];
@@ -418,16 +424,19 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     const int seg = (int)seg64, seg_end = (int)min(seg64 + seg_most, (int64_t)ke);
     const int p0 = seg >> shift, np = ((seg_end - 1) >> shift) - p0 + 1;
     __syncthreads();                       // the last segment's list and ring are idle
-    if (tid < kListPages / 32) none[tid] = 0;
+    if (tid <= kListPages / 32) none[tid] = 0;    // (the last word: any)
     __syncthreads();
-    int bad = 0;
     for (int i = tid; i < np; i += C::NT) {
       const int id = table[p0 + i];
       const bool ok = id >= 0 && id < a.seqs.n_blocks;
       list[i] = (uint64_t)kbase + (ok ? (int64_t)id * a.seqs.block * (int64_t)sizeof(T) : 0);
-      if (!ok) { atomicOr(none + i / 32, 1u << (i % 32)); bad = 1; }
+      if (!ok) {
+        atomicOr(none + i / 32, 1u << (i % 32));
+        none[kListPages / 32] = 1;
+      }
     }
-    const bool seg_bad = __syncthreads_or(bad) != 0;
+    __syncthreads();
+    const bool seg_bad = __builtin_amdgcn_readfirstlane(none[kListPages / 32]) != 0;
     const int tiles = (seg_end - seg + KT - 1) / KT;
     const int iters = (tiles + KG - 1) / KG, mine = (tiles - kg + KG - 1) / KG;
 
