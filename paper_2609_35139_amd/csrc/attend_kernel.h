@@ -144,7 +144,7 @@ __device__ __forceinline__ Item plan_item(const AttendArgs& a, int it, int unit)
 }
 
 // ------------------------------------------------------------- type specifics
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -193,28 +193,36 @@ template <> struct ValueOps<bf16> {
     *(reinterpret_cast<s16x4*>(&r) + 1) = hi;
     return r;
   }
-  __device__ __forceinline__ static bool finite(const frag& v) {
-    const u16x8 b = __builtin_bit_cast(u16x8, v);   // (of the whole: an element's cast reads element 0)
-    int bad = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bad |= (b[e] & 0x7f80) == 0x7f80;
-    return !bad;
+  // (two elements to a word; without compares, whose masks would fill the
+  // scalar registers)
+  // 1 in each half that is infinite or NaN
+  __device__ __forceinline__ static uint32_t not_finite(uint32_t w) {
+    return (((w & 0x7fff7fffu) + 0x00800080u) >> 15) & 0x00010001u;
+  }
+  __device__ __forceinline__ static uint32_t odd_bits(const frag& v) {
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    return (not_finite(w[0]) | not_finite(w[1])) | (not_finite(w[2]) | not_finite(w[3]));
   }
   __device__ __forceinline__ static frag finite_part(const frag& v) {
-    const u16x8 b = __builtin_bit_cast(u16x8, v);
-    u16x8 r;
+    u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (b[e] & 0x7f80) == 0x7f80 ? 0 : b[e];
-    return __builtin_bit_cast(frag, r);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = not_finite(w[i]);
+      w[i] &= ~((m << 16) - m);       // 0xffff in each such half
+    }
+    return __builtin_bit_cast(frag, w);
   }
-  // 1 where the value is infinite with this sign (0 +, 1 -) or NaN
+  // 1.0 where the value is infinite with this sign (0 +, 1 -) or NaN
   __device__ __forceinline__ static frag odd_part(const frag& v, int sign) {
-    const u16x8 b = __builtin_bit_cast(u16x8, v);
-    u16x8 r;
+    u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      r[e] = (b[e] & 0x7fff) > 0x7f80 || b[e] == (sign ? 0xff80 : 0x7f80) ? 0x3f80 : 0;
-    return __builtin_bit_cast(frag, r);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t nan = (((w[i] & 0x7fff7fffu) + 0x007f007fu) >> 15) & 0x00010001u;
+      const uint32_t neg = (w[i] >> 15) & 0x00010001u;
+      const uint32_t m = nan | (not_finite(w[i]) & (sign ? neg : ~neg));
+      w[i] = (m << 14) - (m << 7);    // 0x3f80 in each such half
+    }
+    return __builtin_bit_cast(frag, w);
   }
 };
 template <> struct ValueOps<float> {
@@ -231,26 +239,27 @@ template <> struct ValueOps<float> {
     }
     return r;
   }
-  __device__ __forceinline__ static bool finite(const frag& v) {
-    int bad = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) bad |= (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u;
-    return !bad;
+  __device__ __forceinline__ static uint32_t not_finite(uint32_t w) {
+    return ((w & 0x7fffffffu) + 0x00800000u) >> 31;
+  }
+  __device__ __forceinline__ static uint32_t odd_bits(const frag& v) {
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    return (not_finite(w[0]) | not_finite(w[1])) | (not_finite(w[2]) | not_finite(w[3]));
   }
   __device__ __forceinline__ static frag finite_part(const frag& v) {
-    frag r;
+    u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u ? 0.f : v[e];
-    return r;
+    for (int i = 0; i < 4; ++i) w[i] &= not_finite(w[i]) - 1u;
+    return __builtin_bit_cast(frag, w);
   }
   __device__ __forceinline__ static frag odd_part(const frag& v, int sign) {
-    frag r;
+    u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t b = __float_as_uint(v[e]);
-      r[e] = (b & 0x7fffffffu) > 0x7f800000u || b == (sign ? 0xff800000u : 0x7f800000u) ? 1.f : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t nan = ((w[i] & 0x7fffffffu) + 0x007fffffu) >> 31, neg = w[i] >> 31;
+      w[i] = (nan | (not_finite(w[i]) & (sign ? neg : neg ^ 1u))) * 0x3f800000u;
     }
-    return r;
+    return __builtin_bit_cast(frag, w);
   }
 };
 
@@ -534,7 +543,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       return ts;
     };
 
-    // KS keys that every row of the wave sees.
+    // KS keys that every row of the wave sees
     auto whole = [&](auto other, const char* kt, const char* vt, int k0) {
       // S^T: sub-tile t, row block n: keys k0 + 16 t + 4 g + [0, 4) of row c16
       f32x4 s[NQ][ST];
@@ -555,8 +564,23 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
         for (int n = 0; n < NQ; ++n) transform(s[n], n, k0);
       }
       frag pf[NQ][PF];
+      float ts[NQ];
+      bool over[NQ], any = false;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) l[n] += weigh(s[n], n, pf[n]);
+      for (int n = 0; n < NQ; ++n) {
+        ts[n] = probs(s[n], reference(n), pf[n]);
+        over[n] = m[n] == -INFINITY || !(ts[n] <= kMostSum);
+        any = any || over[n];
+      }
+      if (__any(any)) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          new_reference(s[n], n, any_in_row(over[n]));
+          ts[n] = probs(s[n], reference(n), pf[n]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) l[n] += ts[n];
 #pragma unroll
       for (int f = 0; f < PF; ++f)
 #pragma unroll
@@ -574,7 +598,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       // a value that is not finite must not reach a row that does not see its
       // key (0 * inf): such values are taken out, and added as what they do to
       // the rows that see them
-      int bad = 0;
+      uint32_t bad = 0;
 #pragma unroll
       for (int f = 0; f < PF; ++f)
 #pragma unroll
@@ -582,9 +606,9 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
           if (!EXACT && d * 16 >= D) break;
           // (read by the whole wave: a transposing read crosses lanes)
           const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-          bad |= !VO::finite(vf);
+          bad |= VO::odd_bits(vf);
         }
-      const bool odd = __any(bad);
+      const bool odd = __any(bad != 0);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         f32x4 s[ST];
@@ -660,9 +684,9 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     };
     int i = 0, st = 0;
     auto turn = [&](auto&& work) {
-      // every iteration issues one tile (past the last one, a copy of it into a
-      // slot nobody reads again), so tile i has landed once STAGES - 2 later
-      // ones remain in flight
+      // every turn issues one tile (past the last one, a copy of it into a slot
+      // nobody reads again), so tile i has landed once STAGES - 2 later ones
+      // remain in flight
       wait_vmcnt<(STAGES - 2) * 2 * C::ROUNDS>();
       if (RG > 1) {   // ... in every wave's part, and the slot refilled below is idle
         __builtin_amdgcn_s_barrier();
@@ -671,35 +695,27 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       if (i < mine) {
         issue(min(i + STAGES - 1, mine - 1), st == 0 ? STAGES - 1 : st - 1);
         const char* kt = ring + st * 2 * C::TILE;
-        if (!idle) work(kt, kt + C::TILE, first_key(i));
+        if (!idle) {
+#pragma unroll
+          for (int h = 0; h < KT / KS; ++h)
+            work(kt + h * KS * RB, kt + C::TILE + h * KS * RB, first_key(i) + h * KS);
+        }
       }
       st = st + 1 == STAGES ? 0 : st + 1;
       ++i;
-    };
-    auto parts_of = [&](auto&& work) {       // a tile, KS keys at a time
-      return [&, work](const char* kt, const char* vt, int k0) {
-#pragma unroll
-        for (int h = 0; h < KT / KS; ++h)
-          work(kt + h * KS * RB, vt + h * KS * RB, k0 + h * KS);
-      };
     };
 #pragma unroll
     for (int p = 0; p < STAGES - 1; ++p)
       if (mine > 0) issue(min(p, mine - 1), p);
     for (int pass = 0; pass < 2; ++pass) {
       while (i < iters && (pass == 1 || !inside(i)))
-        turn([&](const char* kt, const char* vt, int k0) {
-          for (int h = 0; h < KT / KS && k0 < seg_end; ++h, k0 += KS)
-            masked(kt + h * KS * RB, vt + h * KS * RB, k0);
-        });
+        turn([&](const char* kt, const char* vt, int k0) { if (k0 < seg_end) masked(kt, vt, k0); });
       if (general)
         while (i < iters && inside(i))
-          turn(parts_of([&](const char* kt, const char* vt, int k0) {
-            whole(std::true_type{}, kt, vt, k0); }));
+          turn([&](const char* kt, const char* vt, int k0) { whole(std::true_type{}, kt, vt, k0); });
       else
         while (i < iters && inside(i))
-          turn(parts_of([&](const char* kt, const char* vt, int k0) {
-            whole(std::false_type{}, kt, vt, k0); }));
+          turn([&](const char* kt, const char* vt, int k0) { whole(std::false_type{}, kt, vt, k0); });
     }
     wait_vmcnt<0>();
   }
@@ -927,11 +943,10 @@ hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
   // for wide heads), two workgroups to a CU.
   constexpr int NARROW = 64 * 128 / (DM * (int)sizeof(T));
   constexpr int KN = NARROW < KEYS ? KEYS : NARROW;
-  constexpr int KW = sizeof(T) == 2 ? (DM > 128 ? 32 : 64) : (DM > 128 ? 16 : 32);
   if (a.rows == 16) {
     CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a);
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KEYS, 2, OCC>), grid, dim3(256), 0, s, a);
   } else {
     return hipErrorInvalidValue;
   }
