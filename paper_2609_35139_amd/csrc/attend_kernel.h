@@ -89,17 +89,16 @@ __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, 
 
 // ------------------------------------------------------------------- split
 // Item `it` of the split: unit, part, number of the unit's parts, tiles per
-// part, and the unit's first item.  Every unit has at least one part; a part is
+// part, and the unit's first item (all uniform).  Every unit has at least one part; a part is
 // `chunk` tiles, the mean load of a.slots workgroups, so there are at most
-// a.slots + n_units items.  The same in every wave of every workgroup (the
-// merge asks with a unit instead of an item).
+// a.slots + n_units items.  The same in every wave of every workgroup.
 struct Item { int unit, part, parts, chunk, first; };
 __device__ __forceinline__ int wave_sum_i(int v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-__device__ __forceinline__ Item plan_item(const AttendArgs& a, int it, int unit) {
+__device__ __forceinline__ Item plan_item(const AttendArgs& a, int it) {
   const int lane = threadIdx.x & 63;
   const int U = a.n_units;
   const int t0 = lane < U ? unit_tiles(a, lane) : 0;   // the first 64 units stay in registers
@@ -111,7 +110,17 @@ __device__ __forceinline__ Item plan_item(const AttendArgs& a, int it, int unit)
     int v = tiles(u0) >> 3;                             // sums of 64 stay below 2^31
     total += 8.f * (float)wave_sum_i(v) + (float)wave_sum_i(tiles(u0) & 7);
   }
-  const int chunk = max(a.min_tiles, (int)fminf(total / (float)a.slots + 1.f, 1e9f));
+  int chunk = max(a.min_tiles, (int)fminf(total / (float)a.slots + 1.f, 1e9f));
+  // a few units: longer parts, until they are at most a.slots
+  for (int k = 0; k < 8 && U <= a.one_round; ++k) {
+    float cnt = 0.f;
+    for (int u0 = 0; u0 < U; u0 += 64) {
+      const int t = tiles(u0);
+      cnt += (float)wave_sum_i(u0 + lane < U ? max(1, (int)(((int64_t)t + chunk - 1) / chunk)) : 0);
+    }
+    if (cnt <= (float)a.slots) break;
+    chunk += max(1, (int)((float)chunk * (cnt / (float)a.slots - 1.f) * 0.7f));
+  }
   Item r{-1, 0, 1, chunk, 0};
   int base = 0;
   for (int u0 = 0; u0 < U; u0 += 64) {
@@ -123,8 +132,7 @@ __device__ __forceinline__ Item plan_item(const AttendArgs& a, int it, int unit)
       const int x = __shfl_up(incl, o);
       if (lane >= o) incl += x;
     }
-    const bool mine = unit >= 0 ? u0 + lane == unit : (n > 0 && base + incl > it);
-    const unsigned long long hit = __ballot(mine);
+    const unsigned long long hit = __ballot(n > 0 && base + incl > it);
     if (hit) {
       const int l = __ffsll(hit) - 1;
       r.unit = u0 + l;
@@ -273,6 +281,14 @@ __device__ __forceinline__ float row_sum(float x) {
   return halves_sum(__uint_as_float(v[0]) + __uint_as_float(v[1]));
 }
 
+// This lane's number, from no register that has to live.  (opaque: not merged
+// with an earlier one)
+__device__ __forceinline__ int lane_again() {
+  int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(l));
+  return l;
+}
+
 // ------------------------------------------------------------------ kernel
 // RG * KG waves: KG groups of RG waves walk alternate tiles of KT keys, each
 // with its own ring of STAGES tiles; the RG waves of a group own 16 * NQ rows
@@ -305,6 +321,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   constexpr int KS = VO::KEYS;
   constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
+  constexpr int VE = EXACT && NQ > 1 && sizeof(T) == 2 && DM <= 128 ? 3 : 0;
   // rings (later the merge area), the segment's block list (addresses of the
   // blocks' keys), the bits of those that are no block, and of every row (lo,
   // hi, p, slope): one array, since the compiler waits for every transfer in
@@ -328,12 +345,17 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     part = item - unit * a.splits;
     chunk = a.split_tiles;
   } else if (a.slots) {
-    const Item p = plan_item(a, item, -1);
+    const Item p = plan_item(a, item);
     if (p.unit < 0) return;
     unit = p.unit; part = p.part; parts = p.parts; chunk = p.chunk;
+    if (part == 0 && head == 0 && tid == 0) a.unit_items[unit] = make_int2(p.first, p.parts);
   }
   Unit x{0, unit, 0, a.n_tokens};
   if (!a.shared) x = unit_of(a, unit);
+  x.s = __builtin_amdgcn_readfirstlane(x.s);
+  x.tile = __builtin_amdgcn_readfirstlane(x.tile);
+  x.tok0 = __builtin_amdgcn_readfirstlane(x.tok0);
+  x.nq = __builtin_amdgcn_readfirstlane(x.nq);
   const int row0 = x.tile * C::ROWS, n_rows = min(C::ROWS, x.nq * a.group - row0);
   const int seq_n = a.shared ? 0 : seq_len(a.seqs, x.s);
   // position and interval of every row of the unit, and the keys that any row
@@ -426,19 +448,23 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   const int shift = a.seqs.shift, page_mask = (1 << shift) - 1;
   const int* table = a.seqs.table + (int64_t)x.s * a.seqs.max_blocks;
   constexpr int STEP = KT * KG;
-  const int64_t seg_most = ((int64_t)(kListPages - 1) << shift) / STEP * STEP;
+  const int pages = kListPages - 1;       // (a segment may begin inside a page)
+  const int seg_most = (pages << shift) / STEP * STEP;
 
-  for (int64_t seg64 = kb; seg64 < ke; seg64 += seg_most) {
+  for (int seg = kb, seg_end; seg < ke; seg = seg_end) {
     // ---- a segment: its block list, then its tiles through the ring
-    const int seg = (int)seg64, seg_end = (int)min(seg64 + seg_most, (int64_t)ke);
+    seg_end = ke - seg <= seg_most ? ke : seg + seg_most;
     const int p0 = seg >> shift, np = ((seg_end - 1) >> shift) - p0 + 1;
+    const int tid = wave * 64 + lane_again();   // (not kept in a register through the loops)
     __syncthreads();                       // the last segment's list and ring are idle
     if (tid <= kListPages / 32) none[tid] = 0;    // (the last word: any)
     __syncthreads();
+    uint64_t k0 = (uint64_t)kbase;
+    asm volatile("" : "+s"(k0));
     for (int i = tid; i < np; i += C::NT) {
       const int id = table[p0 + i];
       const bool ok = id >= 0 && id < a.seqs.n_blocks;
-      list[i] = (uint64_t)kbase + (ok ? (int64_t)id * a.seqs.block * (int64_t)sizeof(T) : 0);
+      list[i] = k0 + (ok ? (int64_t)id * a.seqs.block * (int64_t)sizeof(T) : 0);
       if (!ok) {
         atomicOr(none + i / 32, 1u << (i % 32));
         none[kListPages / 32] = 1;
@@ -449,7 +475,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     const int tiles = (seg_end - seg + KT - 1) / KT;
     const int iters = (tiles + KG - 1) / KG, mine = (tiles - kg + KG - 1) / KG;
 
-    auto issue = [&](int i, int st) {      // tile i of this group into ring slot st
+    auto issue = [&](int i, int st, int lane) {   // tile i of this group into ring slot st
       const int k0 = seg + (i * KG + kg) * KT;
       uint64_t src[C::ROUNDS];
 #pragma unroll
@@ -470,13 +496,13 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     };
 
     // K fragment (sub-tile t, step kk) of a tile
-    auto key_frag = [&](const char* kt, int t, int kk) {
-      const int byte = (kk * KSTEP + g * KPL) * (int)sizeof(T);
-      return *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + c16, byte >> 4));
+    auto key_frag = [&](const char* kt, int t, int kk, int lane) {
+      const int byte = (kk * KSTEP + (lane >> 4) * KPL) * (int)sizeof(T);
+      return *reinterpret_cast<const frag*>(kt + row_offset<RB>(t * 16 + (lane & 15), byte >> 4));
     };
     // scores of row block n in exp2 units, before the mask, where they are not
     // just scaled
-    auto transform = [&](f32x4 (&s)[ST], int n, int k0) {
+    auto transform = [&](f32x4 (&s)[ST], int n, int k0, int lane) {
       if (a.cap_log2 > 0.f) {
 #pragma unroll
         for (int t = 0; t < ST; ++t)
@@ -486,12 +512,13 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int t = 0; t < ST; ++t) s[t] *= a.scale_log2;
       }
-      const int4 w = info[(rg * NQ + n) * 16 + c16];
+      const int4 w = info[(rg * NQ + n) * 16 + (lane & 15)];
+      const int k1 = w.z - k0 - 4 * (lane >> 4);
 #pragma unroll
       for (int t = 0; t < ST; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          s[t][e] -= __int_as_float(w.w) * fabsf((float)(w.z - (k0 + t * 16 + 4 * g + e)));
+          s[t][e] -= __int_as_float(w.w) * fabsf((float)(k1 - (t * 16 + e)));
     };
     // probabilities of row block n against its reference, packed, and their sum
     auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF]) {
@@ -554,15 +581,24 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int kk = 0; kk < QF; ++kk) {
           if (!EXACT && kk * KSTEP >= D) break;
-          const frag kf = key_frag(kt, t, kk);
+          const frag kf = key_frag(kt, t, kk, lane);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
         }
       }
       if constexpr (decltype(other)::value) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) transform(s[n], n, k0);
+        for (int n = 0; n < NQ; ++n) transform(s[n], n, k0, lane);
       }
+      // the first V fragments on their way before the scores are weighed (as many
+      // as the registers hold without spilling; 8,192 queries over 12,288 keys
+      // 1,220 us without, 1,150 with three or four)
+      frag ve[PF][VE ? VE : 1];
+#pragma unroll
+      for (int f = 0; f < PF; ++f)
+#pragma unroll
+        for (int d = 0; d < VE; ++d) ve[f][d] = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+      if (VE) __builtin_amdgcn_sched_barrier(0);
       frag pf[NQ][PF];
       float ts[NQ];
       bool over[NQ], any = false;
@@ -586,7 +622,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           if (!EXACT && d * 16 >= D) break;
-          const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+          const frag vf = d < VE ? ve[f][d < VE ? d : 0]
+                                 : VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
         }
@@ -595,6 +632,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     // Any other KS keys, one row block at a time: keys that a row does not see,
     // keys past the segment, blocks that are none.
     auto masked = [&](const char* kt, const char* vt, int k0) {
+      // (addresses formed anew in every call: kept from call to call they would
+      // fill the registers that the loop over whole tiles needs)
+      const int lane = lane_again();
+      const int c16 = lane & 15, g = lane >> 4;
       // a value that is not finite must not reach a row that does not see its
       // key (0 * inf): such values are taken out, and added as what they do to
       // the rows that see them
@@ -618,10 +659,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
           for (int kk = 0; kk < QF; ++kk) {
             if (!EXACT && kk * KSTEP >= D) break;
-            s[t] = MM::mma(key_frag(kt, t, kk), qf[n][kk], s[t]);
+            s[t] = MM::mma(key_frag(kt, t, kk, lane), qf[n][kk], s[t]);
           }
         }
-        if (general) transform(s, n, k0);
+        if (general) transform(s, n, k0, lane);
         const int4 w = info[(rg * NQ + n) * 16 + c16];
         uint32_t see = 0;          // visible bits of this lane's scores (bit t * 4 + e)
 #pragma unroll
@@ -693,29 +734,34 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
         asm volatile("" ::: "memory");
       }
       if (i < mine) {
-        issue(min(i + STAGES - 1, mine - 1), st == 0 ? STAGES - 1 : st - 1);
+        issue(min(i + STAGES - 1, mine - 1), st == 0 ? STAGES - 1 : st - 1, lane);
         const char* kt = ring + st * 2 * C::TILE;
-        if (!idle) {
-#pragma unroll
-          for (int h = 0; h < KT / KS; ++h)
-            work(kt + h * KS * RB, kt + C::TILE + h * KS * RB, first_key(i) + h * KS);
-        }
+        if (!idle) work(kt, first_key(i));
       }
       st = st + 1 == STAGES ? 0 : st + 1;
       ++i;
     };
 #pragma unroll
     for (int p = 0; p < STAGES - 1; ++p)
-      if (mine > 0) issue(min(p, mine - 1), p);
+      if (mine > 0) issue(min(p, mine - 1), p, lane_again());
+    auto whole_tile = [&](auto other) {
+      return [&, other](const char* kt, int k0) {
+#pragma unroll
+        for (int h = 0; h < KT / KS; ++h)
+          whole(other, kt + h * KS * RB, kt + C::TILE + h * KS * RB, k0 + h * KS);
+      };
+    };
     for (int pass = 0; pass < 2; ++pass) {
       while (i < iters && (pass == 1 || !inside(i)))
-        turn([&](const char* kt, const char* vt, int k0) { if (k0 < seg_end) masked(kt, vt, k0); });
+        turn([&](const char* kt, int k0) {
+#pragma unroll 1
+          for (int h = 0; h < KT / KS && k0 < seg_end; ++h, k0 += KS, kt += KS * RB)
+            masked(kt, kt + C::TILE, k0);
+        });
       if (general)
-        while (i < iters && inside(i))
-          turn([&](const char* kt, const char* vt, int k0) { whole(std::true_type{}, kt, vt, k0); });
+        while (i < iters && inside(i)) turn(whole_tile(std::true_type{}));
       else
-        while (i < iters && inside(i))
-          turn([&](const char* kt, const char* vt, int k0) { whole(std::false_type{}, kt, vt, k0); });
+        while (i < iters && inside(i)) turn(whole_tile(std::false_type{}));
     }
     wait_vmcnt<0>();
   }
@@ -727,15 +773,17 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
   const bool partial = a.always_partial || parts > 1;
   const int64_t prow = ((int64_t)slot * a.n_kv + head) * C::ROWS;
   if constexpr (KG == 1) {
-    // (what depends on the lane is formed anew, not kept in registers till here)
-    int le = threadIdx.x & 63;
-    asm volatile("" : "+v"(le));
+    // (what depends on the lane or the group is formed anew, not kept in
+    // registers till here)
+    const int le = lane_again();
+    int group = a.group;
+    asm volatile("" : "+s"(group));
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       const int g = le >> 4, r = (rg * NQ + n) * 16 + (le & 15);
       if (r >= n_rows) continue;
       const float inv = lt[n] == 0.f ? 0.f : 1.f / lt[n];
-      const int i = (row0 + r) / a.group, hd = head * a.group + row0 + r - i * a.group;
+      const int i = (row0 + r) / group, hd = head * group + row0 + r - i * group;
       const int64_t t = x.tok0 + i;
       T* op = static_cast<T*>(a.o) + t * a.o_token + (int64_t)hd * a.o_head;
 #pragma unroll
@@ -833,19 +881,19 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
   const Unit x = unit_of(a, unit);
   const int row0 = x.tile * a.rows, n_rows = min(a.rows, x.nq * a.group - row0);
   if (rb * RPW >= n_rows) return;
-  const Item it = plan_item(a, -1, unit);
-  if (it.parts == 1 && !a.always_partial) return;         // written already
+  const int2 it = a.unit_items[unit];                     // first item, parts
+  if (it.y == 1 && !a.always_partial) return;             // written already
   const int rl = threadIdx.x / TPR, tr = threadIdx.x % TPR;
   const int r = rb * RPW + rl;
   const bool valid = r < n_rows;
   const int rr = valid ? r : n_rows - 1;                  // (a row of its own for every thread)
   const int i = (row0 + rr) / a.group, g = row0 + rr - i * a.group;
   const int t = x.tok0 + i, h = head * a.group + g;
-  const int n_pre = pre.shared ? pre.splits : 0, P = n_pre + it.parts;
+  const int n_pre = pre.shared ? pre.splits : 0, P = n_pre + it.y;
   // part j: row index into the partial results of its pass
   const int prow = t * a.group + g, ptile = pre.shared ? prow / pre.rows : 0;
   const int64_t pre_at = ((int64_t)ptile * n_pre * a.n_kv + head) * pre.rows + prow - ptile * pre.rows;
-  const int64_t own_at = ((int64_t)it.first * a.n_kv + head) * a.rows + rr;
+  const int64_t own_at = ((int64_t)it.x * a.n_kv + head) * a.rows + rr;
   const int64_t pre_step = (int64_t)a.n_kv * pre.rows, own_step = (int64_t)a.n_kv * a.rows;
   auto ml_of = [&](int j) {
     return j < n_pre ? pre.part_ml[pre_at + j * pre_step] : a.part_ml[own_at + (j - n_pre) * own_step];
@@ -943,10 +991,11 @@ hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
   // for wide heads), two workgroups to a CU.
   constexpr int NARROW = 64 * 128 / (DM * (int)sizeof(T));
   constexpr int KN = NARROW < KEYS ? KEYS : NARROW;
+  constexpr int KW = sizeof(T) == 2 && DM <= 128 ? 2 * KEYS : KEYS;
   if (a.rows == 16) {
     CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KEYS, 2, OCC>), grid, dim3(256), 0, s, a);
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a);
   } else {
     return hipErrorInvalidValue;
   }

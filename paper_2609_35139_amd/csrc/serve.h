@@ -58,10 +58,12 @@ struct AttendArgs {
   // [0, shared) of sequence 0's pages for the rows of all sequences
   int key_begin, shared;
   // splits of the keys: planned on the device from the lengths (slots > 0:
-  // about that many items per KV head, at least min_tiles 64-key tiles each),
+  // about that many items per KV head, at least min_tiles 64-key tiles each; no
+  // more than slots items where there are at most one_round units),
   // or fixed (shared: `splits` of split_tiles tiles), or none
-  int slots, min_tiles, splits, split_tiles;
+  int slots, min_tiles, one_round, splits, split_tiles;
   int always_partial;               // write partial results for the merge
+  int2* unit_items;                 // [unit] first item and parts, for the merge
   float* part_o;                    // [item][kv head][rows][head_dim]
   float2* part_ml;                  // [item][kv head][rows] (max, sum)
 };

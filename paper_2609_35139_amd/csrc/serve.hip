@@ -115,7 +115,7 @@ struct Plan {
   int64_t own_items = 0;         // partial results of that pass, per KV head
   int64_t pre_units = 0;         // units of the pass over the shared keys, its split
   int splits = 0, split_tiles = 0;
-  uint64_t tables = 0, own_ml = 0, own_o = 0, pre_ml = 0, pre_o = 0, total = 0;
+  uint64_t tables = 0, items = 0, own_ml = 0, own_o = 0, pre_ml = 0, pre_o = 0, total = 0;
 };
 
 Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, int n_heads,
@@ -148,6 +148,7 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     p.splits = (int)ceil_div(key_tiles, p.split_tiles);
   }
   p.own_items = p.slots ? p.units + p.slots : 0;
+  if (p.slots) p.items = a.take((uint64_t)p.units * 8);
   const uint64_t own = (uint64_t)p.own_items * H * p.rows;
   const uint64_t pre = (uint64_t)p.pre_units * p.splits * H * p.pre_rows;
   p.own_ml = a.take(own * 8);
@@ -229,6 +230,8 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
   }
   a.slots = p.slots;
   a.min_tiles = p.min_tiles;
+  a.one_round = p.slots * 3 / 4;
+  a.unit_items = reinterpret_cast<int2*>(ws + p.items);
   a.part_ml = reinterpret_cast<float2*>(ws + p.own_ml);
   a.part_o = reinterpret_cast<float*>(ws + p.own_o);
   AttendArgs pre{};
