@@ -93,10 +93,8 @@ __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, 
 // `chunk` tiles, the mean load of a.slots workgroups, so there are at most
 // a.slots + n_units items.  The same in every wave of every workgroup.
 struct Item { int unit, part, parts, chunk, first; };
-__device__ __forceinline__ int wave_sum_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+__device__ __forceinline__ int div_up(int t, int chunk) {
+  return (int)(((unsigned)t + (unsigned)chunk - 1u) / (unsigned)chunk);
 }
 __device__ __forceinline__ Item plan_item(const AttendArgs& a, int it) {
   const int lane = threadIdx.x & 63;
@@ -105,49 +103,42 @@ __device__ __forceinline__ Item plan_item(const AttendArgs& a, int it) {
   auto tiles = [&](int u0) {
     return u0 == 0 ? t0 : (u0 + lane < U ? unit_tiles(a, u0 + lane) : 0);
   };
-  float total = 0.f;   // (a chunk need not be exact, only the same everywhere)
-  for (int u0 = 0; u0 < U; u0 += 64) {
-    int v = tiles(u0) >> 3;                             // sums of 64 stay below 2^31
-    total += 8.f * (float)wave_sum_i(v) + (float)wave_sum_i(tiles(u0) & 7);
-  }
+  // (sums in fp32: a chunk need not be exact, only the same everywhere)
+  float total = 0.f;
+  for (int u0 = 0; u0 < U; u0 += 64) total += wave_sum((float)tiles(u0));
   int chunk = max(a.min_tiles, (int)fminf(total / (float)a.slots + 1.f, 1e9f));
   // a few units: longer parts, until they are at most a.slots
-  for (int k = 0; k < 8 && U <= a.one_round; ++k) {
+  for (int k = 0; k < 8 && U > 1 && U <= a.one_round; ++k) {
     float cnt = 0.f;
-    for (int u0 = 0; u0 < U; u0 += 64) {
-      const int t = tiles(u0);
-      cnt += (float)wave_sum_i(u0 + lane < U ? max(1, (int)(((int64_t)t + chunk - 1) / chunk)) : 0);
-    }
+    for (int u0 = 0; u0 < U; u0 += 64)
+      cnt += wave_sum(u0 + lane < U ? (float)max(1, div_up(tiles(u0), chunk)) : 0.f);
     if (cnt <= (float)a.slots) break;
     chunk += max(1, (int)((float)chunk * (cnt / (float)a.slots - 1.f) * 0.7f));
   }
+  chunk = __builtin_amdgcn_readfirstlane(chunk);
   Item r{-1, 0, 1, chunk, 0};
   int base = 0;
   for (int u0 = 0; u0 < U; u0 += 64) {
-    const int t = tiles(u0);
-    const int n = u0 + lane < U ? max(1, (int)(((int64_t)t + chunk - 1) / chunk)) : 0;
+    const int n = u0 + lane < U ? max(1, div_up(tiles(u0), chunk)) : 0;
     int incl = n;
+    if (U > 1) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(incl, o);
-      if (lane >= o) incl += x;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(incl, o);
+        if (lane >= o) incl += x;
+      }
     }
     const unsigned long long hit = __ballot(n > 0 && base + incl > it);
     if (hit) {
       const int l = __ffsll(hit) - 1;
       r.unit = u0 + l;
-      r.parts = __shfl(n, l);
-      r.first = base + __shfl(incl, l) - r.parts;
+      r.parts = __builtin_amdgcn_readlane(n, l);
+      r.first = base + __builtin_amdgcn_readlane(incl, l) - r.parts;
       r.part = it - r.first;
       break;
     }
-    base += __shfl(incl, 63);
+    base += __builtin_amdgcn_readlane(incl, 63);
   }
-  r.unit = __builtin_amdgcn_readfirstlane(r.unit);
-  r.part = __builtin_amdgcn_readfirstlane(r.part);
-  r.parts = __builtin_amdgcn_readfirstlane(r.parts);
-  r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
-  r.first = __builtin_amdgcn_readfirstlane(r.first);
   return r;
 }
 
@@ -902,10 +893,23 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
     return j < n_pre ? pre.part_o + (pre_at + j * pre_step) * D
                      : a.part_o + (own_at + (j - n_pre) * own_step) * D;
   };
+  const int streams = TPR / tpd, sj = tr / tpd, d0 = (tr - sj * tpd) * 4;
+  const bool active = sj < streams;
+  // what the first parts left is on its way while their weights are found
+  constexpr int EARLY = 8;
+  const float2 none = make_float2(-INFINITY, 0.f);
+  const float2 v0 = tr < P ? ml_of(tr) : none;
+  f32x4 early[EARLY];
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k) {
+    const int j = sj + k * streams;
+    early[k] = active && j < min(P, CHUNK) ? *reinterpret_cast<const f32x4*>(o_of(j) + d0)
+                                           : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   // maximum over the row's parts (a part that saw nothing has sum 0; a NaN sum
   // counts, its maximum may be -inf)
-  float m = -INFINITY;
-  for (int j = tr; j < P; j += TPR) {
+  float m = v0.y != 0.f ? v0.x : -INFINITY;
+  for (int j = tr + TPR; j < P; j += TPR) {
     const float2 v = ml_of(j);
     if (v.y != 0.f) m = fmaxf(m, v.x);
   }
@@ -916,18 +920,15 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
     if ((threadIdx.x & 63) == 0) lsum[threadIdx.x / 64] = m;
     __syncthreads();
     m = fmaxf(fmaxf(lsum[0], lsum[1]), fmaxf(lsum[2], lsum[3]));
-    __syncthreads();
   }
   const float ref = m == -INFINITY ? 0.f : m;
-  const int streams = TPR / tpd, sj = tr / tpd, d0 = (tr - sj * tpd) * 4;
-  const bool active = sj < streams;
   float l = 0.f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
   for (int j0 = 0; j0 < P; j0 += CHUNK) {
     const int n = min(CHUNK, P - j0);
     __syncthreads();
     for (int j = tr; j < n; j += TPR) {
-      const float2 v = ml_of(j0 + j);
+      const float2 v = j0 + j == tr ? v0 : ml_of(j0 + j);
       const float w = v.y == 0.f ? 0.f
                                  : __builtin_amdgcn_exp2f((v.x == -INFINITY ? 0.f : v.x) - ref);
       wts[rl][j] = w;
@@ -935,8 +936,15 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
     }
     __syncthreads();
     if (active) {
+      int j = sj;
+      if (j0 == 0) {
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k)
+          if (sj + k * streams < n) o += wts[rl][sj + k * streams] * early[k];
+        j = sj + EARLY * streams;
+      }
 #pragma unroll 8
-      for (int j = sj; j < n; j += streams)
+      for (; j < n; j += streams)
         o += wts[rl][j] * *reinterpret_cast<const f32x4*>(o_of(j0 + j) + d0);
     }
   }

@@ -135,10 +135,13 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   if (b.off) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
   // split the keys unless the units fill the chip by themselves
   if (p.units * H < (p.rows == 16 ? 8192 : 512)) {
-    p.slots = (int)std::max<int64_t>(1, (p.rows == 16 ? 1024 : 512) / H);
-    p.min_tiles = 4;
+    // one round of two workgroups to a CU, or two where the units by themselves
+    // nearly fill one (their ragged lengths then even out)
+    p.slots = (int)std::max<int64_t>(1, 512 / H);
+    if (p.rows == 16 && p.units * 4 > p.slots * 3) p.slots = (int)std::max<int64_t>(1, 1024 / H);
+    p.min_tiles = p.rows == 16 ? 2 : 4;
     // one part holds all keys there can be
-    if ((int64_t)q->max_blocks * q->block_size <= p.min_tiles * 64) p.slots = 0;
+    if ((int64_t)q->max_blocks * q->block_size <= 256) p.slots = 0;
   }
   if (p.slots && shared > 0) {
     p.pre_units = ceil_div(b.n_tokens * G, p.pre_rows);
