@@ -40,26 +40,41 @@ __device__ __forceinline__ int seq_len(const PagedSeqs& p, int s) {
   const int n = p.lens[s];
   return min(max(n, 0), p.max_len);
 }
-// largest i with off[i] <= x, i < n
-__device__ __forceinline__ int find_offset(const int* off, int n, int x) {
-  int a = 0, b = n;
-  while (b - a > 1) {
-    const int mid = (a + b) >> 1;
-    if (off[mid] <= x) a = mid; else b = mid;
+// The offsets of a ragged batch.
+struct Offsets {
+  const AttendArgs& a;
+  const SeqTable& t;
+  __device__ __forceinline__ int q(int i) const { return a.q_off ? a.q_off[i] : t.q[i]; }
+  __device__ __forceinline__ int unit(int i) const { return a.unit_off ? a.unit_off[i] : t.unit[i]; }
+  // the sequence (the last one that begins at or before it) of a query or unit
+  template <typename F>
+  __device__ __forceinline__ int find(F&& off, int x) const {
+    int lo = 0, hi = a.seqs.n_seqs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (off(mid) <= x) lo = mid; else hi = mid;
+    }
+    return lo;
   }
-  return a;
-}
+  __device__ __forceinline__ int of_query(int t) const {
+    return find([&](int i) { return q(i); }, t);
+  }
+  __device__ __forceinline__ int of_unit(int u) const {
+    return find([&](int i) { return unit(i); }, u);
+  }
+};
 struct Unit {
   int s, tile;       // sequence and its row tile
   int tok0, nq;      // the sequence's first query and number of queries
 };
-__device__ __forceinline__ Unit unit_of(const AttendArgs& a, int u) {
+__device__ __forceinline__ Unit unit_of(const AttendArgs& a, const SeqTable& tab, int u) {
   Unit x;
-  if (a.unit_off) {
-    x.s = find_offset(a.unit_off, a.seqs.n_seqs, u);
-    x.tile = u - a.unit_off[x.s];
-    x.tok0 = a.q_off[x.s];
-    x.nq = a.q_off[x.s + 1] - x.tok0;
+  if (a.ragged) {
+    const Offsets off{a, tab};
+    x.s = off.of_unit(u);
+    x.tile = u - off.unit(x.s);
+    x.tok0 = off.q(x.s);
+    x.nq = off.q(x.s + 1) - x.tok0;
   } else {
     x.s = u / a.units_per_seq;
     x.tile = u - x.s * a.units_per_seq;
@@ -75,8 +90,8 @@ __device__ __forceinline__ int unit_end(const AttendArgs& a, const Unit& x) {
   const int last = min(((x.tile + 1) * a.rows - 1) / a.group, x.nq - 1);
   return n - (x.nq - 1 - last);
 }
-__device__ __forceinline__ int unit_tiles(const AttendArgs& a, int u) {
-  return (max(unit_end(a, unit_of(a, u)) - a.key_begin, 0) + kPlanTile - 1) / kPlanTile;
+__device__ __forceinline__ int unit_tiles(const AttendArgs& a, const SeqTable& tab, int u) {
+  return (max(unit_end(a, unit_of(a, tab, u)) - a.key_begin, 0) + kPlanTile - 1) / kPlanTile;
 }
 // Positions [lo, hi) that query i of a sequence (token t) sees in this pass.
 __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, int i, int t) {
@@ -96,12 +111,12 @@ struct Item { int unit, part, parts, chunk, first; };
 __device__ __forceinline__ int div_up(int t, int chunk) {
   return (int)(((unsigned)t + (unsigned)chunk - 1u) / (unsigned)chunk);
 }
-__device__ __forceinline__ Item plan_item(const AttendArgs& a, int it) {
+__device__ __forceinline__ Item plan_item(const AttendArgs& a, const SeqTable& tab, int it) {
   const int lane = threadIdx.x & 63;
   const int U = a.n_units;
-  const int t0 = lane < U ? unit_tiles(a, lane) : 0;   // the first 64 units stay in registers
+  const int t0 = lane < U ? unit_tiles(a, tab, lane) : 0;   // the first 64 units stay in registers
   auto tiles = [&](int u0) {
-    return u0 == 0 ? t0 : (u0 + lane < U ? unit_tiles(a, u0 + lane) : 0);
+    return u0 == 0 ? t0 : (u0 + lane < U ? unit_tiles(a, tab, u0 + lane) : 0);
   };
   // (sums in fp32: a chunk need not be exact, only the same everywhere)
   float total = 0.f;
@@ -302,7 +317,7 @@ struct AttendCfg {
 };
 
 template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES, int OCC = 1>
-__global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a, SeqTable tab) {
   using C = AttendCfg<T, DM, EXACT, NQ, RG, KG, KT, STAGES>;
   using MM = Mma16<T>;
   using VO = ValueOps<T>;
@@ -336,13 +351,13 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
     part = item - unit * a.splits;
     chunk = a.split_tiles;
   } else if (a.slots) {
-    const Item p = plan_item(a, item);
+    const Item p = plan_item(a, tab, item);
     if (p.unit < 0) return;
     unit = p.unit; part = p.part; parts = p.parts; chunk = p.chunk;
     if (part == 0 && head == 0 && tid == 0) a.unit_items[unit] = make_int2(p.first, p.parts);
   }
   Unit x{0, unit, 0, a.n_tokens};
-  if (!a.shared) x = unit_of(a, unit);
+  if (!a.shared) x = unit_of(a, tab, unit);
   x.s = __builtin_amdgcn_readfirstlane(x.s);
   x.tile = __builtin_amdgcn_readfirstlane(x.tile);
   x.tok0 = __builtin_amdgcn_readfirstlane(x.tok0);
@@ -357,9 +372,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
       const int i = (row0 + tid) / a.group;
       int n = seq_n, nq = x.nq, qi = i;
       if (a.shared) {
-        const int s = a.q_off ? find_offset(a.q_off, a.seqs.n_seqs, i) : i / a.q_per_seq;
-        const int o = a.q_off ? a.q_off[s] : s * a.q_per_seq;
-        nq = a.q_off ? a.q_off[s + 1] - o : a.q_per_seq;
+        const Offsets off{a, tab};
+        const int s = a.ragged ? off.of_query(i) : i / a.q_per_seq;
+        const int o = a.ragged ? off.q(s) : s * a.q_per_seq;
+        nq = a.ragged ? off.q(s + 1) - o : a.q_per_seq;
         n = seq_len(a.seqs, s);
         qi = i - o;
       }
@@ -860,8 +876,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a)
 // go through LDS first, so that the loads of o depend on nothing.
 constexpr int kMergeParts = 512;   // weights held at a time
 template <typename T, int RPW>
-__global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendArgs pre,
-                                                           int row_blocks) {
+__global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, SharedParts pre,
+                                                           SeqTable tab, int row_blocks) {
   __shared__ float wts[RPW][kMergeParts / RPW];
   __shared__ __align__(16) float sums[256 * 4];
   __shared__ float lsum[256];
@@ -869,7 +885,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
   const int D = a.head_dim, tpd = D / 4;                  // threads per part
   const int rb = blockIdx.x % row_blocks;
   const int head = blockIdx.x / row_blocks % a.n_kv, unit = blockIdx.x / row_blocks / a.n_kv;
-  const Unit x = unit_of(a, unit);
+  const Unit x = unit_of(a, tab, unit);
   const int row0 = x.tile * a.rows, n_rows = min(a.rows, x.nq * a.group - row0);
   if (rb * RPW >= n_rows) return;
   const int2 it = a.unit_items[unit];                     // first item, parts
@@ -880,9 +896,9 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
   const int rr = valid ? r : n_rows - 1;                  // (a row of its own for every thread)
   const int i = (row0 + rr) / a.group, g = row0 + rr - i * a.group;
   const int t = x.tok0 + i, h = head * a.group + g;
-  const int n_pre = pre.shared ? pre.splits : 0, P = n_pre + it.y;
+  const int n_pre = pre.splits, P = n_pre + it.y;
   // part j: row index into the partial results of its pass
-  const int prow = t * a.group + g, ptile = pre.shared ? prow / pre.rows : 0;
+  const int prow = t * a.group + g, ptile = n_pre ? prow / pre.rows : 0;
   const int64_t pre_at = ((int64_t)ptile * n_pre * a.n_kv + head) * pre.rows + prow - ptile * pre.rows;
   const int64_t own_at = ((int64_t)it.x * a.n_kv + head) * a.rows + rr;
   const int64_t pre_step = (int64_t)a.n_kv * pre.rows, own_step = (int64_t)a.n_kv * a.rows;
@@ -972,25 +988,26 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, AttendA
 }
 
 template <typename T>
-hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, int most_rows, hipStream_t s) {
+hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTable& tab,
+                        int most_rows, hipStream_t s) {
   // one row per workgroup while there are few (their parts are many), else as
   // many as leave a row's dims to one wave's threads
   const int rows = most_rows < a.rows ? most_rows : a.rows;
   const int64_t tiles = (int64_t)a.n_units * a.n_kv;
   if (tiles * rows <= 4096) {
     CR_LAUNCH((attend_merge_kernel<T, 1>), dim3((unsigned)(tiles * rows)), dim3(256), 0, s, a, pre,
-              rows);
+              tab, rows);
   } else {
     const int blocks = (rows + 3) / 4;
     CR_LAUNCH((attend_merge_kernel<T, 4>), dim3((unsigned)(tiles * blocks)), dim3(256), 0, s, a,
-              pre, blocks);
+              pre, tab, blocks);
   }
   return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ launch
 template <typename T, int DM, bool EXACT>
-hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
+hipError_t attend_as(const AttendArgs& a, const SeqTable& tab, int64_t items, hipStream_t s) {
   const dim3 grid((unsigned)(items * a.n_kv));
   constexpr int WIDE = attend_rows(sizeof(T), DM, EXACT), KEYS = ValueOps<T>::KEYS;
   constexpr int OCC = sizeof(T) == 2 && DM <= 128 ? 2 : 1;   // workgroups to a CU that the registers allow
@@ -1001,9 +1018,9 @@ hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
   constexpr int KN = NARROW < KEYS ? KEYS : NARROW;
   constexpr int KW = sizeof(T) == 2 && DM <= 128 ? 2 * KEYS : KEYS;
   if (a.rows == 16) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a);
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a, tab);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a);
+    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a, tab);
   } else {
     return hipErrorInvalidValue;
   }
@@ -1011,17 +1028,17 @@ hipError_t attend_as(const AttendArgs& a, int64_t items, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t attend(const AttendArgs& a, hipStream_t s) {
+hipError_t attend(const AttendArgs& a, const SeqTable& tab, hipStream_t s) {
   const int64_t items = a.shared ? (int64_t)a.n_units * a.splits
                                  : (int64_t)a.n_units + (a.slots ? a.slots : 0);
   if (items * a.n_kv >= (int64_t)1 << 31) return hipErrorInvalidValue;
   switch (a.head_dim) {
-    case 64: return attend_as<T, 64, true>(a, items, s);
-    case 128: return attend_as<T, 128, true>(a, items, s);
-    case 256: return attend_as<T, 256, true>(a, items, s);
+    case 64: return attend_as<T, 64, true>(a, tab, items, s);
+    case 128: return attend_as<T, 128, true>(a, tab, items, s);
+    case 256: return attend_as<T, 256, true>(a, tab, items, s);
     case 32:
-    case 96: return attend_as<T, 128, false>(a, items, s);
-    default: return attend_as<T, 256, false>(a, items, s);
+    case 96: return attend_as<T, 128, false>(a, tab, items, s);
+    default: return attend_as<T, 256, false>(a, tab, items, s);
   }
 }
 

@@ -45,10 +45,11 @@ struct AttendArgs {
   void* o;
   float* lse;                       // [n_tokens][n_heads] or null
   int n_tokens, n_kv, group, head_dim;
-  // device offsets of the sequences' queries and units, or null where every
-  // sequence has q_per_seq queries and units_per_seq units
+  // where the sequences' queries and units begin: q_per_seq queries and
+  // units_per_seq units for each (ragged 0), or a table, in device memory or
+  // (null) in the launch's SeqTable
+  int ragged, q_per_seq, units_per_seq, n_units, rows;
   const int *q_off, *unit_off;
-  int q_per_seq, units_per_seq, n_units, rows;
   const int *lo, *hi;               // device interval of every query, or null
   float scale_log2;                 // score scale * log2(e)
   float cap_log2, scale_over_cap;   // cap * log2(e) (0: no cap), scale / cap
@@ -72,12 +73,24 @@ struct AttendArgs {
 constexpr int attend_rows(int element_bytes, int head_dim, bool exact) {
   return head_dim > 128 && (element_bytes == 4 || !exact) ? 64 : 128;
 }
+// Offsets of a ragged batch of at most kTableSeqs sequences, passed by value:
+// a launch less than a table in device memory (5 sequences: 4 us).
+constexpr int kTableSeqs = 128;
+struct SeqTable {
+  int q[kTableSeqs + 1], unit[kTableSeqs + 1];
+};
 template <typename T>
-hipError_t attend(const AttendArgs& a, hipStream_t s);
+hipError_t attend(const AttendArgs& a, const SeqTable& tab, hipStream_t s);
 
-// Joins the partial results of a planned pass and, with pre.shared > 0, those
-// of the pass over the shared keys.  most_rows: rows of the longest sequence.
+// The partial results of the pass over the shared keys (splits 0: none).
+struct SharedParts {
+  int splits, rows;
+  const float* part_o;
+  const float2* part_ml;
+};
+// Joins the partial results of a planned pass and those of the shared keys.  most_rows: rows of the longest sequence.
 template <typename T>
-hipError_t attend_merge(const AttendArgs& a, const AttendArgs& pre, int most_rows, hipStream_t s);
+hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTable& tab,
+                        int most_rows, hipStream_t s);
 
 }  // namespace cr

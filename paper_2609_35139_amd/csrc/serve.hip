@@ -132,7 +132,7 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     p.units = q->n_seqs * tiles(b.most);
   }
   Arena a;
-  if (b.off) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
+  if (b.off && q->n_seqs > kTableSeqs) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
   // split the keys unless the units fill the chip by themselves
   if (p.units * H < (p.rows == 16 ? 8192 : 512)) {
     // one round of two workgroups to a CU, or two where the units by themselves
@@ -208,8 +208,19 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
     a.bias = 1;
     for (int h = 0; h < n_heads; ++h) a.slopes_log2[h] = (float)(o.slopes[h] * log2e);
   }
-  if (b.off) {
-    // the sequences' first queries and first units, for the kernels
+  SeqTable tab{};
+  a.ragged = b.off != nullptr;
+  if (!a.ragged) {
+    a.q_per_seq = (int)b.most;
+    a.units_per_seq = (int)ceil_div(b.most * a.group, p.rows);
+  } else if (q->n_seqs <= kTableSeqs) {
+    for (int i = 0; i <= q->n_seqs; ++i) {
+      tab.q[i] = b.off[i];
+      tab.unit[i] = i == 0 ? 0
+                           : tab.unit[i - 1] +
+                                 (int)ceil_div((int64_t)(b.off[i] - b.off[i - 1]) * a.group, p.rows);
+    }
+  } else {
     const int n = q->n_seqs + 1;
     int* dev = reinterpret_cast<int*>(ws + p.tables);
     CR_TRY(timed("attend_table", s, [&] {
@@ -226,10 +237,7 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
       }
       return hipSuccess; }));
     a.q_off = dev;
-    a.unit_off = dev + q->n_seqs + 1;
-  } else {
-    a.q_per_seq = (int)b.most;
-    a.units_per_seq = (int)ceil_div(b.most * a.group, p.rows);
+    a.unit_off = dev + n;
   }
   a.slots = p.slots;
   a.min_tiles = p.min_tiles;
@@ -237,9 +245,9 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
   a.unit_items = reinterpret_cast<int2*>(ws + p.items);
   a.part_ml = reinterpret_cast<float2*>(ws + p.own_ml);
   a.part_o = reinterpret_cast<float*>(ws + p.own_o);
-  AttendArgs pre{};
+  SharedParts parts{};
   if (p.pre_units) {
-    pre = a;
+    AttendArgs pre = a;
     pre.shared = o.shared_len;
     pre.rows = p.pre_rows;
     pre.n_units = (int)p.pre_units;
@@ -249,14 +257,15 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
     pre.always_partial = 1;
     pre.part_ml = reinterpret_cast<float2*>(ws + p.pre_ml);
     pre.part_o = reinterpret_cast<float*>(ws + p.pre_o);
+    parts = SharedParts{p.splits, p.pre_rows, pre.part_o, pre.part_ml};
     a.key_begin = o.shared_len;
     a.always_partial = 1;
-    CR_TRY(timed("attend_shared", s, [&] { return attend<T>(pre, s); }));
+    CR_TRY(timed("attend_shared", s, [&] { return attend<T>(pre, tab, s); }));
   }
-  CR_TRY(timed("attend", s, [&] { return attend<T>(a, s); }));
+  CR_TRY(timed("attend", s, [&] { return attend<T>(a, tab, s); }));
   if (p.slots) {
     const int most_rows = (int)std::min<int64_t>(b.most * a.group, p.rows);
-    CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, pre, most_rows, s); }));
+    CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, parts, tab, most_rows, s); }));
   }
   return CR_OK;
 }

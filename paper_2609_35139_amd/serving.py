@@ -22,6 +22,10 @@ import torch
 
 from . import binding as B
 
+# handle of torch's current stream on a device (the Stream object that
+# torch.cuda.current_stream makes costs more than a launch's other checks)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda i: torch.cuda.current_stream(i).cuda_stream)
 _DTYPE = {torch.bfloat16: B.CR_DTYPE_BF16, torch.float32: B.CR_DTYPE_F32}
 
 
@@ -55,7 +59,7 @@ class PagedCache:
             raise TypeError("pool must be a bf16 or fp32 [L][2][n_blocks][block_size][H][d_h] tensor")
         if not pool.is_cuda or pool.stride(5) != 1:
             raise ValueError("pool must be device memory whose last dimension is contiguous")
-        self.pool = pool
+        self.pool, self.device = pool, pool.device
         L, _, self.n_blocks, self.block_size, H, d = pool.shape
         # (the stride of a dimension of one element addresses nothing)
         st = [x if n > 1 else 0 for x, n in zip(pool.stride(), pool.shape)]
@@ -70,36 +74,38 @@ class PagedCache:
         sequence's new tokens, or None for one each."""
         return Sequences(self, block_table, kv_lens, query_offsets)
 
-    def _rows(self, t: torch.Tensor, n: int, heads: Optional[int], name: str) -> B.cr_rows:
-        if t.dtype != self.pool.dtype or t.device != self.pool.device:
+    def _rows(self, t: torch.Tensor, n: int, heads: int, name: str) -> B.cr_rows:
+        if t.dtype is not self.pool.dtype or t.device != self.device:
             raise TypeError(f"{name} must have the cache's dtype and device")
-        if t.dim() != 3 or t.shape[0] != n or t.shape[2] != self.head_dim or \
-                (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected "
-                             f"({n}, {heads or 'heads'}, {self.head_dim})")
+        if t.shape != (n, heads, self.head_dim):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(n, heads, self.head_dim)}")
         st = t.stride()
         if st[2] != 1:
             raise ValueError(f"{name}: the last dimension must be contiguous")
-        return B.cr_rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if t.shape[1] > 1 else 0)
+        return B.cr_rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if heads > 1 else 0)
 
     def _index(self, t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.device != self.pool.device or t.shape != (n,) or \
+        if t.dtype is not torch.int32 or t.device != self.device or t.shape != (n,) or \
                 not t.is_contiguous():
             raise TypeError(f"{name} must be a contiguous int32 [{n}] tensor on the cache's device")
         return t.data_ptr()
 
-    def _enter(self, stream: Optional[torch.cuda.Stream]):
-        """The cache's device and the call's stream as torch's current ones: the
-        library launches on the current device, and a workspace belongs to the
-        stream that uses it."""
-        dev = self.pool.device
-        if stream is None:
-            return torch.cuda.device(dev)
-        if stream.device != dev:
-            raise ValueError("the stream must be on the cache's device")
-        return torch.cuda.stream(stream)
+    def _on(self, stream: Optional[torch.cuda.Stream], call) -> None:
+        """call(stream handle) with the cache's device and the call's stream as
+        torch's current ones: the library launches on the current device, and a
+        workspace or result allocated here belongs to the stream that uses it."""
+        if stream is not None:
+            if stream.device != self.device:
+                raise ValueError("the stream must be on the cache's device")
+            with torch.cuda.stream(stream):
+                call(stream.cuda_stream)
+        elif torch.cuda.current_device() == self.device.index:
+            call(_raw_stream(self.device.index))
+        else:
+            with torch.cuda.device(self.device):
+                call(_raw_stream(self.device.index))
 
     def append(self, layer: int, seqs: Sequences, k: torch.Tensor, v: torch.Tensor,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -114,19 +120,24 @@ class PagedCache:
         kr, vr = self._rows(k, n, self.n_kv_heads, "k"), self._rows(v, n, self.n_kv_heads, "v")
         pos = self._index(positions, n, "positions")
         rs, keep = (None, None) if rope is None else B.rope_struct(**rope)
-        if rs is not None and keep is not None and len(keep) != self.head_dim // 2:
+        if keep is not None and len(keep) != self.head_dim // 2:
             raise ValueError("inv_freq needs head_dim / 2 entries")
-        with self._enter(stream):
-            qr = qo = None
-            if q is not None:
-                qr = self._rows(q, n, None, "q")
-                if q_out is None:
-                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-                qo = self._rows(q_out, n, q.shape[1], "q_out")
+        heads = 0 if q is None else q.shape[1]
+        qr = None if q is None else self._rows(q, n, heads, "q")
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
+        result = q_out
+
+        def call(handle):
+            nonlocal result
+            if q is not None and result is None:
+                result = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            qo = None if q is None else self._rows(result, n, heads, "q_out")
             B.cr_append_kv(self.pool.data_ptr(), self.layout, layer, seqs.struct, kr, vr, qr, qo,
-                           0 if q is None else q.shape[1], rs, pos,
-                           torch.cuda.current_stream().cuda_stream)
-        return q_out
+                           heads, rs, pos, handle)
+
+        self._on(stream, call)
+        return result
 
     def workspace(self, seqs: Sequences, n_heads: int, shared_len: int = 0) -> torch.Tensor:
         """Device scratch for :meth:`attend` with these arguments."""
@@ -151,7 +162,7 @@ class PagedCache:
         those of cr_attend_options; slopes is a host sequence, lo, hi (int32)
         and lse (fp32 [n_tokens, n_heads]) are device tensors."""
         n, heads = seqs.n_tokens, q.shape[1]
-        qr = self._rows(q, n, None, "q")
+        qr = self._rows(q, n, heads, "q")
         o = B.cr_attend_options(scale, softcap)
         if slopes is not None:
             sl = np.ascontiguousarray(slopes, dtype=np.float32)
@@ -161,22 +172,27 @@ class PagedCache:
         o.lo, o.hi = self._index(lo, n, "lo"), self._index(hi, n, "hi")
         o.shared_len = shared_len
         if lse is not None:
-            if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or \
-                    lse.device != q.device:
-                raise TypeError(f"lse must be a contiguous fp32 [{n}, {heads}] tensor")
+            if lse.dtype is not torch.float32 or lse.shape != (n, heads) or \
+                    not lse.is_contiguous() or lse.device != self.device:
+                raise TypeError(f"lse must be a contiguous fp32 [{n}, {heads}] tensor on the "
+                                "cache's device")
             o.lse = lse.data_ptr()
-        with self._enter(stream):
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            orows = self._rows(out, n, heads, "out")
-            need = self._workspace_bytes(seqs, heads, shared_len)
+        need = self._workspace_bytes(seqs, heads, shared_len)
+        if workspace is not None and workspace.device != self.device:
+            raise ValueError("workspace must be on the cache's device")
+        result = out
+
+        def call(handle):
+            nonlocal result
+            if result is None:
+                result = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             ws = workspace
-            if ws is not None and ws.device != self.pool.device:
-                raise ValueError("workspace must be on the cache's device")
             if ws is None and need:
-                ws = torch.empty(need, dtype=torch.uint8, device=self.pool.device)
-            B.cr_attend(self.pool.data_ptr(), self.layout, layer, seqs.struct, qr, orows, heads, o,
+                ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            B.cr_attend(self.pool.data_ptr(), self.layout, layer, seqs.struct, qr,
+                        self._rows(result, n, heads, "out"), heads, o,
                         None if ws is None else ws.data_ptr(),
-                        0 if ws is None else ws.numel() * ws.element_size(),
-                        torch.cuda.current_stream().cuda_stream)
-        return out
+                        0 if ws is None else ws.numel() * ws.element_size(), handle)
+
+        self._on(stream, call)
+        return result

@@ -14,17 +14,18 @@ hipError_t append_kv(const AppendArgs&, const KeyRope&, const int32_t*, hipStrea
   return hipErrorInvalidValue;
 }
 template <typename T>
-hipError_t attend(const AttendArgs&, hipStream_t) { return hipErrorInvalidValue; }
+hipError_t attend(const AttendArgs&, const SeqTable&, hipStream_t) { return hipErrorInvalidValue; }
 template <typename T>
-hipError_t attend_merge(const AttendArgs&, const AttendArgs&, int, hipStream_t) {
+hipError_t attend_merge(const AttendArgs&, const SharedParts&, const SeqTable&, int, hipStream_t) {
   return hipErrorInvalidValue;
 }
 
 #define STUBS(T)                                                                              \
   template hipError_t append_kv<T>(const AppendArgs&, const KeyRope&, const int32_t*,        \
                                    hipStream_t);                                             \
-  template hipError_t attend<T>(const AttendArgs&, hipStream_t);                             \
-  template hipError_t attend_merge<T>(const AttendArgs&, const AttendArgs&, int, hipStream_t);
+  template hipError_t attend<T>(const AttendArgs&, const SeqTable&, hipStream_t);             \
+  template hipError_t attend_merge<T>(const AttendArgs&, const SharedParts&, const SeqTable&, \
+                                      int, hipStream_t);
 STUBS(bf16)
 STUBS(float)
 #undef STUBS
