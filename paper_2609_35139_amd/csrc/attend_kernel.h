@@ -367,7 +367,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   // position and interval of every row of the unit, and the keys that any row
   // sees (a row past the last one sees everything: it masks nothing)
   if (tid < C::ROWS) {
-    int4 w{INT_MIN, INT_MAX, 0, 0};
+    int4 w{0, INT_MAX, 0, 0};
     if (tid < n_rows) {
       const int i = (row0 + tid) / a.group;
       int n = seq_n, nq = x.nq, qi = i;
@@ -567,20 +567,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       return halves_or((int)(v[0] | v[1])) != 0;
     };
 
-    auto weigh = [&](const f32x4 (&s)[ST], int n, frag (&pf)[PF]) {
-      float ts = probs(s, reference(n), pf);
-      const bool over = m[n] == -INFINITY || !(ts <= kMostSum);
-      if (__any(over)) {
-        new_reference(s, n, any_in_row(over));
-        ts = probs(s, reference(n), pf);
-      }
-      return ts;
-    };
-
-    // KS keys that every row of the wave sees
-    auto whole = [&](auto other, const char* kt, const char* vt, int k0) {
-      // S^T: sub-tile t, row block n: keys k0 + 16 t + 4 g + [0, 4) of row c16
-      f32x4 s[NQ][ST];
+    // S^T of KS keys: sub-tile t, row block n: keys 16 t + 4 g + [0, 4) of row c16
+    auto scores = [&](const char* kt, int lane, f32x4 (&s)[NQ][ST]) {
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
 #pragma unroll
@@ -593,6 +581,11 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
           for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
         }
       }
+    };
+    // KS keys that every row of the wave sees
+    auto whole = [&](auto other, const char* kt, const char* vt, int k0) {
+      f32x4 s[NQ][ST];
+      scores(kt, lane, s);
       if constexpr (decltype(other)::value) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) transform(s[n], n, k0, lane);
@@ -636,88 +629,79 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
         }
     };
 
-    // Any other KS keys, one row block at a time: keys that a row does not see,
-    // keys past the segment, blocks that are none.
+    // Any other KS keys: keys that a row does not see, keys past the segment,
+    // blocks that are none.
     auto masked = [&](const char* kt, const char* vt, int k0) {
       // (addresses formed anew in every call: kept from call to call they would
       // fill the registers that the loop over whole tiles needs)
       const int lane = lane_again();
       const int c16 = lane & 15, g = lane >> 4;
-      // a value that is not finite must not reach a row that does not see its
+      f32x4 s[NQ][ST];
+      scores(kt, lane, s);
+      uint32_t see[NQ];            // visible bits of this lane's scores (bit t * 4 + e)
+      frag pf[NQ][PF];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if (general) transform(s[n], n, k0, lane);
+        const int4 w = info[(rg * NQ + n) * 16 + c16];
+        // of the lane's keys k0 + 4 g + 16 t + e, those in [lo, hi)
+        const int lo = w.x - k0 - 4 * g, hi = min(w.y, seg_end) - k0 - 4 * g;
+        see[n] = 0;
+#pragma unroll
+        for (int t = 0; t < ST; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            see[n] |= (t * 16 + e >= lo && t * 16 + e < hi) ? 1u << (t * 4 + e) : 0u;
+        if (seg_bad) {
+#pragma unroll 1
+          for (int b = 0; b < ST * 4; ++b) {
+            const int pg = (min(k0 + 4 * g + (b >> 2) * 16 + (b & 3), seg_end - 1) >> shift) - p0;
+            if ((none[pg / 32] >> (pg % 32)) & 1) see[n] &= ~(1u << b);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < ST; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!((see[n] >> (t * 4 + e)) & 1)) s[n][t][e] = -INFINITY;
+        float ts = probs(s[n], reference(n), pf[n]);
+        const bool over = m[n] == -INFINITY || !(ts <= kMostSum);
+        if (__any(over)) {
+          new_reference(s[n], n, any_in_row(over));
+          ts = probs(s[n], reference(n), pf[n]);
+        }
+        l[n] += ts;
+      }
+      // A value that is not finite must not reach a row that does not see its
       // key (0 * inf): such values are taken out, and added as what they do to
-      // the rows that see them
-      uint32_t bad = 0;
+      // the rows that see them.
 #pragma unroll
       for (int f = 0; f < PF; ++f)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           if (!EXACT && d * 16 >= D) break;
-          // (read by the whole wave: a transposing read crosses lanes)
-          const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-          bad |= VO::odd_bits(vf);
-        }
-      const bool odd = __any(bad != 0);
+          frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
+          if (__any(VO::odd_bits(vf) != 0)) {
+            const frag pos = VO::odd_part(vf, 0), neg = VO::odd_part(vf, 1);
+            vf = VO::finite_part(vf);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        f32x4 s[ST];
+            for (int n = 0; n < NQ; ++n) {
+              float b[KPL];
 #pragma unroll
-        for (int t = 0; t < ST; ++t) {
-          s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+              for (int e = 0; e < KPL; ++e) b[e] = (see[n] >> (f * KPL + e)) & 1 ? 1.f : 0.f;
+              const frag one = pack_frag(b, (frag*)nullptr);
+              const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+              const f32x4 cp = MM::mma(pos, one, zero), cn = MM::mma(neg, one, zero);
 #pragma unroll
-          for (int kk = 0; kk < QF; ++kk) {
-            if (!EXACT && kk * KSTEP >= D) break;
-            s[t] = MM::mma(key_frag(kt, t, kk, lane), qf[n][kk], s[t]);
-          }
-        }
-        if (general) transform(s, n, k0, lane);
-        const int4 w = info[(rg * NQ + n) * 16 + c16];
-        uint32_t see = 0;          // visible bits of this lane's scores (bit t * 4 + e)
-#pragma unroll
-        for (int t = 0; t < ST; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = k0 + t * 16 + 4 * g + e;
-            bool ok = key >= w.x && key < min(w.y, seg_end);
-            if (seg_bad && ok) {
-              const int pg = (key >> shift) - p0;
-              ok = !((none[pg / 32] >> (pg % 32)) & 1);
-            }
-            if (ok) see |= 1u << (t * 4 + e);
-            else s[t][e] = -INFINITY;
-          }
-        frag pf[PF];
-        l[n] += weigh(s, n, pf);
-#pragma unroll
-        for (int f = 0; f < PF; ++f) {
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            if (!EXACT && d * 16 >= D) break;
-            frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-            if (odd) vf = VO::finite_part(vf);
-            oacc[n][d] = MM::mma(vf, pf[f], oacc[n][d]);
-          }
-        }
-        if (!odd) continue;
-#pragma unroll
-        for (int f = 0; f < PF; ++f) {
-          float b[KPL];
-#pragma unroll
-          for (int e = 0; e < KPL; ++e) b[e] = (see >> (f * KPL + e)) & 1 ? 1.f : 0.f;
-          const frag one = pack_frag(b, (frag*)nullptr);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            if (!EXACT && d * 16 >= D) break;
-            const frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
-#pragma unroll
-            for (int sign = 0; sign < 2; ++sign) {
-              const f32x4 c = MM::mma(VO::odd_part(vf, sign), one, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (c[e] > 0.f) oacc[n][d][e] += sign ? -INFINITY : INFINITY;
+              for (int e = 0; e < 4; ++e) {
+                if (cp[e] > 0.f) oacc[n][d][e] += INFINITY;
+                if (cn[e] > 0.f) oacc[n][d][e] -= INFINITY;
+              }
             }
           }
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
         }
-      }
     };
 
     // ---- the segment's tiles: those before the window that every row of the
