@@ -139,9 +139,13 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     // nearly fill one (their ragged lengths then even out)
     p.slots = (int)std::max<int64_t>(1, 512 / H);
     if (p.rows == 16 && p.units * 4 > p.slots * 3) p.slots = (int)std::max<int64_t>(1, 1024 / H);
-    p.min_tiles = p.rows == 16 ? 2 : 4;
+    // a part has at least two tiles of 64 keys, or one for fp32, where a tile
+    // takes eight times as long: 4 / 2 / 1 tiles took 39 / 28.9 / 24.4 us for 8 x
+    // 161 fp32 questions over 769 keys, 42 / 38.4 / 38.5 us for bf16 documents,
+    // and one took 44.0 instead of 40.4 us for 9 bf16 sequences over 1177 keys
+    p.min_tiles = l->dtype == CR_DTYPE_F32 ? 1 : 2;
     // one part holds all keys there can be
-    if ((int64_t)q->max_blocks * q->block_size <= 256) p.slots = 0;
+    if ((int64_t)q->max_blocks * q->block_size <= 128 * p.min_tiles) p.slots = 0;
   }
   if (p.slots && shared > 0) {
     p.pre_units = ceil_div(b.n_tokens * G, p.pre_rows);
