@@ -550,9 +550,9 @@ CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t laye
  *              slot.  Documents, a bidirectional prefix, windows.
  *  shared_len: the first shared_len slots of every sequence are in the same
  *              blocks (those of sequence 0's row of the table), whose keys are
- *              then read once for the whole batch; at most max_blocks *
- *              block_size.  Changes no result but for rounding.  A sequence may
- *              be shorter.
+ *              then read once for the whole batch where that saves more than
+ *              the extra pass costs; at most max_blocks * block_size.  Changes
+ *              no result but for rounding.  A sequence may be shorter.
  *  lse:        NULL, or device, [n_tokens][n_heads] fp32: the logarithm of the
  *              sum of exponentials of every row's scores.
  */
@@ -594,11 +594,11 @@ CR_API cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t l
 
 /*
  * Per-launch timing (tracing aid, not needed for repair).  While enabled,
- * cr_repair, cr_append_kv and cr_attend bracket every kernel launch with HIP events recorded on the
- * call's own stream.  cr_profile_enable(max_launches) creates the events
- * (host-side allocation happens here, never inside cr_repair);
- * max_launches = 0 disables profiling and destroys them.  Launches beyond
- * max_launches since the last reset are not timed.  cr_profile_read waits for
+ * cr_repair, cr_append_kv and cr_attend bracket every kernel launch with HIP
+ * events recorded on the call's own stream.  cr_profile_enable(max_launches)
+ * creates the events (host-side allocation happens here, never inside
+ * cr_repair); max_launches = 0 disables profiling and destroys them.  Launches
+ * beyond max_launches since the last reset are not timed.  cr_profile_read waits for
  * the recorded events, then fills up to max_stats entries, one per kernel
  * class in first-launch order, and resets the record (also when it returns
  * an error).  A stage whose launch failed is left out of the record: its

@@ -130,6 +130,12 @@ __device__ __forceinline__ Item plan_item(const AttendArgs& a, const SeqTable& t
     if (cnt <= (float)a.slots) break;
     chunk += max(1, (int)((float)chunk * (cnt / (float)a.slots - 1.f) * 0.7f));
   }
+  if (a.split_cost > 0.f) {
+    const int limit = (int)fminf((float)chunk * a.split_cost + a.join_cost, 1e9f);
+    bool longer = false;
+    for (int u0 = 0; u0 < U; u0 += 64) longer |= __any(tiles(u0) > limit);
+    if (!longer) chunk = limit;
+  }
   chunk = __builtin_amdgcn_readfirstlane(chunk);
   Item r{-1, 0, 1, chunk, 0};
   int base = 0;
@@ -355,6 +361,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
     if (p.unit < 0) return;
     unit = p.unit; part = p.part; parts = p.parts; chunk = p.chunk;
     if (part == 0 && head == 0 && tid == 0) a.unit_items[unit] = make_int2(p.first, p.parts);
+  } else if (a.always_partial && head == 0 && tid == 0) {
+    a.unit_items[unit] = make_int2(unit, 1);
   }
   Unit x{0, unit, 0, a.n_tokens};
   if (!a.shared) x = unit_of(a, tab, unit);

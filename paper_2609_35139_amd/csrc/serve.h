@@ -60,9 +60,11 @@ struct AttendArgs {
   int key_begin, shared;
   // splits of the keys: planned on the device from the lengths (slots > 0:
   // about that many items per KV head, at least min_tiles 64-key tiles each; no
-  // more than slots items where there are at most one_round units),
-  // or fixed (shared: `splits` of split_tiles tiles), or none
+  // more than slots items where there are at most one_round units; no split if
+  // the longest unit takes at most chunk * split_cost + join_cost tiles, given
+  // split_cost > 0), or fixed (shared: `splits` of split_tiles tiles), or none
   int slots, min_tiles, one_round, splits, split_tiles;
+  float split_cost, join_cost;
   int always_partial;               // write partial results for the merge
   int2* unit_items;                 // [unit] first item and parts, for the merge
   float* part_o;                    // [item][kv head][rows][head_dim]

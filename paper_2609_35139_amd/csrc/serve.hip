@@ -112,11 +112,33 @@ struct Plan {
   int rows = 0, pre_rows = 0;    // rows of a unit of either pass
   int64_t units = 0;             // of the pass over each sequence's own keys
   int slots = 0, min_tiles = 0;  // its split (slots 0: none)
+  float split_cost = 0.f, join_cost = 0.f;
   int64_t own_items = 0;         // partial results of that pass, per KV head
   int64_t pre_units = 0;         // units of the pass over the shared keys, its split
   int splits = 0, split_tiles = 0;
   uint64_t tables = 0, items = 0, own_ml = 0, own_o = 0, pre_ml = 0, pre_o = 0, total = 0;
 };
+
+// Whether one pass over the shared keys for the rows of all sequences takes less
+// time than every sequence's own.  The pass and the merge of its parts add about
+// 14 us to a call; it saves a unit's turn over the shared keys for each unit of
+// the sequences.  What a unit takes per key and KV head, with the chip full
+// (bf16, 128 dims, in picoseconds): 16 rows 26 (reading the keys, which lie in
+// the caches by then), wide units 64, or 45 where rows are missing.  Measured
+// with 32 query and 8 KV heads, shared pass against none, 100 keys more each: 32
+// sequences of one token over 2048 shared keys 31 / 29 us, over 16384 46 / 121;
+// of 8 tokens over 2048 51 / 45 us, over 16384 101 / 207; of 32 tokens, which
+// fill their units, 322 / 289.
+bool shared_pays(const cr_kv_layout* l, const Batch& b, int G, const Plan& p, int shared) {
+  const double elt = (double)esize(l->dtype), D = l->head_dim;
+  const double wide = D / 128 * (elt == 4 ? 8 : 1) * attend_rows((int)elt, (int)D, D == 256) / 128;
+  const double own = p.rows == 16 ? 26 * D / 128 * elt / 2 : 45 * wide;
+  const double pre = p.pre_rows == 16 ? 26 * D / 128 * elt / 2 : 64 * wide;
+  const double per_key = own * (double)p.units - pre * (double)ceil_div(b.n_tokens * G, p.pre_rows);
+  // (units that were not to be split would leave no partial results otherwise)
+  const double join = p.slots ? 0 : 2.4 * (double)p.units * p.rows * D;
+  return l->n_kv_heads * (per_key * shared - join) > 16e6;
+}
 
 Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, int n_heads,
                  int shared) {
@@ -134,10 +156,16 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   Arena a;
   if (b.off && q->n_seqs > kTableSeqs) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
   // split the keys unless the units fill the chip by themselves
+  int resident = 2;
   if (p.units * H < (p.rows == 16 ? 8192 : 512)) {
-    // one round of two workgroups to a CU, or two where the units by themselves
-    // nearly fill one (their ragged lengths then even out)
-    p.slots = (int)std::max<int64_t>(1, 512 / H);
+    // one round of the workgroups that a CU holds (two, but one where a wave
+    // takes more than 256 registers: 52.6 / 45.9 us with parts for 512 / 256 of
+    // those for 5 x 32 fp32 questions of 128 dims over 3,000 keys), or two rounds
+    // where the units by themselves nearly fill one (their ragged lengths then
+    // even out)
+    resident = p.rows != 16 && D > (l->dtype == CR_DTYPE_F32 ? 64 : 128) ? 1 : 2;
+    const int round = 256 * resident;
+    p.slots = (int)std::max<int64_t>(1, round / H);
     if (p.rows == 16 && p.units * 4 > p.slots * 3) p.slots = (int)std::max<int64_t>(1, 1024 / H);
     // a part has at least two tiles of 64 keys, or one for fp32, where a tile
     // takes eight times as long: 4 / 2 / 1 tiles took 39 / 28.9 / 24.4 us for 8 x
@@ -147,15 +175,27 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     // one part holds all keys there can be
     if ((int64_t)q->max_blocks * q->block_size <= 128 * p.min_tiles) p.slots = 0;
   }
-  if (p.slots && shared > 0) {
+  if (shared_pays(l, b, G, p, shared)) {
     p.pre_units = ceil_div(b.n_tokens * G, p.pre_rows);
     const int64_t key_tiles = ceil_div(shared, 64);
     const int64_t want = std::max<int64_t>(1, 512 / (p.pre_units * H));
-    p.split_tiles = (int)std::max<int64_t>(p.min_tiles, ceil_div(key_tiles, want));
+    p.split_tiles = (int)std::max<int64_t>(2, ceil_div(key_tiles, want));
     p.splits = (int)ceil_div(key_tiles, p.split_tiles);
   }
-  p.own_items = p.slots ? p.units + p.slots : 0;
-  if (p.slots) p.items = a.take((uint64_t)p.units * 8);
+  // No split where it gains less than the merge takes: 2 us and 2.4 us for every
+  // million sums, at 2 us for a wide bf16 tile of 128 dims.  A workgroup that
+  // has its CU to itself takes two thirds of the time per tile, and with more
+  // units than fit one round a split pays for very uneven lengths alone.  20
+  // sequences of 32 tokens, 300 keys, 8 KV heads: 36 us split, 28 in one part;
+  // 32 of them over 600 keys 48 and 37.5, over 2400 95 and 107; a prompt of 2000
+  // tokens, 63 units, over 4800 keys 313 and 216.
+  if (p.slots && !p.pre_units && p.rows != 16) {
+    const double tile = 2.0 * D / 128 * p.rows / 128 * (l->dtype == CR_DTYPE_F32 ? 8 : 1);
+    p.split_cost = p.units > p.slots * 3 / 4 ? 2.f : p.units * H <= 256 && resident > 1 ? 1.5f : 1.f;
+    p.join_cost = (float)((2 + 2.4e-6 * (double)p.units * H * p.rows * D) / tile);
+  }
+  p.own_items = p.slots ? p.units + p.slots : p.pre_units ? p.units : 0;
+  if (p.own_items) p.items = a.take((uint64_t)p.units * 8);
   const uint64_t own = (uint64_t)p.own_items * H * p.rows;
   const uint64_t pre = (uint64_t)p.pre_units * p.splits * H * p.pre_rows;
   p.own_ml = a.take(own * 8);
@@ -245,6 +285,8 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
   }
   a.slots = p.slots;
   a.min_tiles = p.min_tiles;
+  a.split_cost = p.split_cost;
+  a.join_cost = p.join_cost;
   a.one_round = p.slots * 3 / 4;
   a.unit_items = reinterpret_cast<int2*>(ws + p.items);
   a.part_ml = reinterpret_cast<float2*>(ws + p.own_ml);
@@ -267,7 +309,7 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
     CR_TRY(timed("attend_shared", s, [&] { return attend<T>(pre, tab, s); }));
   }
   CR_TRY(timed("attend", s, [&] { return attend<T>(a, tab, s); }));
-  if (p.slots) {
+  if (p.own_items) {
     const int most_rows = (int)std::min<int64_t>(b.most * a.group, p.rows);
     CR_TRY(timed("attend_merge", s, [&] { return attend_merge<T>(a, parts, tab, most_rows, s); }));
   }

@@ -101,9 +101,9 @@ def append_oracle(b, layer, theta=1e6, scale=1.0, positions=None, rotate=True):
 
 
 def attend_oracle(b, layer, scale=None, softcap=0.0, slopes=None, lo=None, hi=None, pool=None,
-                  q=None, table=None):
+                  q=None, tokens=None):
     """(out, lse, bound on out's error, bound on lse's) in 64 bits, from the
-    keys that a query sees alone."""
+    keys that a query sees alone; of the given tokens (None: all)."""
     scale = 1 / math.sqrt(b.d) if scale is None else scale
     pool = (b.pool if pool is None else pool).double()
     q = (b.qh if q is None else q).double()
@@ -113,7 +113,9 @@ def attend_oracle(b, layer, scale=None, softcap=0.0, slopes=None, lo=None, hi=No
     tol, ltol = torch.zeros_like(out), torch.zeros_like(lse)
     half = HALF[b.dtype]
     most = b.table.shape[1] * b.bs
-    for t, (s, p) in enumerate(b.slots()):
+    slots = b.slots()
+    for t in range(b.N) if tokens is None else tokens:
+        s, p = slots[t]
         n = min(max(b.lens[s], 0), most)
         a = 0 if lo is None else max(int(lo[t]), 0)
         e = min(p + 1 if hi is None else int(hi[t]), n)

@@ -222,6 +222,128 @@ def test_shared_prefix(dtype, d, shared, q, lens):
            slopes=[0.01 * h for h in range(8)])
 
 
+def _launched(call):
+    """(result, names of the launches) of a call."""
+    from paper_2609_35139_amd import binding as B
+    B.cr_profile_enable(64)
+    try:
+        out = call()
+        return out, {r["name"] for r in B.cr_profile_read()}
+    finally:
+        B.cr_profile_enable(0)
+
+
+READ_ONCE = {
+    # tokens of many sequences; some end inside the prefix, some see nothing
+    "tokens": dict(dtype="bf16", heads=16, kv_heads=8, d=128, q=[1] * 120, shared=1000,
+                   more=lambda s: [37, -400, 300, 1, -1000, 129][s % 6]),
+    # more sequences than travel with a launch, rows that fill no unit; with the
+    # shorter prefix the pass would cost more than it saves
+    "questions": dict(dtype="bf16", heads=24, kv_heads=4, d=128, q=[3, 4, 0, 5] * 44, shared=2201,
+                      more=lambda s: 7 + s % 90),
+    "questions-short": dict(dtype="bf16", heads=24, kv_heads=4, d=128, q=[3, 4, 0, 5] * 44,
+                            shared=1001, more=lambda s: 7 + s % 90, once=False),
+    "f32": dict(dtype="f32", heads=8, kv_heads=8, d=64, q=[1] * 100, shared=900,
+                more=lambda s: s % 80),
+    "d256": dict(dtype="bf16", heads=8, kv_heads=8, d=256, q=[1] * 70, shared=600,
+                 more=lambda s: 3 * s),
+    # no unit is split: as many as fill the chip
+    "many": dict(dtype="bf16", heads=8, kv_heads=8, d=64, q=[1] * 1040, shared=700,
+                 more=lambda s: 1 + s % 20),
+    # 512 parts of the prefix and one more, for a few rows
+    "far": dict(dtype="bf16", heads=1, kv_heads=1, d=64, q=[1] * 16, shared=131072,
+                more=lambda s: 5 * s),
+    # 56 parts of the prefix and 14 more, for many rows
+    "wide-group": dict(dtype="bf16", heads=16, kv_heads=1, d=128, q=[1] * 70, shared=14336,
+                       more=lambda s: 1800 - s),
+}
+
+
+@pytest.mark.parametrize("name", READ_ONCE)
+def test_shared_prefix_read_once(name):
+    """Batches for which the pass over the shared keys pays (but one), and
+    without it, against the oracle."""
+    c = dict(READ_ONCE[name])
+    shared, more, once = c.pop("shared"), c.pop("more"), c.pop("once", True)
+    lens = [shared + more(s) for s in range(len(c["q"]))]
+    b = Batch(lens=lens, bs=16, seed=33, shared=-(-shared // 16) * 16, **c)
+    cache, seqs, q, _, _ = b.cuda()
+    lse = torch.empty(b.N, b.heads, device="cuda")
+    out, names = _launched(lambda: cache.attend(0, seqs, q, lse=lse, shared_len=shared))
+    assert ("attend_shared" in names) == once
+    plain, names = _launched(lambda: cache.attend(0, seqs, q))
+    assert "attend_shared" not in names
+    assert torch.equal(out, cache.attend(0, seqs, q, shared_len=shared))
+    tell = range(b.N) if name in ("tokens", "f32", "d256", "far") else range(0, b.N, 7)
+    ref, rl, tol, ltol = attend_oracle(b, 0, tokens=tell)
+    for what, x in (("shared", out), ("plain", plain)):
+        assert_within(x[list(tell)], ref[list(tell)], tol[list(tell)], what)
+    assert_within(lse[list(tell)], rl[list(tell)], ltol[list(tell)], "lse")
+
+
+def test_shared_prefix_masked_and_replayed():
+    """The pass over shared keys under windows, a cap and distance slopes, in a
+    captured graph that is replayed while the queries change."""
+    shared, n = 1000, 120
+    b = Batch("bf16", 16, 8, 128, 16, [1] * n, [shared + s % 50 for s in range(n)], seed=35,
+              shared=1008)
+    cache, seqs, q, _, _ = b.cuda()
+    p = np.array([j for _, j in b.slots()])
+    lo, hi = p - 300 - 7 * np.arange(n), np.where(p % 4 == 1, 0, p + 1)
+    opt = dict(softcap=8.0, slopes=[0.01 * h for h in range(16)])
+    dev = dict(lo=torch.tensor(lo, dtype=torch.int32).cuda(),
+               hi=torch.tensor(hi, dtype=torch.int32).cuda(), shared_len=shared, **opt)
+    q = q.contiguous()
+    first, names = _launched(lambda: cache.attend(0, seqs, q, **dev))
+    assert "attend_shared" in names
+    ref, _, tol, _ = attend_oracle(b, 0, lo=lo, hi=hi, **opt)
+    assert_within(first, ref, tol, "masked")
+    ws, out = cache.workspace(seqs, 16, shared), torch.empty_like(q)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.attend(0, seqs, q, out=out, workspace=ws, **dev)
+    for i in range(4):
+        q.mul_(0.9)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, cache.attend(0, seqs, q, **dev)), i
+
+
+@pytest.mark.parametrize("name", ["plan-of-200", "tokens-unsplit", "questions-unsplit", "even", "uneven"])
+def test_how_a_batch_is_split(name):
+    """Batches whose units are planned beyond one wave's worth, are too many to
+    split, or are split or left whole by the device's rule."""
+    c = {
+        "plan-of-200": dict(heads=2, kv_heads=1, d=64, q=[s % 21 for s in range(200)],
+                            lens=[21 + (37 * s) % 300 for s in range(200)]),
+        "tokens-unsplit": dict(heads=8, kv_heads=8, d=64, q=[1] * 1030,
+                               lens=[1 + (13 * s) % 280 for s in range(1030)]),
+        "questions-unsplit": dict(heads=16, kv_heads=16, d=64, q=[17] * 33,
+                                  lens=[17 + 11 * s for s in range(33)]),
+        "even": dict(heads=16, kv_heads=4, d=128, q=[32] * 20, lens=[332] * 20),
+        "uneven": dict(heads=16, kv_heads=4, d=128, q=[32, 9, 17], lens=[4000, 32, 600]),
+    }[name]
+    _check(Batch("bf16", bs=16, seed=37, **c))
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own."""
+    b = Batch("bf16", 8, 2, 128, 16, [1] * 6, [3000, 40, 900, 2500, 1, 700], seed=39)
+    cache, seqs, q, _, _ = b.cuda()
+    q = q.contiguous()
+    want = cache.attend(0, seqs, q)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [cache.workspace(seqs, 8) for _ in streams]
+    outs = [torch.empty(20, *q.shape, dtype=q.dtype, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, w, o in zip(streams, ws, outs):
+            cache.attend(0, seqs, q, out=o[i], workspace=w, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(x, want) for x in o)
+
+
 def test_pool_of_other_strides_and_strided_rows():
     """Block-major pool with K and V and layers inside a block; queries and
     results with strides of their own; only the result's rows are written."""
