@@ -171,6 +171,11 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // Rows of RB bytes in 16-byte chunks; chunk c of row r lies in slot
 // c ^ f(r), f periodic in 16 rows, so that the 16 rows of a fragment read and
 // the four rows of a transposing read start in distinct banks.
+constexpr int tile_row_bytes(int bytes) {
+  int r = 64;
+  while (r < bytes) r *= 2;
+  return r;
+}
 template <int RB>
 __device__ __forceinline__ int row_swizzle(int row) {
   constexpr int CPR = RB / 16;
@@ -304,15 +309,15 @@ __device__ __forceinline__ int lane_again() {
 // ------------------------------------------------------------------ kernel
 // RG * KG waves: KG groups of RG waves walk alternate tiles of KT keys, each
 // with its own ring of STAGES tiles; the RG waves of a group own 16 * NQ rows
-// each.  DM: head_dim (EXACT) or an upper bound of it.
-template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES>
+// each.
+template <typename T, int D, int NQ, int RG, int KG, int KT, int STAGES>
 struct AttendCfg {
   static constexpr int WAVES = RG * KG, NT = 64 * WAVES, ROWS = 16 * NQ * RG;
-  static constexpr int RB = DM * (int)sizeof(T), CPR = RB / 16, RPW = 1024 / RB;
+  static constexpr int RB = tile_row_bytes(D * (int)sizeof(T)), CPR = RB / 16, RPW = 1024 / RB;
   static constexpr int TILE = KT * RB;                    // bytes of a K or V tile
   static constexpr int ROUNDS = TILE / (RG * 1024);       // transfers per wave and tile
   static constexpr int RING = STAGES * 2 * TILE;
-  static constexpr int MLD = DM + 4;                      // merge rows, in floats
+  static constexpr int MLD = D + 4;                      // merge rows, in floats
   static constexpr int MERGE = KG > 1 ? KG * ROWS * (MLD + 2) * 4 : 0;
   static constexpr int LDS = KG * RING > MERGE ? KG * RING : MERGE;
   static_assert(ROUNDS * RG * 1024 == TILE && RPW >= 1 && KT % ValueOps<T>::KEYS == 0, "tile");
@@ -322,18 +327,18 @@ struct AttendCfg {
   static_assert(KT <= 128 && KT * KG < kListPages, "bits of a lane's scores, keys of a list");
 };
 
-template <typename T, int DM, bool EXACT, int NQ, int RG, int KG, int KT, int STAGES, int OCC = 1>
+template <typename T, int D, int NQ, int RG, int KG, int KT, int STAGES, int OCC = 1>
 __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a, SeqTable tab) {
-  using C = AttendCfg<T, DM, EXACT, NQ, RG, KG, KT, STAGES>;
+  using C = AttendCfg<T, D, NQ, RG, KG, KT, STAGES>;
   using MM = Mma16<T>;
   using VO = ValueOps<T>;
   using frag = typename MM::frag;
   constexpr int KPL = MM::KPL, KSTEP = MM::KSTEP;
   // a wave works on KS keys of a tile at a time
   constexpr int KS = VO::KEYS;
-  constexpr int QF = DM / KSTEP, DT = DM / 16, ST = KS / 16, PF = KS / VO::KEYS;
+  constexpr int QF = D / KSTEP, DT = D / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
-  constexpr int VE = EXACT && NQ > 1 && sizeof(T) == 2 && DM <= 128 ? 3 : 0;
+  constexpr int VE = NQ > 1 && sizeof(T) == 2 && D >= 64 && D <= 128 ? 3 : 0;
   // rings (later the merge area), the segment's block list (addresses of the
   // blocks' keys), the bits of those that are no block, and of every row (lo,
   // hi, p, slope): one array, since the compiler waits for every transfer in
@@ -346,7 +351,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wave / RG, rg = wave % RG;
-  const int D = EXACT ? DM : a.head_dim;
   const int head = blockIdx.x % a.n_kv;                    // KV head
   const int item = blockIdx.x / a.n_kv;
 
@@ -426,8 +430,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
                   (int64_t)(head * a.group + row0 + min(r, n_rows - 1) - i * a.group) * a.q_head;
 #pragma unroll
     for (int kk = 0; kk < QF; ++kk)
-      qf[n][kk] = r < n_rows && (EXACT || kk * KSTEP < D)
-                      ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
+      qf[n][kk] = r < n_rows ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
@@ -497,7 +500,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       for (int r = 0; r < C::ROUNDS; ++r) {
         const int row = (r * RG + rg) * C::RPW + lane / C::CPR;
         int ch = (lane % C::CPR) ^ row_swizzle<RB>(row);
-        if (!EXACT && ch * 16 >= D * (int)sizeof(T)) ch = 0;
+        if (D * (int)sizeof(T) < RB && ch * 16 >= D * (int)sizeof(T)) ch = 0;   // (never read)
         const int key = min(k0 + row, seg_end - 1);      // never past the last key seen
         src[r] = list[(key >> shift) - p0] + (uint64_t)(uint32_t)(key & page_mask) * token_bytes + ch * 16;
       }
@@ -583,7 +586,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
         for (int n = 0; n < NQ; ++n) s[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < QF; ++kk) {
-          if (!EXACT && kk * KSTEP >= D) break;
           const frag kf = key_frag(kt, t, kk, lane);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) s[n][t] = MM::mma(kf, qf[n][kk], s[n][t]);
@@ -629,7 +631,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       for (int f = 0; f < PF; ++f)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          if (!EXACT && d * 16 >= D) break;
           const frag vf = d < VE ? ve[f][d < VE ? d : 0]
                                  : VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
 #pragma unroll
@@ -687,7 +688,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       for (int f = 0; f < PF; ++f)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          if (!EXACT && d * 16 >= D) break;
           frag vf = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
           if (__any(VO::odd_bits(vf) != 0)) {
             const frag pos = VO::odd_part(vf, 0), neg = VO::odd_part(vf, 1);
@@ -787,7 +787,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       T* op = static_cast<T*>(a.o) + t * a.o_token + (int64_t)hd * a.o_head;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        if (!EXACT && d * 16 >= D) break;
         if (partial) {
           *reinterpret_cast<f32x4*>(a.part_o + (prow + r) * D + d * 16 + 4 * g) = oacc[n][d];
         } else {
@@ -817,8 +816,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       const int r = kg * C::ROWS + (rg * NQ + n) * 16 + c16;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        if (EXACT || d * 16 < D)
-          *reinterpret_cast<f32x4*>(mo + r * C::MLD + d * 16 + 4 * g) = oacc[n][d];
+        *reinterpret_cast<f32x4*>(mo + r * C::MLD + d * 16 + 4 * g) = oacc[n][d];
       if (g == 0) ml[r] = make_float2(m[n], lt[n]);
     }
     __syncthreads();
@@ -1005,21 +1003,23 @@ hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTa
 }
 
 // ------------------------------------------------------------------ launch
-template <typename T, int DM, bool EXACT>
+template <typename T, int D>
 hipError_t attend_as(const AttendArgs& a, const SeqTable& tab, int64_t items, hipStream_t s) {
   const dim3 grid((unsigned)(items * a.n_kv));
-  constexpr int WIDE = attend_rows(sizeof(T), DM, EXACT), KEYS = ValueOps<T>::KEYS;
-  constexpr int OCC = sizeof(T) == 2 && DM <= 128 ? 2 : 1;   // workgroups to a CU that the registers allow
+  constexpr int WIDE = attend_rows(sizeof(T), D), KEYS = ValueOps<T>::KEYS;
+  constexpr int RB = tile_row_bytes(D * (int)sizeof(T));
+  constexpr int OCC = attend_resident(sizeof(T), D);
   // 16 rows (the heads of a group for one new token): bound by reading the
-  // keys.  Two waves with a ring of two 16 KB tiles of their own each (32 KB
-  // for wide heads), two workgroups to a CU.
-  constexpr int NARROW = 64 * 128 / (DM * (int)sizeof(T));
-  constexpr int KN = NARROW < KEYS ? KEYS : NARROW;
-  constexpr int KW = sizeof(T) == 2 && DM <= 128 ? 2 * KEYS : KEYS;
+  // keys.  Two waves with a ring of two 8 KB tiles of K and of V each (16 KB for
+  // wide heads), two workgroups to a CU.
+  constexpr int KN = 8192 / RB < KEYS ? KEYS : 8192 / RB;
+  // wide units: a transfer of 1 KB for each of the four waves at least
+  constexpr int KM = sizeof(T) == 2 && D <= 128 ? 2 * KEYS : KEYS;
+  constexpr int KW = KM < 4096 / RB ? 4096 / RB : KM;
   if (a.rows == 16) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a, tab);
+    CR_LAUNCH((attend_kernel<T, D, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a, tab);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, DM, EXACT, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a, tab);
+    CR_LAUNCH((attend_kernel<T, D, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a, tab);
   } else {
     return hipErrorInvalidValue;
   }
@@ -1032,12 +1032,15 @@ hipError_t attend(const AttendArgs& a, const SeqTable& tab, hipStream_t s) {
                                  : (int64_t)a.n_units + (a.slots ? a.slots : 0);
   if (items * a.n_kv >= (int64_t)1 << 31) return hipErrorInvalidValue;
   switch (a.head_dim) {
-    case 64: return attend_as<T, 64, true>(a, tab, items, s);
-    case 128: return attend_as<T, 128, true>(a, tab, items, s);
-    case 256: return attend_as<T, 256, true>(a, tab, items, s);
-    case 32:
-    case 96: return attend_as<T, 128, false>(a, tab, items, s);
-    default: return attend_as<T, 256, false>(a, tab, items, s);
+    case 32: return attend_as<T, 32>(a, tab, items, s);
+    case 64: return attend_as<T, 64>(a, tab, items, s);
+    case 96: return attend_as<T, 96>(a, tab, items, s);
+    case 128: return attend_as<T, 128>(a, tab, items, s);
+    case 160: return attend_as<T, 160>(a, tab, items, s);
+    case 192: return attend_as<T, 192>(a, tab, items, s);
+    case 224: return attend_as<T, 224>(a, tab, items, s);
+    case 256: return attend_as<T, 256>(a, tab, items, s);
+    default: return hipErrorInvalidValue;
   }
 }
 

@@ -70,10 +70,16 @@ struct AttendArgs {
   float* part_o;                    // [item][kv head][rows][head_dim]
   float2* part_ml;                  // [item][kv head][rows] (max, sum)
 };
-// Rows of a wide unit: 128, or 64 where the accumulators of heads over 128 fill
-// the registers (exact: the kernel is compiled for the very head_dim).
-constexpr int attend_rows(int element_bytes, int head_dim, bool exact) {
-  return head_dim > 128 && (element_bytes == 4 || !exact) ? 64 : 128;
+// Rows of a wide unit: 128, or 64 where 128 rows' accumulators would leave a
+// SIMD one wave (bf16 heads of 256: 327 / 241 us with 128 / 64 rows for 11 x 400
+// tokens over 5,000 keys, 64 / 53 for 8 x 32; fp32 heads of 128: 50 / 36 for 60 x
+// 3 over 300); and how many such workgroups a CU holds (fp32 heads over 192 take
+// more than 256 registers even so).
+constexpr int attend_rows(int element_bytes, int head_dim) {
+  return head_dim > (element_bytes == 4 ? 96 : 128) ? 64 : 128;
+}
+constexpr int attend_resident(int element_bytes, int head_dim) {
+  return element_bytes == 4 && head_dim > 192 ? 1 : 2;
 }
 // Offsets of a ragged batch of at most kTableSeqs sequences, passed by value:
 // a launch less than a table in device memory (5 sequences: 4 us).

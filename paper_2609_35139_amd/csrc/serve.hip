@@ -131,7 +131,7 @@ struct Plan {
 // fill their units, 322 / 289.
 bool shared_pays(const cr_kv_layout* l, const Batch& b, int G, const Plan& p, int shared) {
   const double elt = (double)esize(l->dtype), D = l->head_dim;
-  const double wide = D / 128 * (elt == 4 ? 8 : 1) * attend_rows((int)elt, (int)D, D == 256) / 128;
+  const double wide = D / 128 * (elt == 4 ? 8 : 1) * attend_rows((int)elt, (int)D) / 128;
   const double own = p.rows == 16 ? 26 * D / 128 * elt / 2 : 45 * wide;
   const double pre = p.pre_rows == 16 ? 26 * D / 128 * elt / 2 : 64 * wide;
   const double per_key = own * (double)p.units - pre * (double)ceil_div(b.n_tokens * G, p.pre_rows);
@@ -144,7 +144,7 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
                  int shared) {
   Plan p;
   const int G = n_heads / l->n_kv_heads, D = l->head_dim, H = l->n_kv_heads;
-  const int wide = attend_rows((int)esize(l->dtype), D, D == 256);
+  const int wide = attend_rows((int)esize(l->dtype), D);
   p.rows = b.most * G <= 16 ? 16 : wide;
   p.pre_rows = b.n_tokens * G <= 16 ? 16 : wide;
   auto tiles = [&](int64_t n) { return ceil_div(n * G, p.rows); };
@@ -163,9 +163,16 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     // those for 5 x 32 fp32 questions of 128 dims over 3,000 keys), or two rounds
     // where the units by themselves nearly fill one (their ragged lengths then
     // even out)
-    resident = p.rows != 16 && D > (l->dtype == CR_DTYPE_F32 ? 64 : 128) ? 1 : 2;
+    resident = p.rows == 16 ? 2 : attend_resident((int)esize(l->dtype), D);
     const int round = 256 * resident;
     p.slots = (int)std::max<int64_t>(1, round / H);
+    // wide units that fill between half and two thirds of a round: three parts
+    // each in two rounds, where a tile takes long next to the merge (11 x 400
+    // tokens over 5,000 keys, 2 KV heads: bf16 of 256 dims 241 -> 207 us, fp32 of
+    // 192 1289 -> 909; bf16 of 128 dims lost 5 to 20 us)
+    if (p.rows != 16 && (D > 128 || l->dtype == CR_DTYPE_F32) && p.units * 2 > p.slots &&
+        p.units * 3 <= p.slots * 2)
+      p.slots *= 2;
     if (p.rows == 16 && p.units * 4 > p.slots * 3) p.slots = (int)std::max<int64_t>(1, 1024 / H);
     // a part has at least two tiles of 64 keys, or one for fp32, where a tile
     // takes eight times as long: 4 / 2 / 1 tiles took 39 / 28.9 / 24.4 us for 8 x

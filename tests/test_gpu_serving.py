@@ -162,6 +162,17 @@ def test_attend_options(name, kind):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", range(32, 257, 32))
+def test_every_head_dim(dtype, d):
+    """One token each and questions, split and whole."""
+    for q, lens in (([1] * 3, [40, 500, 129]), ([1, 40, 9], [30, 900, 200])):
+        b = Batch(dtype, 4, 2, d, 16, q, lens, seed=23)
+        _check(b)
+        p = np.array([j for _, j in b.slots()])
+        _check(b, softcap=10.0, slopes=[0.02, 0.0, 0.3, 0.01], lo=p - 70, hi=p + 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_values_of_hidden_keys_do_not_matter(dtype):
     """Infinities and NaN in keys that some rows of a tile see and others do
     not: a padded batch, documents of another query."""
