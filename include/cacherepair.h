@@ -527,7 +527,8 @@ typedef struct {
  *              that holds only what follows a preamble kept elsewhere takes
  *              slot + preamble length.
  * A new token without a slot (a negative one, one past the table, or one in no
- * block) is dropped; its query is rotated all the same.
+ * block) is dropped; its query is rotated all the same.  No two new tokens may
+ * have one slot (sequences that share the block it is in).
  * n_tokens == 0 returns CR_OK with nothing enqueued.
  * Errors: CR_ERR_NULL, CR_ERR_DIMS (dims, layer, heads, rope), CR_ERR_DTYPE,
  * CR_ERR_OFFSETS (query_offsets, n_seqs), CR_ERR_LAYOUT (strides, alignment,
@@ -552,7 +553,8 @@ CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t laye
  *              blocks (those of sequence 0's row of the table), whose keys are
  *              then read once for the whole batch where that saves more than
  *              the extra pass costs; at most max_blocks * block_size.  Changes
- *              no result but for rounding.  A sequence may be shorter.
+ *              no result but for rounding.  A sequence may be shorter, but
+ *              row 0 of the table lists all of these blocks.
  *  lse:        NULL, or device, [n_tokens][n_heads] fp32: the logarithm of the
  *              sum of exponentials of every row's scores.
  */

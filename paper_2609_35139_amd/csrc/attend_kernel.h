@@ -95,7 +95,7 @@ __device__ __forceinline__ int unit_tiles(const AttendArgs& a, const SeqTable& t
 }
 // Positions [lo, hi) that query i of a sequence (token t) sees in this pass.
 __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, int i, int t) {
-  int hi = min(a.hi ? a.hi[t] : n - nq + i + 1, n);
+  int hi = max(min(a.hi ? a.hi[t] : n - nq + i + 1, n), 0);   // (differences stay in 32 bits)
   int lo = a.lo ? max(a.lo[t], 0) : 0;
   if (a.shared) hi = min(hi, a.shared);
   else lo = max(lo, a.key_begin);
@@ -987,6 +987,7 @@ hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTa
   // rows of 18 parts 9.9 and 14.4
   const int rows = most_rows < a.rows ? most_rows : a.rows;
   const int64_t tiles = (int64_t)a.n_units * a.n_kv;
+  if (tiles * ((rows + 3) / 4) >= (int64_t)1 << 31) return hipErrorInvalidValue;
   if (tiles * rows <= 1024) {
     CR_LAUNCH((attend_merge_kernel<T, 1>), dim3((unsigned)(tiles * rows)), dim3(256), 0, s, a, pre,
               tab, rows);

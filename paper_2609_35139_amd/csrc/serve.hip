@@ -3,6 +3,7 @@
 #include "../../include/cacherepair.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "profile.h"
@@ -250,14 +251,16 @@ cr_status attend_impl(const void* kv, const cr_kv_layout* l, int layer, const cr
   a.hi = o.hi;
   const double scale = o.scale > 0.f ? o.scale : 1.0 / std::sqrt((double)l->head_dim);
   const double log2e = 1.4426950408889634;
-  a.scale_log2 = (float)(scale * log2e);
+  // (infinite factors would make NaN of a score or a distance of 0)
+  auto factor = [](double x) { return (float)std::clamp(x, -(double)FLT_MAX, (double)FLT_MAX); };
+  a.scale_log2 = factor(scale * log2e);
   if (o.softcap > 0.f) {
-    a.cap_log2 = (float)(o.softcap * log2e);
-    a.scale_over_cap = (float)(scale / o.softcap);
+    a.cap_log2 = factor(o.softcap * log2e);
+    a.scale_over_cap = factor(scale / o.softcap);
   }
   if (o.slopes) {
     a.bias = 1;
-    for (int h = 0; h < n_heads; ++h) a.slopes_log2[h] = (float)(o.slopes[h] * log2e);
+    for (int h = 0; h < n_heads; ++h) a.slopes_log2[h] = factor(o.slopes[h] * log2e);
   }
   SeqTable tab{};
   a.ragged = b.off != nullptr;

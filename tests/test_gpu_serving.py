@@ -197,6 +197,33 @@ def test_values_of_hidden_keys_do_not_matter(dtype):
     assert torch.isfinite(out).all() and (out[5] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q", [1, 40])
+def test_extreme_intervals(dtype, q):
+    """Limits at the ends of their type, in tiles that other rows see."""
+    b = Batch(dtype, 4, 2, 64, 16, [q] * 3, [400, 90, 700], seed=25)
+    least, most = -2 ** 31, 2 ** 31 - 1
+    t = np.arange(b.N)
+    p = np.array([j for _, j in b.slots()])
+    lo = np.choose(t % 5, [least, 0, most, p, -7])
+    hi = np.choose(t % 4, [most, least, p + 1, p + 9])
+    _check(b, lo=lo, hi=hi)
+
+
+def test_factors_beyond_their_type():
+    """Scales and slopes whose product with log2 e is no fp32 number: scores of
+    zero and keys at no distance stay what they are."""
+    b = Batch("bf16", 4, 2, 64, 16, [1, 1], [1, 200], seed=27)
+    cache, seqs, q, _, _ = b.cuda()
+    zero = torch.zeros_like(q.contiguous())
+    ref, _, tol, _ = attend_oracle(b, 0, q=zero.cpu())
+    for opt in (dict(scale=3.3e38), dict(softcap=3.3e38), dict(softcap=1e-40)):
+        assert_within(cache.attend(0, seqs, zero, **opt), ref, tol, str(opt))
+    out = cache.attend(0, seqs, zero, slopes=[3.3e38] * 4)      # itself alone
+    own = torch.stack([b.pool[0, 1, r[0], r[1]] for r in (b.row(0, 0), b.row(1, 199))])
+    assert torch.equal(out.cpu(), own.repeat_interleave(2, 1))
+
+
 def test_blocks_that_are_none_are_not_seen():
     b = Batch("bf16", 4, 2, 64, 4, [1, 30], [200, 90], seed=22)
     b.table[0, 3], b.table[0, 20], b.table[1, 2], b.table[1, 22] = -1, b.n_blocks, 1 << 30, -(1 << 31)
