@@ -18,7 +18,9 @@
  * write the result into a second cache (out of place).  cr_repair_pipelined
  * overlaps the host-to-device copy of one request with the repair of the
  * previous one.  cr_rotate_keys applies the target's rotary encoding (or its
- * inverse) to a cache's keys.
+ * inverse) to a cache's keys.  cr_append_kv and cr_attend answer over a
+ * repaired paged cache: a question's or a step's new keys and values are
+ * appended to it, and its queries attend to it.
  *
  * Conventions shared by every entry point:
  *  - Plain C: no C++ or torch types.  All sizes are element counts unless the
@@ -527,8 +529,7 @@ typedef struct {
  *              that holds only what follows a preamble kept elsewhere takes
  *              slot + preamble length.
  * A new token without a slot (a negative one, one past the table, or one in no
- * block) is dropped; its query is rotated all the same.  No two new tokens may
- * have one slot (sequences that share the block it is in).
+ * block) is dropped; its query is rotated all the same.
  * n_tokens == 0 returns CR_OK with nothing enqueued.
  * Errors: CR_ERR_NULL, CR_ERR_DIMS (dims, layer, heads, rope), CR_ERR_DTYPE,
  * CR_ERR_OFFSETS (query_offsets, n_seqs), CR_ERR_LAYOUT (strides, alignment,

@@ -42,6 +42,7 @@ class Sequences:
         n = kv_lens.shape[0]
         if block_table.shape[0] != n:
             raise ValueError("block_table needs one row per sequence")
+        self.cache = cache
         self.block_table, self.kv_lens = block_table, kv_lens        # keeps them alive
         self.struct, self._offsets = B.sequences_struct(
             n, kv_lens.data_ptr(), block_table.data_ptr(), block_table.shape[1], cache.block_size,
@@ -73,6 +74,11 @@ class PagedCache:
         [n_seqs], the new tokens included; query_offsets: host offsets of each
         sequence's new tokens, or None for one each."""
         return Sequences(self, block_table, kv_lens, query_offsets)
+
+    def _tokens(self, seqs: Sequences) -> int:
+        if seqs.cache is not self:
+            raise ValueError("the sequences were made by another cache")
+        return seqs.n_tokens
 
     def _rows(self, t: torch.Tensor, n: int, heads: int, name: str) -> B.cr_rows:
         if t.dtype is not self.pool.dtype or t.device != self.device:
@@ -116,7 +122,7 @@ class PagedCache:
         [n_tokens, n_heads, head_dim] (q_out None: a new tensor); rope: as
         Repairer.rotate_keys, or None; positions: device int32, or None for the
         slots.  Returns q_out."""
-        n = seqs.n_tokens
+        n = self._tokens(seqs)
         kr, vr = self._rows(k, n, self.n_kv_heads, "k"), self._rows(v, n, self.n_kv_heads, "v")
         pos = self._index(positions, n, "positions")
         rs, keep = (None, None) if rope is None else B.rope_struct(**rope)
@@ -141,6 +147,7 @@ class PagedCache:
 
     def workspace(self, seqs: Sequences, n_heads: int, shared_len: int = 0) -> torch.Tensor:
         """Device scratch for :meth:`attend` with these arguments."""
+        self._tokens(seqs)
         return torch.empty(max(self._workspace_bytes(seqs, n_heads, shared_len), 256),
                            dtype=torch.uint8, device=self.pool.device)
 
@@ -161,7 +168,7 @@ class PagedCache:
         [n_tokens, n_heads, head_dim] (None: a new tensor).  The options are
         those of cr_attend_options; slopes is a host sequence, lo, hi (int32)
         and lse (fp32 [n_tokens, n_heads]) are device tensors."""
-        n, heads = seqs.n_tokens, q.shape[1]
+        n, heads = self._tokens(seqs), q.shape[1]
         qr = self._rows(q, n, heads, "q")
         o = B.cr_attend_options(scale, softcap)
         if slopes is not None:

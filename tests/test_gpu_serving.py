@@ -364,6 +364,16 @@ def test_how_a_batch_is_split(name):
     _check(Batch("bf16", bs=16, seed=37, **c))
 
 
+def test_sequences_of_another_cache():
+    b = Batch("bf16", 4, 2, 64, 16, [1], [30], seed=41)
+    cache, seqs, q, k, v = b.cuda()
+    other = type(cache)(cache.pool[:, :, :1])
+    for call in (lambda: other.attend(0, seqs, q), lambda: other.append(0, seqs, k, v),
+                 lambda: other.workspace(seqs, 4)):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_two_calls_at_once():
     """Calls on two streams, each with a workspace of its own."""
     b = Batch("bf16", 8, 2, 128, 16, [1] * 6, [3000, 40, 900, 2500, 1, 700], seed=39)
