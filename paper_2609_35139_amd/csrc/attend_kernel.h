@@ -116,9 +116,10 @@ __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, 
 
 // ------------------------------------------------------------------- split
 // Item `it` of the split: unit, part, number of the unit's parts, tiles per
-// part, and the unit's first item (all uniform).  Every unit has at least one part; a part is
-// `chunk` tiles, the mean load of a.slots workgroups, so there are at most
-// a.slots + n_units items.  The same in every wave of every workgroup.
+// part, and the unit's first item (all uniform).  Every unit has at least one
+// part; a part is `chunk` tiles, the mean load of a.slots workgroups, so there
+// are at most a.slots + n_units items.  The same in every wave of every
+// workgroup.
 struct Item { int unit, part, parts, chunk, first; };
 __device__ __forceinline__ int div_up(int t, int chunk) {
   return (int)(((unsigned)t + (unsigned)chunk - 1u) / (unsigned)chunk);
