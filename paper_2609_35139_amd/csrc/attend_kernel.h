@@ -31,7 +31,7 @@
 //    merge) most is the chain of dependent reads and the second launch.
 //  - long prompts, wide units: bound by the waves' own instructions, the matrix
 //    pipes work 43% of the time; 8,192 queries over 12,288 keys, 32 heads of 128
-//    in 1,130 us, 970 TFLOP/s.
+//    in 1,090 us, 1,010 TFLOP/s.
 //  - in between (8 to 300 queries a sequence), the parts' partial results and
 //    uneven rounds cost as much as the products; see attend_plan.
 #pragma once
@@ -640,6 +640,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       }
 #pragma unroll
       for (int n = 0; n < NQ; ++n) l[n] += ts[n];
+      // this product ahead of the other wave's instructions, which then weighs its
+      // scores under it: 1,117 / 1,091 us for 8,192 queries over 12,288 keys, fp32
+      // and wide heads 3 to 8% (around the scores' product instead it costs 2%)
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int f = 0; f < PF; ++f)
 #pragma unroll
@@ -649,6 +653,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
           for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
         }
+      __builtin_amdgcn_s_setprio(0);
     };
 
     // Any other KS keys: keys that a row does not see, keys past the segment,
