@@ -389,6 +389,18 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   x.nq = __builtin_amdgcn_readfirstlane(x.nq);
   const int row0 = x.tile * C::ROWS, n_rows = min(C::ROWS, x.nq * a.group - row0);
   const int seq_n = a.shared ? 0 : seq_len(a.seqs, x.s);
+  // this lane's rows, on their way from here
+  frag qf[NQ][QF];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = (rg * NQ + n) * 16 + c16;
+    const int i = (row0 + min(r, n_rows - 1)) / a.group;
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(x.tok0 + i) * a.q_token +
+                  (int64_t)(head * a.group + row0 + min(r, n_rows - 1) - i * a.group) * a.q_head;
+#pragma unroll
+    for (int kk = 0; kk < QF; ++kk)
+      qf[n][kk] = r < n_rows ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
+  }
   // position and interval of every row of the unit, and the keys that any row
   // sees (a row past the last one sees everything: it masks nothing)
   if (tid < C::ROWS) {
@@ -430,20 +442,13 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   kb = __builtin_amdgcn_readfirstlane(kb);
   ke = __builtin_amdgcn_readfirstlane(ke);
 
-  // ---- this lane's rows
-  frag qf[NQ][QF];
-  int wlo = INT_MIN, whi = INT_MAX;      // window that every row of the wave sees
+  // ---- the window that every row of the wave sees
+  int wlo = INT_MIN, whi = INT_MAX;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int r = (rg * NQ + n) * 16 + c16;
     wlo = max(wlo, info[r].x);
     whi = min(whi, info[r].y);
-    const int i = (row0 + min(r, n_rows - 1)) / a.group;
-    const T* qp = static_cast<const T*>(a.q) + (int64_t)(x.tok0 + i) * a.q_token +
-                  (int64_t)(head * a.group + row0 + min(r, n_rows - 1) - i * a.group) * a.q_head;
-#pragma unroll
-    for (int kk = 0; kk < QF; ++kk)
-      qf[n][kk] = r < n_rows ? load_frag<T, frag>(qp + kk * KSTEP + g * KPL) : frag{};
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
@@ -452,12 +457,6 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   }
   wlo = __builtin_amdgcn_readfirstlane(wlo);
   whi = __builtin_amdgcn_readfirstlane(whi);
-  // (waited for here: a load still pending at the loops' entry would have every
-  // turn of them wait for all transfers in flight)
-#pragma unroll
-  for (int n = 0; n < NQ; ++n)
-#pragma unroll
-    for (int kk = 0; kk < QF; ++kk) asm volatile("" : "+v"(qf[n][kk]));
   const bool idle = rg * NQ * 16 >= n_rows;     // no row: the wave only stages
 
   f32x4 oacc[NQ][DT];
@@ -501,6 +500,12 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
         none[kListPages / 32] = 1;
       }
     }
+    // (the rows are waited for here: a load still pending at the loops' entry would
+    // have every turn of them wait for all transfers in flight)
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int kk = 0; kk < QF; ++kk) asm volatile("" : "+v"(qf[n][kk]));
     __syncthreads();
     const bool seg_bad = __builtin_amdgcn_readfirstlane(none[kListPages / 32]) != 0;
     const int tiles = (seg_end - seg + KT - 1) / KT;
