@@ -442,7 +442,7 @@ def sequences_struct(n_seqs, kv_lens, block_table, max_blocks, block_size, n_blo
     off = None
     q = cr_sequences()
     if query_offsets is not None:
-        off = np.ascontiguousarray(query_offsets, dtype=np.int32)
+        off = np.array(query_offsets, dtype=np.int32, order="C")   # (a copy: the caller's may change)
         if off.shape != (n_seqs + 1,):
             raise ValueError("query_offsets needs one entry more than there are sequences")
         q.query_offsets = off.ctypes.data_as(POINTER(c_int32))

@@ -185,8 +185,9 @@ class PagedCache:
                                 "cache's device")
             o.lse = lse.data_ptr()
         need = self._workspace_bytes(seqs, heads, shared_len)
-        if workspace is not None and workspace.device != self.device:
-            raise ValueError("workspace must be on the cache's device")
+        if workspace is not None and (workspace.device != self.device or
+                                      not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous tensor on the cache's device")
         result = out
 
         def call(handle):

@@ -374,6 +374,16 @@ def test_sequences_of_another_cache():
             call()
 
 
+def test_workspace_that_is_no_memory_of_its_size():
+    b = Batch("bf16", 4, 2, 64, 16, [1], [900], seed=43)
+    cache, seqs, q, _, _ = b.cuda()
+    need = cache.workspace(seqs, 4).numel()
+    for ws in (torch.empty(1, dtype=torch.uint8, device="cuda").expand(need),
+               torch.empty(need, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            cache.attend(0, seqs, q, workspace=ws)
+
+
 def test_two_calls_at_once():
     """Calls on two streams, each with a workspace of its own."""
     b = Batch("bf16", 8, 2, 128, 16, [1] * 6, [3000, 40, 900, 2500, 1, 700], seed=39)

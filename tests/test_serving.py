@@ -152,6 +152,13 @@ def test_a_batch_without_tokens_is_a_no_op():
     B.cr_attend(0x10000, lay, 0, q, empty, B.cr_rows(0x10000, 0, 0), 4, None, None, 0)
 
 
+def test_offsets_are_the_batch_s_own():
+    off = np.array([0, 2, 5], dtype=np.int32)
+    q, keep = B.sequences_struct(2, 0x1000, 0x2000, 4, 16, 8, 16 * 128, off)
+    off[:] = 99
+    assert [q.query_offsets[i] for i in range(3)] == [0, 2, 5] == keep.tolist()
+
+
 def test_workspace_does_not_grow_with_the_table():
     """The split is bounded by the chip, not by the longest context there can be."""
     sizes = []
