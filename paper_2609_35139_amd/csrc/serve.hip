@@ -156,14 +156,18 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   }
   Arena a;
   if (b.off && q->n_seqs > kTableSeqs) p.tables = a.take(2 * ((uint64_t)q->n_seqs + 1) * 4);
-  // split the keys unless the units fill the chip by themselves
+  // split the keys unless the units fill the chip by themselves (single tokens
+  // over 64 to 8,000 keys, 8 KV heads, split / whole: 128 sequences 176 / 202 us,
+  // 256 342 / 356; 512 over up to 2,000 keys 283 / 234; wide units: 64 x 32 tokens
+  // over 1,000 keys 74 / 65)
   int resident = 2;
-  if (p.units * H < (p.rows == 16 ? 8192 : 512)) {
+  bool two_rounds = false;
+  if (p.units * H < (p.rows == 16 ? 4096 : 512)) {
     // one round of the workgroups that a CU holds (two, but one where a wave
     // takes more than 256 registers: 52.6 / 45.9 us with parts for 512 / 256 of
     // those for 5 x 32 fp32 questions of 128 dims over 3,000 keys), or two rounds
     // where the units by themselves nearly fill one (their ragged lengths then
-    // even out)
+    // even out: 64 of the sequences above 94 / 101 us with / without)
     resident = p.rows == 16 ? 2 : attend_resident((int)esize(l->dtype), D);
     const int round = 256 * resident;
     p.slots = (int)std::max<int64_t>(1, round / H);
@@ -174,14 +178,21 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     if (p.rows != 16 && (D > 128 || l->dtype == CR_DTYPE_F32) && p.units * 2 > p.slots &&
         p.units * 3 <= p.slots * 2)
       p.slots *= 2;
-    if (p.rows == 16 && p.units * 4 > p.slots * 3) p.slots = (int)std::max<int64_t>(1, 1024 / H);
+    two_rounds = p.rows == 16 && p.units * 4 > p.slots * 3;
+    if (two_rounds) p.slots = (int)std::max<int64_t>(1, 1024 / H);
     // a part has at least two tiles of 64 keys, or one for fp32, where a tile
     // takes eight times as long: 4 / 2 / 1 tiles took 39 / 28.9 / 24.4 us for 8 x
     // 161 fp32 questions over 769 keys, 42 / 38.4 / 38.5 us for bf16 documents,
     // and one took 44.0 instead of 40.4 us for 9 bf16 sequences over 1177 keys
     p.min_tiles = l->dtype == CR_DTYPE_F32 ? 1 : 2;
-    // one part holds all keys there can be
-    if ((int64_t)q->max_blocks * q->block_size <= 128 * p.min_tiles) p.slots = 0;
+    // so few keys as the table can hold are not worth a merge: 128 KB of a head's
+    // for single tokens (64 KB for fp32), 512 keys at most (split / whole: 400 keys
+    // of 64 dims 13.5 / 9.6 us, 500 of 128 16.9 / 13.7, 400 of 256 16.8 / 20.4; fp32
+    // of 128 dims 100 keys 13.5 / 13.5, 200 15.5 / 18.4)
+    const int64_t row = D * (int64_t)esize(l->dtype), few = l->dtype == CR_DTYPE_F32 ? 1 << 16 : 1 << 17;
+    if ((int64_t)q->max_blocks * q->block_size <=
+        (p.rows == 16 ? std::min<int64_t>(512, few / row) : 128 * p.min_tiles))
+      p.slots = 0;
   }
   if (shared_pays(l, b, G, p, shared)) {
     p.pre_units = ceil_div(b.n_tokens * G, p.pre_rows);
@@ -190,7 +201,14 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
     p.split_tiles = (int)std::max<int64_t>(2, ceil_div(key_tiles, want));
     p.splits = (int)ceil_div(key_tiles, p.split_tiles);
   }
-  // No split where it gains less than the merge takes: 2 us and 2.4 us for every
+  // Nor single tokens of much the same lengths that fill the chip, or a unit of
+  // up to two tiles more than a part (64 tokens, 8 KV heads, split / whole: 200
+  // keys 29 / 24 us, 400 35 / 30, 1,000 57 / 53; 100 tokens over 4,000 378 / 304).
+  if (p.slots && !p.pre_units && p.rows == 16 && l->dtype == CR_DTYPE_BF16) {
+    p.split_cost = two_rounds ? std::max(1.f, 1.5f * (float)p.slots / (float)p.units) : 1.f;
+    p.join_cost = 2.f;
+  }
+  // No split of wide units where it gains less than the merge takes: 2 us and 2.4 us for every
   // million sums, at 2 us for a wide bf16 tile of 128 dims.  A workgroup that
   // has its CU to itself takes two thirds of the time per tile, and with more
   // units than fit one round a split pays for very uneven lengths alone.  20
