@@ -62,6 +62,20 @@ def test_append_copies_without_rope_and_in_place():
     assert torch.equal(same, ref)
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,d", [("bf16", 14, 3, 128), ("f32", 5, 1, 256),
+                                                    ("bf16", 24, 4, 96)])
+def test_append_of_many_tokens(dtype, heads, kv_heads, d):
+    """Enough tokens for several heads to a thread, heads that do not divide
+    evenly among them; queries rotated where they lie."""
+    b = Batch(dtype, heads, kv_heads, d, 16, [700, 0, 1, 41], [900, 5, 300, 41], seed=19)
+    cache, seqs, q, k, v = b.cuda()
+    pool, qo, ep, eq = append_oracle(b, 0)
+    got = cache.append(0, seqs, k, v, q=q, q_out=q, rope=dict(theta=1e6))
+    assert got.data_ptr() == q.data_ptr()
+    assert_within(cache.pool, pool, ep, "cache")
+    assert_within(got, qo, eq, "queries")
+
+
 def test_append_frequency_table_and_many_sequences():
     """300 sequences of zero to two tokens (more than one launch's table), the
     model's own frequencies."""
@@ -347,7 +361,8 @@ def test_shared_prefix_masked_and_replayed():
         assert torch.equal(out, cache.attend(0, seqs, q, **dev)), i
 
 
-@pytest.mark.parametrize("name", ["plan-of-200", "tokens-unsplit", "questions-unsplit", "even", "uneven"])
+@pytest.mark.parametrize("name", ["plan-of-200", "tokens-unsplit", "questions-unsplit", "even",
+                                  "uneven", "even-tokens", "uneven-tokens", "short-table"])
 def test_how_a_batch_is_split(name):
     """Batches whose units are planned beyond one wave's worth, are too many to
     split, or are split or left whole by the device's rule."""
@@ -360,6 +375,9 @@ def test_how_a_batch_is_split(name):
                                   lens=[17 + 11 * s for s in range(33)]),
         "even": dict(heads=16, kv_heads=4, d=128, q=[32] * 20, lens=[332] * 20),
         "uneven": dict(heads=16, kv_heads=4, d=128, q=[32, 9, 17], lens=[4000, 32, 600]),
+        "even-tokens": dict(heads=8, kv_heads=8, d=64, q=[1] * 64, lens=[700 - s for s in range(64)]),
+        "uneven-tokens": dict(heads=8, kv_heads=8, d=64, q=[1] * 64, lens=[3000] + [100] * 63),
+        "short-table": dict(heads=4, kv_heads=2, d=64, q=[1] * 3, lens=[500, 512, 1]),
     }[name]
     _check(Batch("bf16", bs=16, seed=37, **c))
 
