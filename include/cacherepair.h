@@ -489,9 +489,11 @@ CR_API cr_status cr_repair_static(void* kv, const cr_kv_layout* layout,
  *                 undefined).  max_blocks * block_size < 2^31 - 256.
  *  block_size, n_blocks, stride_block: as cr_kv_pages; rows of a block (the
  *                 layout's stride_token) less than 4 GiB apart.
- * The kernels never leave the cache: a length counts as at least 0 and at most
- * max_blocks * block_size, and a block id outside [0, n_blocks) is no block
- * (its keys are not seen, tokens appended to it are dropped).
+ * The kernels never leave the cache: a length below 0 counts as 0, and a block
+ * id outside [0, n_blocks) is no block (its keys are not seen, tokens appended
+ * to it are dropped).  A length may pass the table, max_blocks * block_size:
+ * new tokens whose slots lie past the table are dropped by cr_append_kv, and
+ * cr_attend takes such a length as the table's own.
  *
  * cr_rows: a [n_tokens][heads][head_dim] operand in device memory, storage
  * dtype, dim stride 1; strides in elements, multiples of 8, not negative; base

@@ -53,10 +53,9 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, KeyRope kr, A
     i = t - b.offs[lo];
   }
   const PagedSeqs& ps = a.seqs;
-  const int n = min(max(ps.lens[s], 0), ps.max_len);
-  const int slot = n - nq + i;
+  const int slot = max(ps.lens[s], 0) - nq + i;
   int64_t row = -1;                      // element offset of the token's row, -1: dropped
-  if (slot >= 0) {
+  if (slot >= 0 && slot < ps.max_len) {
     const int id = ps.table[(int64_t)s * ps.max_blocks + (slot >> ps.shift)];
     if (id >= 0 && id < ps.n_blocks)
       row = (int64_t)id * ps.block + (int64_t)(slot & ((1 << ps.shift) - 1)) * ps.token;

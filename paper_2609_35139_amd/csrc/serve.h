@@ -11,8 +11,9 @@ constexpr int kMaxQueryHeads = 256;
 
 // One layer of a paged cache and the sequences in it.  Token t of sequence s
 // lies in block table[s * max_blocks + (t >> shift)], row t & (2^shift - 1).
-// lens and table are device memory that only the kernels read: a length is
-// clamped to [0, max_len] and a block outside [0, n_blocks) is no block.
+// lens and table are device memory that only the kernels read: a length below 0
+// counts as 0, no slot from max_len on exists, and a block outside [0, n_blocks)
+// is no block.
 struct PagedSeqs {
   int64_t token, head, block;       // strides in elements
   int shift, n_blocks, max_blocks, max_len, n_seqs;

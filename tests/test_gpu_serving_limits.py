@@ -1,0 +1,89 @@
+"""cr_append_kv and cr_attend on the GPU at the limits of their arguments,
+against their definitions in 64 bits (tests/serving_helpers.py)."""
+import pytest
+import torch
+
+from serving_helpers import Batch, append_oracle, assert_within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_35139_amd import binding
+    binding.load()
+
+
+class Outgrown(Batch):
+    """A batch whose lengths have grown by `more` past what its table was made
+    for: slots count from the true length, and those past the table are none."""
+
+    def __init__(self, *args, more, **kwargs):
+        super().__init__(*args, **kwargs)
+        self.lens = [min(n + m, 2 ** 31 - 1) for n, m in zip(self.lens, more)]
+
+    def slots(self):
+        return [(s, max(n, 0) - nq + i)
+                for s, (nq, n) in enumerate(zip(self.q, self.lens)) for i in range(nq)]
+
+
+# ----------------------------------------------- lengths past the block table
+PAST = {
+    # the last row, the first one past it, tokens on both sides, all past it
+    "tokens": dict(dtype="bf16", heads=4, kv_heads=2, d=64, bs=16, q=[1] * 4, lens=[32, 32, 20, 31],
+                   more=[0, 1, 12, 2]),
+    "questions": dict(dtype="bf16", heads=4, kv_heads=2, d=64, bs=4, q=[6, 6, 3, 9],
+                      lens=[48, 48, 48, 40], more=[3, 0, 3, 12]),
+    "f32": dict(dtype="f32", heads=3, kv_heads=1, d=96, bs=1, q=[40, 5, 2], lens=[50, 50, 9],
+                more=[7, 50, 2]),
+    "far": dict(dtype="bf16", heads=2, kv_heads=2, d=64, bs=16, q=[1, 4, 2], lens=[64, 64, 60],
+                more=[1 << 30, 1 << 31, 5]),
+}
+
+
+def _past(name):
+    c = dict(PAST[name])
+    return Outgrown(c.pop("dtype"), c.pop("heads"), c.pop("kv_heads"), c.pop("d"), c.pop("bs"),
+                    c.pop("q"), c.pop("lens"), seed=71 + len(name), **c)
+
+
+@pytest.mark.parametrize("name", PAST)
+def test_append_drops_tokens_past_the_table(name):
+    """Such a token leaves every row as it was; the others, and all queries,
+    take the positions that the length gives them."""
+    b = _past(name)
+    cache, seqs, q, k, v = b.cuda()
+    got = cache.append(0, seqs, k, v, q=q, rope=dict(theta=1e6))
+    pool, qo, ep, eq = append_oracle(b, 0)
+    # a position's angle is off by four roundings in 64 bits on either side
+    pos = torch.tensor([j for _, j in b.slots()], dtype=torch.float64)[:, None, None]
+    half = b.d // 2
+    size = (b.qh[..., :half].double().abs() + b.qh[..., half:].double().abs()).repeat(1, 1, 2)
+    assert_within(cache.pool, pool, ep, "cache")        # rows of no new token: exactly
+    assert_within(got, qo, eq + 2.0 ** -50 * pos.abs() * size, "queries")
+
+
+def test_append_replayed_past_the_table():
+    """A captured append whose lengths outgrow the table while it is replayed."""
+    b = Batch("bf16", 4, 2, 64, 4, [1, 1], [6, 3], seed=73, table_slack=0)
+    cache, _, q, k, v = b.cuda()
+    lens = torch.tensor(b.lens, dtype=torch.int32).cuda()
+    seqs = cache.sequences(b.table.cuda(), lens)
+    out = torch.empty_like(q)
+    step = lambda: cache.append(0, seqs, k, v, q=q, q_out=out, rope=dict(theta=1e4))
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    want = Outgrown("bf16", 4, 2, 64, 4, [1, 1], [6, 3], seed=73, more=[0, 0])
+    for i in range(6):
+        want.lens = [6 + i, 3 + i]
+        want.pool = cache.pool.cpu()
+        g.replay()
+        torch.cuda.synchronize()
+        pool, qo, ep, eq = append_oracle(want, 0, theta=1e4)
+        assert_within(cache.pool, pool, ep, f"cache {i}")
+        assert_within(out, qo, eq, f"queries {i}")
+        lens.add_(1)
