@@ -492,8 +492,9 @@ CR_API cr_status cr_repair_static(void* kv, const cr_kv_layout* layout,
  * The kernels never leave the cache: a length below 0 counts as 0, and a block
  * id outside [0, n_blocks) is no block (its keys are not seen, tokens appended
  * to it are dropped).  A length may pass the table, max_blocks * block_size:
- * new tokens whose slots lie past the table are dropped by cr_append_kv, and
- * cr_attend takes such a length as the table's own.
+ * tokens keep the slots that it gives them, there are no keys in slots past the
+ * table, and new tokens with such a slot are dropped (their queries see what the
+ * table holds).
  *
  * cr_rows: a [n_tokens][heads][head_dim] operand in device memory, storage
  * dtype, dim stride 1; strides in elements, multiples of 8, not negative; base
@@ -550,7 +551,7 @@ CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t laye
  *              the score of the query in slot p and the key in slot j.
  *  lo, hi:     device, n_tokens int32 each, or NULL: query t sees the keys in
  *              slots [lo[t], hi[t]) of its sequence (within the sequence's
- *              length).  lo NULL = 0; hi NULL = causal, up to the query's own
+ *              length and the table).  lo NULL = 0; hi NULL = causal, up to the query's own
  *              slot.  Documents, a bidirectional prefix, windows.
  *  shared_len: the first shared_len slots of every sequence are in the same
  *              blocks (those of sequence 0's row of the table), whose keys are

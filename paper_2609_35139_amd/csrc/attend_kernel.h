@@ -48,10 +48,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostSum = 16777216.f;   // 2^24: a lane's share of a tile's probabilities
 
 // ------------------------------------------------------------ units and rows
-__device__ __forceinline__ int seq_len(const PagedSeqs& p, int s) {
-  const int n = p.lens[s];
-  return min(max(n, 0), p.max_len);
-}
+// A sequence's length: its queries' slots count from it, but keys lie only in
+// slots below max_len.
+__device__ __forceinline__ int seq_len(const PagedSeqs& p, int s) { return max(p.lens[s], 0); }
 // The offsets of a ragged batch.
 struct Offsets {
   const AttendArgs& a;
@@ -98,16 +97,17 @@ __device__ __forceinline__ Unit unit_of(const AttendArgs& a, const SeqTable& tab
 // One past the last position that a unit's queries may see.
 __device__ __forceinline__ int unit_end(const AttendArgs& a, const Unit& x) {
   const int n = seq_len(a.seqs, x.s);
-  if (a.hi) return n;
+  if (a.hi) return min(n, a.seqs.max_len);
   const int last = min(((x.tile + 1) * a.rows - 1) / a.group, x.nq - 1);
-  return n - (x.nq - 1 - last);
+  return min(n - (x.nq - 1 - last), a.seqs.max_len);
 }
 __device__ __forceinline__ int unit_tiles(const AttendArgs& a, const SeqTable& tab, int u) {
   return (max(unit_end(a, unit_of(a, tab, u)) - a.key_begin, 0) + kPlanTile - 1) / kPlanTile;
 }
 // Positions [lo, hi) that query i of a sequence (token t) sees in this pass.
 __device__ __forceinline__ int2 interval_of(const AttendArgs& a, int n, int nq, int i, int t) {
-  int hi = max(min(a.hi ? a.hi[t] : n - nq + i + 1, n), 0);   // (differences stay in 32 bits)
+  const int most = min(n, a.seqs.max_len);
+  int hi = max(min(a.hi ? a.hi[t] : n - nq + i + 1, most), 0);   // (differences stay in 32 bits)
   int lo = a.lo ? max(a.lo[t], 0) : 0;
   if (a.shared) hi = min(hi, a.shared);
   else lo = max(lo, a.key_begin);

@@ -1,9 +1,10 @@
 """cr_append_kv and cr_attend on the GPU at the limits of their arguments,
 against their definitions in 64 bits (tests/serving_helpers.py)."""
+import numpy as np
 import pytest
 import torch
 
-from serving_helpers import Batch, append_oracle, assert_within
+from serving_helpers import Batch, append_oracle, assert_within, attend_oracle
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +88,44 @@ def test_append_replayed_past_the_table():
         assert_within(cache.pool, pool, ep, f"cache {i}")
         assert_within(out, qo, eq, f"queries {i}")
         lens.add_(1)
+
+
+# (a bias of a billion positions would leave no score its bits)
+@pytest.mark.parametrize("name,bias", [(n, False) for n in PAST] +
+                         [(n, True) for n in PAST if n != "far"])
+def test_attend_past_the_table(name, bias):
+    """Queries keep the slots that the length gives them: those in the table
+    see up to their own key, those past it everything that the table holds."""
+    b = _past(name)
+    opt = dict(slopes=[0.05 * (h + 1) for h in range(b.heads)]) if bias else {}
+    cache, seqs, q, _, _ = b.cuda()
+    lse = torch.empty(b.N, b.heads, device="cuda")
+    out = cache.attend(0, seqs, q, lse=lse, **opt)
+    ref, rl, tol, ltol = attend_oracle(b, 0, **opt)
+    assert_within(out, ref, tol, "out")
+    assert_within(lse, rl, ltol, "lse")
+
+
+@pytest.mark.parametrize("q", [[1] * 120, [5, 9, 0, 7] * 30])
+def test_shared_prefix_past_the_table(q):
+    """The same with the documents read once, and with limits of the caller's."""
+    from paper_2609_35139_amd import binding as B
+    lens = [3000 + 20 + s % 40 for s in range(len(q))]
+    b = Outgrown("bf16", 16, 8, 64, 16, q, lens, seed=79, shared=3008,
+                 more=[s % 3 * 30 for s in range(len(q))])
+    cache, seqs, qh, _, _ = b.cuda()
+    B.cr_profile_enable(8)
+    try:
+        out = cache.attend(0, seqs, qh, shared_len=3000)
+        assert "attend_shared" in {r["name"] for r in B.cr_profile_read()}
+    finally:
+        B.cr_profile_enable(0)
+    tell = list(range(0, b.N, 5))
+    ref, _, tol, _ = attend_oracle(b, 0, tokens=tell)
+    assert_within(out[tell], ref[tell], tol[tell], "shared")
+    p = np.array([j for _, j in b.slots()])
+    lo, hi = p - 90, p + 1
+    out = cache.attend(0, seqs, qh, shared_len=3000, lo=torch.tensor(lo, dtype=torch.int32).cuda(),
+                       hi=torch.tensor(hi, dtype=torch.int32).cuda())
+    ref, _, tol, _ = attend_oracle(b, 0, lo=lo, hi=hi, tokens=tell)
+    assert_within(out[tell], ref[tell], tol[tell], "windows")
