@@ -200,8 +200,25 @@ __device__ __forceinline__ int row_offset(int row, int chunk) {
   return row * RB + ((chunk ^ row_swizzle<RB>(row)) << 4);
 }
 
-// tanh(x): for bf16 through one exponential and a reciprocal (absolute error
-// about 2^-22, far below a bf16 score's own), for fp32 the library's.
+// A capped score is cap * tanh(u), u = score / cap.  For |u| <= 1/2 that is
+// score * tanh(u) / u, the quotient a polynomial in u^2: the error is relative to
+// the score however large the cap (2^-23; a cap times a tanh that is off by 2^-23
+// would be off by 0.1 for a cap of a million).  tanh(u) / u - 1 = u^2 (c_0 + c_1
+// u^2 + ...), a least-squares fit reweighted towards the largest errors until
+// they level out (Lawson's iteration), relative error 2^-26.
+constexpr float kCapSmall = 0.5f;
+constexpr float kCapPoly[4] = {-0.333331435918808f, 0.13325878977775574f, -0.05304549261927605f,
+                               0.01724149100482464f};
+__device__ __forceinline__ float tanh_over(float u) {
+  const float w = u * u;
+  float p = kCapPoly[3];
+#pragma unroll
+  for (int k = 2; k >= 0; --k) p = __builtin_fmaf(p, w, kCapPoly[k]);
+  return __builtin_fmaf(p, w, 1.f);
+}
+// tanh(x) for |x| > 1/2: for bf16 through one exponential and a reciprocal
+// (relative error up to 2^-20, as large as that of a score's fp32 sum over 16
+// dims), for fp32 the library's.
 template <typename T> __device__ __forceinline__ float tanh_of(float x);
 template <> __device__ __forceinline__ float tanh_of<float>(float x) { return tanhf(x); }
 template <> __device__ __forceinline__ float tanh_of<bf16>(float x) {
@@ -540,10 +557,32 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
     // just scaled
     auto transform = [&](f32x4 (&s)[ST], int n, int k0, int lane) {
       if (a.cap_log2 > 0.f) {
+        // few scores are past half the cap in earnest: the second form is formed
+        // only where a wave has one (the second for every score / as here: 4,096
+        // queries over 8,192 keys, cap 30, 700 / 689 us; cap 2, most scores past
+        // it, 735 / 915)
+        f32x4 y[ST];
+        float top = 0.f;
 #pragma unroll
         for (int t = 0; t < ST; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][e] = a.cap_log2 * tanh_of<T>(s[t][e] * a.scale_over_cap);
+          for (int e = 0; e < 4; ++e) {
+            const float u = s[t][e] * a.scale_over_cap;
+            y[t][e] = s[t][e] * a.scale_log2 * tanh_over(u);
+            top = fmaxf(top, fabsf(u));
+          }
+        if (__any(top > kCapSmall)) {
+#pragma unroll
+          for (int t = 0; t < ST; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float u = s[t][e] * a.scale_over_cap;
+              const float z = a.cap_log2 * tanh_of<T>(u);
+              y[t][e] = fabsf(u) > kCapSmall ? z : y[t][e];
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < ST; ++t) s[t] = y[t];
       } else {
 #pragma unroll
         for (int t = 0; t < ST; ++t) s[t] *= a.scale_log2;

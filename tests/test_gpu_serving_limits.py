@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from serving_helpers import Batch, append_oracle, assert_within, attend_oracle
+from serving_helpers import HALF, Batch, append_oracle, assert_within, attend_oracle
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +129,45 @@ def test_shared_prefix_past_the_table(q):
                        hi=torch.tensor(hi, dtype=torch.int32).cuda())
     ref, _, tol, _ = attend_oracle(b, 0, lo=lo, hi=hi, tokens=tell)
     assert_within(out[tell], ref[tell], tol[tell], "windows")
+
+
+# ------------------------------------------------------------------ score caps
+def _capped(b, cap):
+    """(out, lse, bounds) of causal attention with capped scores, in 64 bits.
+    A cap leaves its score's error no larger, and adds one that is relative to
+    the capped score, whatever the cap: 2^-20."""
+    out = torch.zeros(b.N, b.heads, b.d, dtype=torch.float64)
+    lse = torch.zeros(b.N, b.heads, dtype=torch.float64)
+    tol, ltol = torch.zeros_like(out), torch.zeros_like(lse)
+    half = HALF[b.dtype]
+    pool, q = b.pool[0].double(), b.qh.double()
+    for t, (s, p) in enumerate(b.slots()):
+        at = torch.tensor([b.row(s, j) for j in range(p + 1)])
+        for h in range(b.heads):
+            k, v = (pool[c, at[:, 0], at[:, 1], h * b.kv_heads // b.heads] for c in (0, 1))
+            x = (k @ q[t, h]) / b.d ** 0.5
+            e = (k.abs() @ q[t, h].abs()).max() / b.d ** 0.5 * (b.d + 8) * 2.0 ** -24
+            x = cap * torch.tanh(x / cap)
+            e = float(e + 2.0 ** -20 * x.abs().max() + 2.0 ** -21 * (1 + x.abs().max()))
+            w = torch.softmax(x, 0)
+            out[t, h], lse[t, h] = w @ v, torch.logsumexp(x, 0)
+            # (the terms of serving_helpers.attend_oracle)
+            ltol[t, h] = 2 * e + 2.0 ** -16 + (half if b.dtype == "bf16" else 0.0)
+            tol[t, h] = ltol[t, h] * (w @ v.abs() + out[t, h].abs()) + half * out[t, h].abs()
+    return out, lse, tol, ltol
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.7, 6.0, 30.0, 1e3, 1e5, 1e8, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_caps_of_every_size(dtype, cap):
+    """Scores from far below the cap to far above it; a large cap changes
+    nothing.  Single tokens, and questions in whole and in masked tiles."""
+    for q, lens in (([1] * 3, [300, 70, 1]), ([40, 7], [400, 90])):
+        b = Batch(dtype, 4, 2, 64, 16, q, lens, seed=83)
+        b.pool[:, 0] *= 3                    # scores of about 3
+        cache, seqs, qh, _, _ = b.cuda()
+        lse = torch.empty(b.N, b.heads, device="cuda")
+        out = cache.attend(0, seqs, qh, softcap=cap, lse=lse)
+        ref, rl, tol, ltol = _capped(b, cap)
+        assert_within(out, ref, tol, f"out {q}")
+        assert_within(lse, rl, ltol, f"lse {q}")
