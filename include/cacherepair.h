@@ -534,9 +534,10 @@ typedef struct {
  * A new token without a slot (a negative one, one past the table, or one in no
  * block) is dropped; its query is rotated all the same.
  * n_tokens == 0 returns CR_OK with nothing enqueued.
- * Errors: CR_ERR_NULL, CR_ERR_DIMS (dims, layer, heads, rope), CR_ERR_DTYPE,
- * CR_ERR_OFFSETS (query_offsets, n_seqs), CR_ERR_LAYOUT (strides, alignment,
- * block geometry), CR_ERR_DEVICE before any enqueue; CR_ERR_LAUNCH.
+ * Errors: CR_ERR_NULL, CR_ERR_DIMS (dims, layer, heads, rope, a batch that takes
+ * 2^32 threads), CR_ERR_DTYPE, CR_ERR_OFFSETS (query_offsets, n_seqs),
+ * CR_ERR_LAYOUT (strides, alignment, block geometry), CR_ERR_DEVICE before any
+ * enqueue; CR_ERR_LAUNCH.
  */
 CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t layer,
                        const cr_sequences* seqs, const cr_rows* k, const cr_rows* v,

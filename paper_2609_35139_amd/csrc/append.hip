@@ -128,14 +128,10 @@ hipError_t append_kv(const AppendArgs& a, const KeyRope& kr_in, const int32_t* o
   for (int i = 0; i < kr.half; ++i) kr.f[i] = kr.f[i] / (2.0 * M_PI);
   const int heads = a.n_kv + (a.q ? a.n_heads : 0);
   auto launch = [&](const AppendBatch& b, int tokens) {
-    // one head per thread while that leaves a CU one workgroup at most, else four
-    // that share their angles (one / two / four / eight heads: 64 tokens of 18
-    // heads 5.7 / 6.3 / 6.8 / 10.0 us, 11,243 of 40 77 / 63 / 57 / 55)
-    const int hpt = (int64_t)tokens * heads * (a.head_dim / 16) <= 256 * 256 ? 1 : 4;
-    const int64_t per_token = std::max((int64_t)((heads + hpt - 1) / hpt) * (a.head_dim / 16),
-                                       (int64_t)a.n_kv * (a.head_dim / 8));
-    const dim3 grid((unsigned)((tokens * per_token + 255) / 256), 2);
-    if (hpt == 1) {
+    const int64_t groups = append_groups(tokens, a.n_kv, heads, a.head_dim);
+    if (!fits_launch(groups, 256)) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)groups, 2);
+    if (append_heads(tokens, heads, a.head_dim) == 1) {
       CR_LAUNCH((append_kernel<T, 1>), grid, dim3(256), 0, s, a, kr, b);
     } else {
       CR_LAUNCH((append_kernel<T, 4>), grid, dim3(256), 0, s, a, kr, b);

@@ -1042,25 +1042,18 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendArgs a, SharedP
 template <typename T>
 hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTable& tab,
                         int most_rows, hipStream_t s) {
-  // one row per workgroup while there are few (their parts are many), else as
-  // many as leave a row's dims a thread each (8 rather than 4 rows: 13.7 rather
-  // than 21.5 us for 8 questions' 50,000 rows, 6.1 rather than 8.5 for 12,000).
-  // Few: 2,800 rows of 6 parts took 11.0 us one by one and 7.1 by eights, 1,024
-  // rows of 18 parts 9.9 and 14.4
   const int rows = most_rows < a.rows ? most_rows : a.rows;
   const int64_t tiles = (int64_t)a.n_units * a.n_kv;
-  if (tiles * ((rows + 3) / 4) >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  if (tiles * rows <= 1024) {
-    CR_LAUNCH((attend_merge_kernel<T, 1>), dim3((unsigned)(tiles * rows)), dim3(256), 0, s, a, pre,
-              tab, rows);
+  const int rpw = merge_rows(tiles, rows, a.head_dim), blocks = (rows + rpw - 1) / rpw;
+  const int64_t groups = merge_groups(tiles, rows, a.head_dim);
+  if (!fits_launch(groups, 256)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)groups);
+  if (rpw == 1) {
+    CR_LAUNCH((attend_merge_kernel<T, 1>), grid, dim3(256), 0, s, a, pre, tab, blocks);
+  } else if (rpw == 8) {
+    CR_LAUNCH((attend_merge_kernel<T, 8>), grid, dim3(256), 0, s, a, pre, tab, blocks);
   } else {
-    const int rpw = a.head_dim <= 128 ? 8 : 4, blocks = (rows + rpw - 1) / rpw;
-    const dim3 grid((unsigned)(tiles * blocks));
-    if (rpw == 8) {
-      CR_LAUNCH((attend_merge_kernel<T, 8>), grid, dim3(256), 0, s, a, pre, tab, blocks);
-    } else {
-      CR_LAUNCH((attend_merge_kernel<T, 4>), grid, dim3(256), 0, s, a, pre, tab, blocks);
-    }
+    CR_LAUNCH((attend_merge_kernel<T, 4>), grid, dim3(256), 0, s, a, pre, tab, blocks);
   }
   return hipGetLastError();
 }
@@ -1068,7 +1061,7 @@ hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTa
 // ------------------------------------------------------------------ launch
 template <typename T, int D>
 hipError_t attend_as(const AttendArgs& a, const SeqTable& tab, int64_t items, hipStream_t s) {
-  const dim3 grid((unsigned)(items * a.n_kv));
+  const dim3 grid((unsigned)attend_groups(items, a.n_kv));
   constexpr int WIDE = attend_rows(sizeof(T), D), KEYS = ValueOps<T>::KEYS;
   constexpr int RB = tile_row_bytes(D * (int)sizeof(T));
   constexpr int OCC = attend_resident(sizeof(T), D);
@@ -1080,9 +1073,10 @@ hipError_t attend_as(const AttendArgs& a, const SeqTable& tab, int64_t items, hi
   constexpr int KM = sizeof(T) == 2 && D <= 128 ? 2 * KEYS : KEYS;
   constexpr int KW = KM < 4096 / RB ? 4096 / RB : KM;
   if (a.rows == 16) {
-    CR_LAUNCH((attend_kernel<T, D, 1, 1, 2, KN, 2>), grid, dim3(128), 0, s, a, tab);
+    CR_LAUNCH((attend_kernel<T, D, 1, 1, 2, KN, 2>), grid, dim3(attend_threads(16)), 0, s, a, tab);
   } else if (a.rows == WIDE) {
-    CR_LAUNCH((attend_kernel<T, D, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(256), 0, s, a, tab);
+    CR_LAUNCH((attend_kernel<T, D, WIDE / 64, 4, 1, KW, 2, OCC>), grid, dim3(attend_threads(WIDE)), 0,
+              s, a, tab);
   } else {
     return hipErrorInvalidValue;
   }
@@ -1093,7 +1087,7 @@ template <typename T>
 hipError_t attend(const AttendArgs& a, const SeqTable& tab, hipStream_t s) {
   const int64_t items = a.shared ? (int64_t)a.n_units * a.splits
                                  : (int64_t)a.n_units + (a.slots ? a.slots : 0);
-  if (items * a.n_kv >= (int64_t)1 << 31) return hipErrorInvalidValue;
+  if (!fits_launch(attend_groups(items, a.n_kv), attend_threads(a.rows))) return hipErrorInvalidValue;
   switch (a.head_dim) {
     case 32: return attend_as<T, 32>(a, tab, items, s);
     case 64: return attend_as<T, 64>(a, tab, items, s);

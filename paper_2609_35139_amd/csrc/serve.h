@@ -9,6 +9,11 @@ namespace cr {
 
 constexpr int kMaxQueryHeads = 256;
 
+// HIP launches fewer than 2^32 threads along a dimension.
+constexpr bool fits_launch(int64_t workgroups, int threads) {
+  return workgroups <= (((int64_t)1 << 32) - 1) / threads;
+}
+
 // One layer of a paged cache and the sequences in it.  Token t of sequence s
 // lies in block table[s * max_blocks + (t >> shift)], row t & (2^shift - 1).
 // lens and table are device memory that only the kernels read: a length below 0
@@ -32,6 +37,18 @@ struct AppendArgs {
   const int* positions;             // device, null: the slot
   int rotate;                       // 0: copied as they are
 };
+// Heads (keys and queries) that a thread rotates: one while that leaves a CU one
+// workgroup at most, else four that share their angles (one / two / four / eight
+// heads: 64 tokens of 18 heads 5.7 / 6.3 / 6.8 / 10.0 us, 11,243 of 40 77 / 63 /
+// 57 / 55); and the workgroups of 256 threads of a launch.
+constexpr int append_heads(int64_t tokens, int64_t heads, int64_t head_dim) {
+  return tokens * heads * (head_dim / 16) <= 256 * 256 ? 1 : 4;
+}
+constexpr int64_t append_groups(int64_t tokens, int64_t n_kv, int64_t heads, int64_t head_dim) {
+  const int hpt = append_heads(tokens, heads, head_dim);
+  const int64_t rotated = (heads + hpt - 1) / hpt * (head_dim / 16), copied = n_kv * (head_dim / 8);
+  return (tokens * (rotated > copied ? rotated : copied) + 255) / 256;
+}
 template <typename T>
 hipError_t append_kv(const AppendArgs& a, const KeyRope& kr, const int32_t* offsets,
                      hipStream_t s);
@@ -88,6 +105,10 @@ constexpr int kTableSeqs = 128;
 struct SeqTable {
   int q[kTableSeqs + 1], unit[kTableSeqs + 1];
 };
+// Workgroups of a pass, one for each item and KV head, and their threads: two
+// waves for 16 rows, else four.
+constexpr int64_t attend_groups(int64_t items, int64_t n_kv) { return items * n_kv; }
+constexpr int attend_threads(int rows) { return rows == 16 ? 128 : 256; }
 template <typename T>
 hipError_t attend(const AttendArgs& a, const SeqTable& tab, hipStream_t s);
 
@@ -97,6 +118,19 @@ struct SharedParts {
   const float* part_o;
   const float2* part_ml;
 };
+// Rows that a workgroup (of 256 threads) of the merge joins, of at most `rows`
+// rows in each of `tiles` units and KV heads: one while there are few (their parts
+// are many), else as many as leave a row's dims a thread each (8 rather than 4
+// rows: 13.7 rather than 21.5 us for 8 questions' 50,000 rows, 6.1 rather than 8.5
+// for 12,000).  Few: 2,800 rows of 6 parts took 11.0 us one by one and 7.1 by
+// eights, 1,024 rows of 18 parts 9.9 and 14.4
+constexpr int merge_rows(int64_t tiles, int rows, int head_dim) {
+  return tiles * rows <= 1024 ? 1 : head_dim <= 128 ? 8 : 4;
+}
+constexpr int64_t merge_groups(int64_t tiles, int rows, int head_dim) {
+  const int per = merge_rows(tiles, rows, head_dim);
+  return tiles * ((rows + per - 1) / per);
+}
 // Joins the partial results of a planned pass and those of the shared keys.  most_rows: rows of the longest sequence.
 template <typename T>
 hipError_t attend_merge(const AttendArgs& a, const SharedParts& pre, const SeqTable& tab,

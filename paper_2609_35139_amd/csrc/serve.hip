@@ -232,6 +232,15 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   return p;
 }
 
+// Whether every launch of a planned call is one that HIP makes.
+bool launches_fit(const cr_kv_layout* l, const Batch& b, int n_heads, const Plan& p) {
+  const int64_t H = l->n_kv_heads, G = n_heads / H;
+  const int most_rows = (int)std::min<int64_t>(b.most * G, p.rows);
+  return fits_launch(attend_groups(p.units + p.slots, H), attend_threads(p.rows)) &&
+         fits_launch(attend_groups(p.pre_units * p.splits, H), attend_threads(p.pre_rows)) &&
+         (!p.own_items || fits_launch(merge_groups(p.units * H, most_rows, l->head_dim), 256));
+}
+
 cr_status check_attend(const cr_kv_layout* l, const cr_sequences* q, int n_heads, int shared,
                        Batch* b) {
   cr_status st = check_cache(l);
@@ -383,9 +392,8 @@ cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t layer,
         (q->stride_token != q_out->stride_token || q->stride_head != q_out->stride_head))
       return CR_ERR_LAYOUT;
   }
-  // (a launch of at most 2^31 workgroups)
-  if ((double)b.n_tokens * (H + (q ? n_heads : 0)) * (D / 8) >= 256.0 * 2147483647.0)
-    return CR_ERR_DIMS;
+  // (in 64 bits: tokens below 2^31, heads at most 2^17)
+  if (!fits_launch(append_groups(b.n_tokens, H, H + (q ? n_heads : 0), D), 256)) return CR_ERR_DIMS;
   if (b.n_tokens == 0) return CR_OK;
   st = check_device();
   if (st != CR_OK) return st;
@@ -418,7 +426,9 @@ cr_status cr_attend_workspace_bytes(const cr_kv_layout* layout, const cr_sequenc
   Batch b;
   const cr_status st = check_attend(layout, seqs, n_heads, shared_len, &b);
   if (st != CR_OK) return st;
-  *bytes = b.n_tokens ? attend_plan(layout, seqs, b, n_heads, shared_len).total : 0;
+  const Plan p = b.n_tokens ? attend_plan(layout, seqs, b, n_heads, shared_len) : Plan{};
+  if (b.n_tokens && !launches_fit(layout, b, n_heads, p)) return CR_ERR_DIMS;
+  *bytes = p.total;
   return CR_OK;
 }
 
@@ -447,7 +457,7 @@ cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t layer,
   if (q->data == out->data) return CR_ERR_LAYOUT;
   if (b.n_tokens == 0) return CR_OK;
   const Plan p = attend_plan(layout, seqs, b, n_heads, o.shared_len);
-  if (p.units * layout->n_kv_heads >= kMostTokens) return CR_ERR_DIMS;
+  if (!launches_fit(layout, b, n_heads, p)) return CR_ERR_DIMS;
   if (p.total) {
     if (!workspace) return CR_ERR_NULL;
     if (workspace_bytes < p.total || !aligned(workspace, ALIGN)) return CR_ERR_WORKSPACE;
