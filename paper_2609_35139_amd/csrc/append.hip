@@ -17,12 +17,14 @@ struct AppendBatch {
 
 // A thread rotates 8 rotate-half pairs (i0 .. i0 + 7 and their partners) of
 // HPT heads of one token: its eight angles serve all of them.  The angle
-// p f_i is formed in turns in fp64 and reduced to half a turn, which leaves a
-// multiple of pi that fp32 evaluates to full precision at any position.
-// Grid y = 1 copies the values, 8 elements of one head per thread.
+// p f_i is formed in turns in fp64 and reduced to half a turn, its cosine and
+// sine are fp64 and rounded to 32 bits once, as in the repair's own rotation
+// (fp32 functions of the reduced angle: 55.5 instead of 56.1 us at 11,000 tokens,
+// 5.0 instead of 5.1 at 64, and an error of 3.0e-8 instead of 1.9e-8 of fp32
+// keys).  Grid y = 1 copies the values, 8 elements of one head per thread.
 // Bound by memory: each element is read and written once, 16 bytes at a time.
-// 11,000 tokens of 32 + 8 heads of 128 (276 MB with the values) take 57 us, 4.8
-// TB/s; 64 single tokens take 6 us, which is a launch and two dependent reads.
+// 11,243 tokens of 32 + 8 heads of 128 (276 MB with the values) take 56 us, 4.9
+// TB/s; 64 single tokens take 5.1 us, which is a launch and two dependent reads.
 template <typename T, int HPT>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, KeyRope kr, AppendBatch b) {
   const int per_head = blockIdx.y == 0 ? a.head_dim / 16 : a.head_dim / 8;
@@ -74,9 +76,10 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, KeyRope kr, A
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const double turns = p * kr.f[c0 + e];
-      const float r = (float)(turns - rint(turns));
-      cs[e] = cospif(2.f * r) * (float)kr.scale;
-      sn[e] = sinpif(2.f * r) * (float)kr.scale;
+      double s, c;
+      sincospi(2. * (turns - rint(turns)), &s, &c);
+      cs[e] = (float)(kr.scale * c);
+      sn[e] = (float)(kr.scale * s);
     }
   }
   // heads [0, n_kv) are keys, the others queries; a head is loaded before the

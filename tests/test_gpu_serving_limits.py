@@ -171,3 +171,31 @@ def test_caps_of_every_size(dtype, cap):
         ref, rl, tol, ltol = _capped(b, cap)
         assert_within(out, ref, tol, f"out {q}")
         assert_within(lse, rl, ltol, f"lse {q}")
+
+
+# ----------------------------------------------------------------- roundings
+@pytest.mark.parametrize("far", [0, 1 << 20])
+def test_append_rounds_cosines_and_sines_once(far):
+    """fp32: of a rotated pair's element only the cosine, the sine, two products
+    and their difference are rounded to 32 bits."""
+    b = Batch("f32", 6, 2, 128, 16, [300, 70], [900, 70], seed=89)
+    cache, seqs, q, k, v = b.cuda()
+    p = [far + j for _, j in b.slots()]
+    got = cache.append(0, seqs, k, v, q=q, rope=dict(theta=1e6, scale=1.25),
+                       positions=torch.tensor(p, dtype=torch.int32).cuda())
+    p = torch.tensor(p, dtype=torch.float64)[:, None, None]
+    ang = p * 1e6 ** (-torch.arange(64, dtype=torch.float64) / 64)
+    c, s = 1.25 * ang.cos(), 1.25 * ang.sin()
+
+    def rotated(x):
+        u, w = x[..., :64].double(), x[..., 64:].double()
+        y = torch.cat([c * u - s * w, c * w + s * u], -1)
+        size = torch.cat([(c * u).abs() + (s * w).abs(), (c * w).abs() + (s * u).abs()], -1)
+        # (the angle in 64 bits: four roundings on either side)
+        off = 2.0 ** -50 * p * 1.25 * (u.abs() + w.abs()).repeat(1, 1, 2)
+        return y, 2.0 ** -24 * (2 * size + y.abs()) + off
+
+    assert_within(got, *rotated(b.qh), "queries")
+    ref, tol = rotated(b.kh)
+    at = torch.tensor([b.row(*x) for x in b.slots()])
+    assert_within(cache.pool[0, 0, at[:, 0], at[:, 1]], ref, tol, "keys")
