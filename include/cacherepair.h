@@ -580,8 +580,10 @@ typedef struct {
  *   g = n_heads / n_kv_heads,
  * over the keys that the query sees.  A query that sees none gets zeros (lse
  * -inf); what lies in keys and values that it does not see, infinities and
- * NaN among them, does not matter.  Scores, softmax and sums are fp32; bf16
- * caches round the probabilities to bf16 for the product with V.
+ * NaN among them, does not matter.  Scores, softmax and sums are fp32.  bf16
+ * caches round the probabilities for the product with V: to 16 bits where no
+ * sequence has more than 16 rows (its queries times g), else to bf16, as in the
+ * pass over shared keys.
  *  q, out:    [n_tokens][n_heads][head_dim]; n_heads a multiple of n_kv_heads,
  *             at most 256.  out must not overlap q or the cache.
  *  options:   NULL = causal, scale 1 / sqrt(head_dim).

@@ -368,6 +368,15 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   constexpr int KS = VO::KEYS;
   constexpr int QF = D / KSTEP, DT = D / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
+  // The matrix instructions take bf16 probabilities.  Units of 16 rows, bound by
+  // reading the keys, multiply V by what that rounding leaves over too (16 bits in
+  // all, an error of 0.0017 instead of 0.0020 of the output, bf16's own rounding
+  // 0.0017; 148 us with and without for 64 sequences of 64 to 16,000 keys of 128
+  // dims, 242 and 235 for 32 of 2,000 to 8,000 of 256).  Wide units do not: 8,192 queries over 12,288 keys would take 1,619 instead of 1,137
+  // us, 590 tokens of questions 93 instead of 65.  Their sum is then of the rounded
+  // ones, so that the weights still add up to one.
+  constexpr bool FINE = sizeof(T) == 2 && RG == 1;
+  constexpr int PL = FINE ? PF : 1;
   constexpr int VE = NQ > 1 && sizeof(T) == 2 && D >= 64 && D <= 128 ? 3 : 0;
   // rings (later the merge area), the segment's block list (addresses of the
   // blocks' keys), the bits of those that are no block, and of every row (lo,
@@ -595,8 +604,9 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
         for (int e = 0; e < 4; ++e)
           s[t][e] -= __int_as_float(w.w) * fabsf((float)(k1 - (t * 16 + e)));
     };
-    // probabilities of row block n against its reference, packed, and their sum
-    auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF]) {
+    // probabilities of row block n against its reference, packed, what that
+    // leaves over (FINE), and their sum
+    auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF], frag (&pl)[PL]) {
       float ts = 0.f;
 #pragma unroll
       for (int f = 0; f < PF; ++f) {
@@ -605,7 +615,17 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
         for (int e = 0; e < KPL; ++e)
           pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f * (KPL / 4) + e / 4][e % 4], cc, -ref));
         pf[f] = pack_frag(pv, (frag*)nullptr);
-        ts = frag_sum(pf[f], ts);
+        if constexpr (FINE) {
+          float rest[KPL];
+#pragma unroll
+          for (int e = 0; e < KPL; ++e) {
+            ts += pv[e];
+            rest[e] = pv[e] - to_f32(pf[f][e]);
+          }
+          pl[f] = pack_frag(rest, (frag*)nullptr);
+        } else {
+          ts = frag_sum(pf[f], ts);
+        }
       }
       return ts;
     };
@@ -666,12 +686,12 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
         for (int d = 0; d < VE; ++d) ve[f][d] = VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
       if (VE) __builtin_amdgcn_sched_barrier(0);
-      frag pf[NQ][PF];
+      frag pf[NQ][PF], pl[NQ][PL];
       float ts[NQ];
       bool over[NQ], any = false;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        ts[n] = probs(s[n], reference(n), pf[n]);
+        ts[n] = probs(s[n], reference(n), pf[n], pl[n]);
         over[n] = m[n] == -INFINITY || !(ts[n] <= kMostSum);
         any = any || over[n];
       }
@@ -679,7 +699,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
           new_reference(s[n], n, any_in_row(over[n]));
-          ts[n] = probs(s[n], reference(n), pf[n]);
+          ts[n] = probs(s[n], reference(n), pf[n], pl[n]);
         }
       }
 #pragma unroll
@@ -695,7 +715,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
           const frag vf = d < VE ? ve[f][d < VE ? d : 0]
                                  : VO::template load<RB>(vt, f * VO::KEYS, d * 16, lane);
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          for (int n = 0; n < NQ; ++n) {
+            if constexpr (FINE) oacc[n][d] = MM::mma(vf, pl[n][f], oacc[n][d]);
+            oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          }
         }
       __builtin_amdgcn_s_setprio(0);
     };
@@ -710,7 +733,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       f32x4 s[NQ][ST];
       scores(kt, lane, s);
       uint32_t see[NQ];            // visible bits of this lane's scores (bit t * 4 + e)
-      frag pf[NQ][PF];
+      frag pf[NQ][PF], pl[NQ][PL];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         if (general) transform(s[n], n, k0, lane);
@@ -735,11 +758,11 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (!((see[n] >> (t * 4 + e)) & 1)) s[n][t][e] = -INFINITY;
-        float ts = probs(s[n], reference(n), pf[n]);
+        float ts = probs(s[n], reference(n), pf[n], pl[n]);
         const bool over = m[n] == -INFINITY || !(ts <= kMostSum);
         if (__any(over)) {
           new_reference(s[n], n, any_in_row(over));
-          ts = probs(s[n], reference(n), pf[n]);
+          ts = probs(s[n], reference(n), pf[n], pl[n]);
         }
         l[n] += ts;
       }
@@ -770,7 +793,10 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
             }
           }
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          for (int n = 0; n < NQ; ++n) {
+            if constexpr (FINE) oacc[n][d] = MM::mma(vf, pl[n][f], oacc[n][d]);
+            oacc[n][d] = MM::mma(vf, pf[n][f], oacc[n][d]);
+          }
         }
     };
 

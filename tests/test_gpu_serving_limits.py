@@ -199,3 +199,24 @@ def test_append_rounds_cosines_and_sines_once(far):
     ref, tol = rotated(b.kh)
     at = torch.tensor([b.row(*x) for x in b.slots()])
     assert_within(cache.pool[0, 0, at[:, 0], at[:, 1]], ref, tol, "keys")
+
+
+@pytest.mark.parametrize("d", range(32, 257, 32))
+def test_single_tokens_keep_their_weights(d):
+    """bf16, calls of at most 16 rows: no probability is rounded to bf16, so the
+    result's own rounding is the only one of that size."""
+    for q, lens in (([1] * 5, [3, 17, 900, 64, 2500]), ([2, 1], [31, 333])):
+        b = Batch("bf16", 8, 2, d, 16, q, lens, seed=97)
+        cache, seqs, qh, _, _ = b.cuda()
+        lse = torch.empty(b.N, b.heads, device="cuda")
+        out = cache.attend(0, seqs, qh, lse=lse)
+        ref, rl, tol, ltol = attend_oracle(b, 0)
+        # serving_helpers.attend_oracle's bounds, where a weight's own error is
+        # 2^-16 and no more than half a step (2^-8) of bf16 comes on top: taken off
+        # here for the weights (a part of their sum and of the output's size),
+        # 2^-17 put in for the two bf16 parts of a weight
+        assert_within(lse, rl, ltol - HALF["bf16"] + 2.0 ** -17, f"lse {q}")
+        half = HALF["bf16"]
+        rest = tol - half * ref.abs()                       # (rel)(sum of w |v| + |o|)
+        fine = rest * ((ltol - half + 2.0 ** -17) / ltol)[..., None] + half * ref.abs()
+        assert_within(out, ref, fine, f"out {q}")
