@@ -605,8 +605,8 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
           s[t][e] -= __int_as_float(w.w) * fabsf((float)(k1 - (t * 16 + e)));
     };
     // probabilities of row block n against its reference, packed, what that
-    // leaves over (FINE), and their sum
-    auto probs = [&](const f32x4 (&s)[ST], float ref, frag (&pf)[PF], frag (&pl)[PL]) {
+    // leaves over (FINE), and their sum; all: every row sees every key
+    auto probs = [&](auto all, const f32x4 (&s)[ST], float ref, frag (&pf)[PF], frag (&pl)[PL]) {
       float ts = 0.f;
 #pragma unroll
       for (int f = 0; f < PF; ++f) {
@@ -614,16 +614,24 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
         for (int e = 0; e < KPL; ++e)
           pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f * (KPL / 4) + e / 4][e % 4], cc, -ref));
-        pf[f] = pack_frag(pv, (frag*)nullptr);
         if constexpr (FINE) {
+          // cut off, not rounded, so that the rest has the probability's sign; and
+          // no rest of 0 where a value may be infinite (2^-126, the least that the
+          // exponential returns)
+          u32x4 top;
           float rest[KPL];
 #pragma unroll
           for (int e = 0; e < KPL; ++e) {
+            const uint32_t w = __float_as_uint(pv[e]);
+            top[e / 2] = e % 2 ? top[e / 2] | (w & 0xffff0000u) : w >> 16;
+            rest[e] = pv[e] - __uint_as_float(w & 0xffff0000u);
+            if (decltype(all)::value) rest[e] = fmaxf(rest[e], 0x1p-126f);
             ts += pv[e];
-            rest[e] = pv[e] - to_f32(pf[f][e]);
           }
+          pf[f] = __builtin_bit_cast(frag, top);
           pl[f] = pack_frag(rest, (frag*)nullptr);
         } else {
+          pf[f] = pack_frag(pv, (frag*)nullptr);
           ts = frag_sum(pf[f], ts);
         }
       }
@@ -691,7 +699,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
       bool over[NQ], any = false;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        ts[n] = probs(s[n], reference(n), pf[n], pl[n]);
+        ts[n] = probs(std::true_type{}, s[n], reference(n), pf[n], pl[n]);
         over[n] = m[n] == -INFINITY || !(ts[n] <= kMostSum);
         any = any || over[n];
       }
@@ -699,7 +707,7 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
           new_reference(s[n], n, any_in_row(over[n]));
-          ts[n] = probs(s[n], reference(n), pf[n], pl[n]);
+          ts[n] = probs(std::true_type{}, s[n], reference(n), pf[n], pl[n]);
         }
       }
 #pragma unroll
@@ -758,11 +766,11 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (!((see[n] >> (t * 4 + e)) & 1)) s[n][t][e] = -INFINITY;
-        float ts = probs(s[n], reference(n), pf[n], pl[n]);
+        float ts = probs(std::false_type{}, s[n], reference(n), pf[n], pl[n]);
         const bool over = m[n] == -INFINITY || !(ts <= kMostSum);
         if (__any(over)) {
           new_reference(s[n], n, any_in_row(over));
-          ts = probs(s[n], reference(n), pf[n], pl[n]);
+          ts = probs(std::false_type{}, s[n], reference(n), pf[n], pl[n]);
         }
         l[n] += ts;
       }

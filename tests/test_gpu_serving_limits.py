@@ -220,3 +220,21 @@ def test_single_tokens_keep_their_weights(d):
         rest = tol - half * ref.abs()                       # (rel)(sum of w |v| + |o|)
         fine = rest * ((ltol - half + 2.0 ** -17) / ltol)[..., None] + half * ref.abs()
         assert_within(out, ref, fine, f"out {q}")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64)])
+@pytest.mark.parametrize("q", [1, 40])
+def test_values_that_are_not_finite_where_all_rows_see_them(dtype, d, q):
+    """Infinities and NaN in the middle of long sequences, in tiles without a
+    mask: the dims that hold them become infinite or NaN, no others."""
+    b = Batch(dtype, 4, 2, d, 16, [q] * 3, [700, 300, 1500], seed=101)
+    odd = {(0, 133): (3, float("inf")), (0, 400): (d - 1, -float("inf")), (1, 77): (8, float("nan")),
+           (1, 78): (9, float("inf")), (1, 79): (9, -float("inf")), (2, 1000): (d // 2, -float("inf")),
+           (2, 1001): (d // 2, -float("inf"))}
+    for (s, j), (i, x) in odd.items():
+        at = b.row(s, j)
+        b.pool[0, 1, at[0], at[1], 1, i] = x
+    cache, seqs, qh, _, _ = b.cuda()
+    out = cache.attend(0, seqs, qh)
+    ref, _, tol, _ = attend_oracle(b, 0)
+    assert_within(out, ref, tol, "out")
