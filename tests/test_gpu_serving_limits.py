@@ -238,3 +238,35 @@ def test_values_that_are_not_finite_where_all_rows_see_them(dtype, d, q):
     out = cache.attend(0, seqs, qh)
     ref, _, tol, _ = attend_oracle(b, 0)
     assert_within(out, ref, tol, "out")
+
+
+# ------------------------------------------------------- how a batch is cut up
+SPLIT = {
+    # as many units as fill the chip, or tables that hold few keys: no parts
+    "many tokens": (False, dict(heads=8, kv_heads=8, q=[1] * 1030, lens=[1 + 13 * s % 280 for s in range(1030)])),
+    "many questions": (False, dict(heads=16, kv_heads=16, q=[17] * 33, lens=[17 + 11 * s for s in range(33)])),
+    "short table": (False, dict(heads=4, kv_heads=2, q=[1] * 3, lens=[500, 512, 1])),
+    "short questions": (False, dict(heads=8, kv_heads=2, q=[20, 30], lens=[100, 128])),
+    # parts, joined by a launch of their own (whole units leave it nothing to do)
+    "one token": (True, dict(heads=4, kv_heads=2, q=[1], lens=[4000])),
+    "even tokens": (True, dict(heads=8, kv_heads=8, q=[1] * 64, lens=[700 - s for s in range(64)])),
+    "uneven tokens": (True, dict(heads=8, kv_heads=8, q=[1] * 64, lens=[3000] + [100] * 63)),
+    "questions": (True, dict(heads=16, kv_heads=4, q=[32, 9, 17], lens=[4000, 32, 600])),
+}
+
+
+@pytest.mark.parametrize("name", SPLIT)
+def test_which_batches_are_split(name):
+    from paper_2609_35139_amd import binding as B
+    split, c = SPLIT[name]
+    b = Batch("bf16", d=64, bs=16, seed=103, **c)
+    cache, seqs, qh, _, _ = b.cuda()
+    B.cr_profile_enable(8)
+    try:
+        out = cache.attend(0, seqs, qh)
+        assert ("attend_merge" in {r["name"] for r in B.cr_profile_read()}) == split
+    finally:
+        B.cr_profile_enable(0)
+    tell = list(range(0, b.N, max(1, b.N // 64)))
+    ref, _, tol, _ = attend_oracle(b, 0, tokens=tell)
+    assert_within(out[tell], ref[tell], tol[tell], name)

@@ -60,3 +60,15 @@ def test_append_with_more_threads_than_a_launch_has():
     with pytest.raises(B.CrError) as e:
         B.cr_append_kv(0x10000, lay, 0, q, *rows, None, None, 0, None, None)
     assert e.value.name == "CR_ERR_DIMS"
+
+
+def test_the_serving_kernels_are_among_the_resources_reported():
+    """... so that none of them can spill unseen."""
+    import os
+    from paper_2609_35139_amd import build
+    if not os.path.exists(build.RESOURCES):
+        pytest.skip("library not built here")
+    names = [line.split()[0] for line in open(build.RESOURCES)]
+    for element in ("DF16b", "f"):
+        for kernel, count in (("append_kernel", 2), ("attend_kernel", 16), ("attend_merge_kernel", 3)):
+            assert sum(f"{kernel}I{element}L" in n for n in names) == count, (kernel, element)
