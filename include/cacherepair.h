@@ -580,7 +580,10 @@ typedef struct {
  *   g = n_heads / n_kv_heads,
  * over the keys that the query sees.  A query that sees none gets zeros (lse
  * -inf); what lies in keys and values that it does not see, infinities and
- * NaN among them, does not matter.  Scores, softmax and sums are fp32.  bf16
+ * NaN among them, does not matter.  A value that it sees and that is infinite
+ * or NaN makes that dimension of its result infinite or NaN (either of them for
+ * an infinite one whose weight is too small for fp32).  Sums are divided at the
+ * end: finite values beyond 2^75 may overflow them.  Scores, softmax and sums are fp32.  bf16
  * caches round the probabilities for the product with V: to 16 bits where no
  * sequence has more than 16 rows (its queries times g), else to bf16, as in the
  * pass over shared keys.

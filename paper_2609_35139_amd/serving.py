@@ -11,6 +11,11 @@ device, by every replay of a captured step)::
     for layer in range(L):
         cache.append(layer, step, k, v, q=q, q_out=q, rope={"theta": 1e6})
         o = cache.attend(layer, step, q)
+
+Calls go to ``stream``, or to torch's current stream on the cache's device.
+Where that is not the stream that a tensor was allocated on, the caller orders
+the two and keeps the tensor (or calls its ``record_stream``) until the call
+has run, as for any torch operation on another stream.
 """
 from __future__ import annotations
 
