@@ -23,15 +23,15 @@
 // of one dim per lane: for bf16 the LDS reads that transpose 16-bit elements
 // deliver that from the row-major tile.
 //
-// What it reaches (a large copy runs at 3.95 TB/s, a large product at 1,333
-// TFLOP/s in bf16 and 153 in fp32 on the same card):
+// What it reaches (a large copy runs at 5.1 TB/s, a large product at 1,250
+// TFLOP/s in bf16 and 144 in fp32):
 //  - one token per sequence, rows of 16: bound by reading keys and values, 64
-//    sequences of 64 to 16,000 keys (716 MB) in 147 us, 4.9 TB/s; 4 of 131,072
+//    sequences of 64 to 16,000 keys (716 MB) in 148 us, 4.8 TB/s; 4 of 131,072
 //    (513 MB) in 98 us, 5.2 TB/s.  Of a single one of 4,096 keys (14 us with the
 //    merge) most is the chain of dependent reads and the second launch.
 //  - long prompts, wide units: bound by the waves' own instructions, the matrix
 //    pipes work 43% of the time; 8,192 queries over 12,288 keys, 32 heads of 128
-//    in 1,090 us, 1,010 TFLOP/s.
+//    in 1,100 us, 1,000 TFLOP/s.
 //  - in between (8 to 300 queries a sequence), the parts' partial results and
 //    uneven rounds cost as much as the products; see attend_plan.
 #pragma once
@@ -369,12 +369,13 @@ __global__ __launch_bounds__(64 * RG * KG, OCC) void attend_kernel(AttendArgs a,
   constexpr int QF = D / KSTEP, DT = D / 16, ST = KS / 16, PF = KS / VO::KEYS;
   constexpr int RB = C::RB;
   // The matrix instructions take bf16 probabilities.  Units of 16 rows, bound by
-  // reading the keys, multiply V by what that rounding leaves over too (16 bits in
-  // all, an error of 0.0017 instead of 0.0020 of the output, bf16's own rounding
-  // 0.0017; 148 us with and without for 64 sequences of 64 to 16,000 keys of 128
-  // dims, 242 and 235 for 32 of 2,000 to 8,000 of 256).  Wide units do not: 8,192 queries over 12,288 keys would take 1,619 instead of 1,137
-  // us, 590 tokens of questions 93 instead of 65.  Their sum is then of the rounded
-  // ones, so that the weights still add up to one.
+  // reading the keys, multiply V by what that leaves over too (16 bits in all, an
+  // error of 0.0017 instead of 0.0020 of the output, bf16's own rounding 0.0017;
+  // 148 us with and without for 64 sequences of 64 to 16,000 keys of 128 dims, 242
+  // and 235 for 32 of 2,000 to 8,000 of 256).  Wide units round to bf16 (8,192
+  // queries over 12,288 keys would take 1,619 instead of 1,137 us, 590 tokens of
+  // questions 93 instead of 65); their sum is then of the rounded ones, so that the
+  // weights still add up to one.
   constexpr bool FINE = sizeof(T) == 2 && RG == 1;
   constexpr int PL = FINE ? PF : 1;
   constexpr int VE = NQ > 1 && sizeof(T) == 2 && D >= 64 && D <= 128 ? 3 : 0;

@@ -129,7 +129,12 @@ struct Plan {
 // with 32 query and 8 KV heads, shared pass against none, 100 keys more each: 32
 // sequences of one token over 2048 shared keys 31 / 29 us, over 16384 46 / 121;
 // of 8 tokens over 2048 51 / 45 us, over 16384 101 / 207; of 32 tokens, which
-// fill their units, 322 / 289.
+// fill their units, 322 / 289.  Other types and dims by the bytes of a narrow
+// unit's keys and the matrix instructions of a wide one's: of one token, fp32 of
+// 128 dims over 512 42 / 38, over 2048 47 / 80, bf16 of 64 over 2048 26.2 / 25.6,
+// over 16384 36 / 81, of 256 over 2048 45 / 89; of 8 tokens, fp32 of 64 dims over
+// 512 46.0 / 47.5 (it takes the slower), over 2048 77 / 110, bf16 of 256 over 512
+// 50 / 36, over 16384 202 / 299.
 bool shared_pays(const cr_kv_layout* l, const Batch& b, int G, const Plan& p, int shared) {
   const double elt = (double)esize(l->dtype), D = l->head_dim;
   const double wide = D / 128 * (elt == 4 ? 8 : 1) * attend_rows((int)elt, (int)D) / 128;
@@ -210,7 +215,9 @@ Plan attend_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, i
   }
   // No split of wide units where it gains less than the merge takes: 2 us and 2.4 us for every
   // million sums, at 2 us for a wide bf16 tile of 128 dims.  A workgroup that
-  // has its CU to itself takes two thirds of the time per tile, and with more
+  // has its CU to itself takes two thirds of the time per tile (split_cost 1.5 / 1:
+  // 16 sequences of 32 tokens over 300 keys 25.8 / 33.0 us, 24 over 600 36.3 /
+  // 42.2, 8 to 24 over 1200 and more even), and with more
   // units than fit one round a split pays for very uneven lengths alone.  20
   // sequences of 32 tokens, 300 keys, 8 KV heads: 36 us split, 28 in one part;
   // 32 of them over 600 keys 48 and 37.5, over 2400 95 and 107; a prompt of 2000
