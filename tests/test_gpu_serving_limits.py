@@ -270,3 +270,30 @@ def test_which_batches_are_split(name):
     tell = list(range(0, b.N, max(1, b.N // 64)))
     ref, _, tol, _ = attend_oracle(b, 0, tokens=tell)
     assert_within(out[tell], ref[tell], tol[tell], name)
+
+
+@pytest.mark.parametrize("dtype,d,q", [("bf16", 128, [1] * 120), ("bf16", 64, [5, 0, 9, 7] * 30),
+                                       ("f32", 64, [1] * 120), ("f32", 128, [3, 0, 9, 4] * 20)])
+def test_shared_pass_under_masks(dtype, d, q):
+    """The pass over shared keys (a prefix that ends inside a page; sequences
+    that end inside it, hold nothing or have no query), causal and under
+    windows, a cap and distance slopes."""
+    from paper_2609_35139_amd import binding as B
+    shared = 3001
+    lens = [shared + [40, -1700, 300, 9, -3001, 129, 1][s % 7] for s in range(len(q))]
+    b = Batch(dtype, 16, 8, d, 16, q, lens, seed=107, shared=3008)
+    cache, seqs, qh, _, _ = b.cuda()
+    p = np.array([j for _, j in b.slots()])
+    tell = list(range(0, b.N, 6))
+    for opt in ({}, dict(lo=p - 500, hi=np.where(p % 4 == 1, 0, p + 1), softcap=8.0,
+                         slopes=[0.01 * h for h in range(16)])):
+        dev = {k: torch.tensor(v, dtype=torch.int32).cuda() if k in ("lo", "hi") else v
+               for k, v in opt.items()}
+        B.cr_profile_enable(8)
+        try:
+            out = cache.attend(0, seqs, qh, shared_len=shared, **dev)
+            assert "attend_shared" in {r["name"] for r in B.cr_profile_read()}
+        finally:
+            B.cr_profile_enable(0)
+        ref, _, tol, _ = attend_oracle(b, 0, tokens=tell, **opt)
+        assert_within(out[tell], ref[tell], tol[tell], str(sorted(opt)))
