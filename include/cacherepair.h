@@ -20,7 +20,8 @@
  * previous one.  cr_rotate_keys applies the target's rotary encoding (or its
  * inverse) to a cache's keys.  cr_append_kv and cr_attend answer over a
  * repaired paged cache: a question's or a step's new keys and values are
- * appended to it, and its queries attend to it.
+ * appended to it, and its queries attend to it; cr_weigh_keys, cr_choose_slots
+ * and cr_compact_kv keep such a cache within a budget, cr_sample draws tokens.
  *
  * Conventions shared by every entry point:
  *  - Plain C: no C++ or torch types.  All sizes are element counts unless the
@@ -605,8 +606,153 @@ CR_API cr_status cr_attend(const void* kv, const cr_kv_layout* layout, int32_t l
                     uint64_t workspace_bytes, void* stream);
 
 /*
+ * Keeping an answer going.  A cache grows with every token of the answer, and
+ * the logits of a step have to become its token.  cr_weigh_keys adds up how
+ * much attention every cached slot receives, cr_choose_slots says which slots
+ * stay when a sequence is over its budget, cr_compact_kv moves them to the
+ * front, and cr_sample draws the tokens.
+ *
+ * cr_key_weights: one fp32 weight for every slot of the table, of every layer,
+ * sequence and KV head, in device memory: slot j of them at
+ *   data + layer*stride_layer + seq*stride_seq + head*stride_head + j,
+ * j < max_blocks * block_size; strides in elements, not negative, rows not
+ * overlapping (rows that begin on 16 bytes are read faster).
+ */
+typedef struct {
+    float* data;
+    int64_t stride_layer, stride_seq, stride_head;
+} cr_key_weights;
+
+/*
+ * Adds to the weight of every slot of layer `layer` the probabilities that the
+ * batch's queries give it:
+ *   W[s, h, j] += sum over the queries t of sequence s and the heads g of KV
+ *                 head h's group of exp(score(q[t, g], K_j[h]) - lse[t, g]),
+ * scores as in cr_attend, over the keys that a query sees.  Weights of slots that no
+ * query sees stay as they are.
+ *  kv, layout, layer, seqs, q, n_heads: as in the call of cr_attend that it
+ *             goes with (the values are not read).
+ *  options:   as in that call, with lse: READ here, what that call left there.
+ *             A row whose lse is -inf gives nothing.  shared_len changes nothing.
+ *  weights:   all layers' weights; must not overlap any input.
+ *  workspace: device scratch of cr_weigh_workspace_bytes for the same
+ *             arguments, 256-byte aligned; contents undefined after the call.
+ *             Calls that may overlap in time need their own.
+ * Scores, exponentials and sums are fp32, the sums in an order that depends on
+ * sizes and lengths alone.  A key that is seen and not finite makes its own
+ * slot's weight infinite or NaN; where lse is NaN, all that the row sees.
+ * n_tokens == 0 returns CR_OK with nothing enqueued.
+ * Errors as cr_attend; CR_ERR_NULL also without options or lse, CR_ERR_LAYOUT
+ * also for the weights' strides and alignment.
+ */
+CR_API cr_status cr_weigh_workspace_bytes(const cr_kv_layout* layout, const cr_sequences* seqs,
+                                   int32_t n_heads, uint64_t* bytes);
+CR_API cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32_t layer,
+                        const cr_sequences* seqs, const cr_rows* q, int32_t n_heads,
+                        const cr_attend_options* options, const cr_key_weights* weights,
+                        void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * The slots that stay, for every layer, sequence and KV head by itself.  Of n =
+ * min(kv_lens[s], slots of the table) slots m = min(n, budget) stay: the last
+ * min(recent, m); the first min(first, what is left of m); and for the rest of m
+ * those of the largest weight among the others, the lowest slot of equal ones.
+ * NaN counts as -inf.
+ *  seqs:      n_seqs, kv_lens and the table's extent are used (the table itself
+ *             is not read, query_offsets and the blocks are ignored).
+ *  budgets:   device, n_seqs, or NULL: a sequence's own budget, within [0, budget].
+ *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget] int32: the slots
+ *             that stay, ascending, then -1.
+ *  kept_lens: device, n_seqs int32: m.
+ * n_layers and n_kv_heads are the layout's; nothing else of it is used.
+ * Errors: CR_ERR_NULL, CR_ERR_DIMS (layers, heads, budget < 1, first or recent
+ * < 0, a table of more than 2^30 slots, a batch that takes 2^32 threads),
+ * CR_ERR_OFFSETS (n_seqs), CR_ERR_LAYOUT (table, weights), CR_ERR_DEVICE before
+ * any enqueue; CR_ERR_LAUNCH.
+ */
+typedef struct {
+    int32_t budget, first, recent;
+    const int32_t* budgets;
+} cr_choice;
+
+CR_API cr_status cr_choose_slots(const cr_kv_layout* layout, const cr_sequences* seqs,
+                          const cr_key_weights* weights, const cr_choice* choice,
+                          int32_t* kept, int32_t* kept_lens, void* stream);
+
+/*
+ * Moves the slots that stay to the front, in all layers:
+ *   K, V, W[l, s, h, i] <- K, V, W[l, s, h, kept[l, s, h, i]],  i < kept_lens[s],
+ * and sets the weights from there to the sequence's old end to 0.  kv_lens are
+ * the lengths before; those after are kept_lens, which the caller makes the
+ * batch's (and gives cr_append_kv positions from then on: a token's slot is no
+ * longer its position).  Keys keep the rotation of the position that they had.
+ *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget], as cr_choose_slots
+ *             leaves it or the caller's own: ascending, each below its
+ *             sequence's length (an entry that is no such slot, or whose slot
+ *             lies in no block, moves nothing).
+ *  table_out: NULL = in place; a block that several sequences share must not be
+ *             compacted in place.  Otherwise device, n_seqs rows of
+ *             max_blocks_out block ids: the blocks to fill, none of which may
+ *             be a block that is read; what they hold is left alone where
+ *             nothing moves.  A slot past that table is dropped.
+ *  weights:   NULL = none.
+ * Errors as cr_choose_slots, and CR_ERR_DTYPE; layout and blocks as
+ * cr_append_kv.
+ */
+CR_API cr_status cr_compact_kv(void* kv, const cr_kv_layout* layout, const cr_sequences* seqs,
+                        const int32_t* kept, int32_t budget, const int32_t* kept_lens,
+                        const int32_t* table_out, int32_t max_blocks_out,
+                        const cr_key_weights* weights, void* stream);
+
+/*
+ * Draws a token from every row of logits.  A row's tokens stand in the order of
+ * their logits x, the lowest index of equal ones first; x_0 is the largest:
+ *   p_i = exp((x_i - x_0) / temperature).
+ * Of the first top_k tokens those stay before which the p sum to less than top_p
+ * times the sum over the top_k, and whose p is at least min_p; the first token
+ * always stays.  The token drawn is the first one, by index, up to which the p
+ * that stay sum to more than u times their sum.
+ *  logits:    device, n_rows rows of vocab logits, stride_row elements apart
+ *             (>= 0); dtype CR_DTYPE_BF16 or CR_DTYPE_F32; aligned to its
+ *             elements.  vocab at most 2^20.
+ *  options:   for all rows, or per row (device, n_rows) where the pointer is not
+ *             NULL.  temperature <= 0 or NaN: the first token.  top_k <= 0 or >=
+ *             vocab: no limit.  top_p >= 1: no limit; <= 0 or NaN: the first
+ *             token.  min_p <= 0: no limit; > 1 or NaN: the first token.
+ *             options NULL = temperature 1, no limits.
+ *  u:         device, n_rows fp32 random numbers in [0, 1) (below 0 and NaN
+ *             count as 0, from 1 on as just below 1).
+ *  tokens:    device, n_rows int32.
+ *  log_probs: NULL, or device, n_rows fp32: the logarithm of the probability
+ *             with which the token was drawn (0 for a first token).
+ * NaN logits count as -inf, which is never drawn; a row of them alone gives token
+ * -1, log-probability -inf.  Infinite logits share all of the probability.
+ * Probabilities are formed in 64 bits and held in steps of 2^-44 of the largest
+ * (2^-42 for vocab > 2^18); their sums are exact.
+ * n_rows == 0 returns CR_OK with nothing enqueued.
+ * Errors: CR_ERR_NULL, CR_ERR_DIMS (n_rows < 0 or 2^32 threads, vocab),
+ * CR_ERR_DTYPE, CR_ERR_LAYOUT (stride, alignment), CR_ERR_DEVICE before any
+ * enqueue; CR_ERR_LAUNCH.
+ */
+typedef struct {
+    const void* data;
+    int32_t dtype, n_rows, vocab;
+    int64_t stride_row;
+} cr_logits;
+
+typedef struct {
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float *temperatures, *top_ps, *min_ps;
+    const int32_t* top_ks;
+} cr_sampling;
+
+CR_API cr_status cr_sample(const cr_logits* logits, const cr_sampling* options, const float* u,
+                    int32_t* tokens, float* log_probs, void* stream);
+
+/*
  * Per-launch timing (tracing aid, not needed for repair).  While enabled,
- * cr_repair, cr_append_kv and cr_attend bracket every kernel launch with HIP
+ * cr_repair and the calls that answer over a cache bracket every kernel launch with HIP
  * events recorded on the call's own stream.  cr_profile_enable(max_launches)
  * creates the events (host-side allocation happens here, never inside
  * cr_repair); max_launches = 0 disables profiling and destroys them.  Launches

@@ -32,7 +32,9 @@ EXPORTS = ["cr_version", "cr_status_string", "cr_weights_layout", "cr_prepared_b
            "cr_default_options", "cr_repair_ex", "cr_rotate_workspace_bytes", "cr_rotate_keys",
            "cr_pipeline_create", "cr_pipeline_destroy", "cr_pipeline_staging_bytes",
            "cr_repair_pipelined", "cr_workspace_view", "cr_profile_enable", "cr_profile_read",
-           "cr_repair_static", "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend"]
+           "cr_repair_static", "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend",
+           "cr_weigh_workspace_bytes", "cr_weigh_keys", "cr_choose_slots", "cr_compact_kv",
+           "cr_sample"]
 CR_STATIC_SCRATCH_BYTES = 128 << 20
 CR_MASK = {"block_causal": 0, "token_causal": 1, "bidirectional": 2, "block_diagonal": 3}
 CR_APPLY = {"kv": 0, "k": 1, "v": 2}
@@ -94,6 +96,27 @@ class cr_rows(ctypes.Structure):
 class cr_attend_options(ctypes.Structure):
     _fields_ = [("scale", c_float), ("softcap", c_float), ("slopes", POINTER(c_float)),
                 ("lo", c_void_p), ("hi", c_void_p), ("shared_len", c_int32), ("lse", c_void_p)]
+
+
+class cr_key_weights(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("stride_layer", c_int64), ("stride_seq", c_int64),
+                ("stride_head", c_int64)]
+
+
+class cr_choice(ctypes.Structure):
+    _fields_ = [("budget", c_int32), ("first", c_int32), ("recent", c_int32),
+                ("budgets", c_void_p)]
+
+
+class cr_logits(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("dtype", c_int32), ("n_rows", c_int32), ("vocab", c_int32),
+                ("stride_row", c_int64)]
+
+
+class cr_sampling(ctypes.Structure):
+    _fields_ = [("temperature", c_float), ("top_p", c_float), ("min_p", c_float),
+                ("top_k", c_int32), ("temperatures", c_void_p), ("top_ps", c_void_p),
+                ("min_ps", c_void_p), ("top_ks", c_void_p)]
 
 
 class cr_kernel_stat(ctypes.Structure):
@@ -160,12 +183,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cr_attend.argtypes = [c_void_p, P(cr_kv_layout), c_int32, P(cr_sequences), P(cr_rows),
                               P(cr_rows), c_int32, P(cr_attend_options), c_void_p, c_uint64,
                               c_void_p]
+    lib.cr_weigh_workspace_bytes.argtypes = [P(cr_kv_layout), P(cr_sequences), c_int32,
+                                             P(c_uint64)]
+    lib.cr_weigh_keys.argtypes = [c_void_p, P(cr_kv_layout), c_int32, P(cr_sequences), P(cr_rows),
+                                  c_int32, P(cr_attend_options), P(cr_key_weights), c_void_p,
+                                  c_uint64, c_void_p]
+    lib.cr_choose_slots.argtypes = [P(cr_kv_layout), P(cr_sequences), P(cr_key_weights),
+                                    P(cr_choice), c_void_p, c_void_p, c_void_p]
+    lib.cr_compact_kv.argtypes = [c_void_p, P(cr_kv_layout), P(cr_sequences), c_void_p, c_int32,
+                                  c_void_p, c_void_p, c_int32, P(cr_key_weights), c_void_p]
+    lib.cr_sample.argtypes = [P(cr_logits), P(cr_sampling), c_void_p, c_void_p, c_void_p, c_void_p]
     for name in ["cr_weights_layout", "cr_prepared_bytes", "cr_prepare_weights",
                  "cr_workspace_bytes", "cr_chunk_schedule", "cr_repair", "cr_repair_ex",
                  "cr_rotate_workspace_bytes", "cr_rotate_keys", "cr_pipeline_create",
                  "cr_pipeline_destroy", "cr_pipeline_staging_bytes", "cr_repair_pipelined",
                  "cr_workspace_view", "cr_profile_enable", "cr_profile_read", "cr_repair_static",
-                 "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend"]:
+                 "cr_append_kv", "cr_attend_workspace_bytes", "cr_attend",
+                 "cr_weigh_workspace_bytes", "cr_weigh_keys", "cr_choose_slots", "cr_compact_kv",
+                 "cr_sample"]:
         getattr(lib, name).restype = c_int32
     _lib = lib
     return lib
@@ -474,6 +509,40 @@ def cr_attend(kv: int, layout: cr_kv_layout, layer: int, seqs: cr_sequences, q: 
               stream: Optional[int] = None) -> None:
     _check(load().cr_attend(kv, layout, layer, seqs, q, out, n_heads, options, workspace,
                             workspace_bytes, stream), "cr_attend")
+
+
+def cr_weigh_workspace_bytes(layout: cr_kv_layout, seqs: cr_sequences, n_heads: int) -> int:
+    b = c_uint64(0)
+    _check(load().cr_weigh_workspace_bytes(layout, seqs, n_heads, ctypes.byref(b)),
+           "cr_weigh_workspace_bytes")
+    return b.value
+
+
+def cr_weigh_keys(kv: int, layout: cr_kv_layout, layer: int, seqs: cr_sequences, q: cr_rows,
+                  n_heads: int, options: Optional[cr_attend_options], weights: cr_key_weights,
+                  workspace: Optional[int], workspace_bytes: int,
+                  stream: Optional[int] = None) -> None:
+    _check(load().cr_weigh_keys(kv, layout, layer, seqs, q, n_heads, options, weights, workspace,
+                                workspace_bytes, stream), "cr_weigh_keys")
+
+
+def cr_choose_slots(layout: cr_kv_layout, seqs: cr_sequences, weights: cr_key_weights,
+                    choice: cr_choice, kept: int, kept_lens: int,
+                    stream: Optional[int] = None) -> None:
+    _check(load().cr_choose_slots(layout, seqs, weights, choice, kept, kept_lens, stream),
+           "cr_choose_slots")
+
+
+def cr_compact_kv(kv: int, layout: cr_kv_layout, seqs: cr_sequences, kept: int, budget: int,
+                  kept_lens: int, table_out: Optional[int], max_blocks_out: int,
+                  weights: Optional[cr_key_weights], stream: Optional[int] = None) -> None:
+    _check(load().cr_compact_kv(kv, layout, seqs, kept, budget, kept_lens, table_out,
+                                max_blocks_out, weights, stream), "cr_compact_kv")
+
+
+def cr_sample(logits: cr_logits, options: Optional[cr_sampling], u: int, tokens: int,
+              log_probs: Optional[int], stream: Optional[int] = None) -> None:
+    _check(load().cr_sample(logits, options, u, tokens, log_probs, stream), "cr_sample")
 
 
 def cr_workspace_view(dims: cr_dims, layout: cr_kv_layout, n_tokens: int,

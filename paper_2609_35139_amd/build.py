@@ -13,12 +13,13 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.hip", "gemm.hip", "attention.hip", "rowops.hip", "serve.hip", "append.hip",
-           "attend_bf16.hip", "attend_f32.hip"]
+           "attend_bf16.hip", "attend_f32.hip", "answer.hip", "weigh.hip", "slots.hip",
+           "sample.hip"]
 # Per-source code generation options.  The attention kernels' score and
 # output accumulators are read by VALU code every key tile; keeping MFMA
 # operands in VGPRs avoids a copy out of the accumulation registers per tile.
 EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-         for src in ("attention.hip", "attend_bf16.hip", "attend_f32.hip")}
+         for src in ("attention.hip", "attend_bf16.hip", "attend_f32.hip", "weigh.hip")}
 LIB = os.path.join(HERE, "libcacherepair.so")
 ARCH = "gfx950"
 CFLAGS = [

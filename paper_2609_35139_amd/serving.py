@@ -1,5 +1,6 @@
 """Torch-side marshalling of answering over a paged cache (``cr_append_kv``,
-``cr_attend``): device buffers and streams only, like :mod:`repairer`.
+``cr_attend``, ``cr_weigh_keys``, ``cr_choose_slots``, ``cr_compact_kv``) and of
+``cr_sample``: device buffers and streams only, like :mod:`repairer`.
 
 :class:`PagedCache` wraps the block pool that a paged repair writes
 (``binding.paged_layout``); :meth:`PagedCache.sequences` describes a batch and
@@ -10,7 +11,15 @@ device, by every replay of a captured step)::
     step = cache.sequences(block_table, kv_lens)    # one new token per sequence
     for layer in range(L):
         cache.append(layer, step, k, v, q=q, q_out=q, rope={"theta": 1e6})
-        o = cache.attend(layer, step, q)
+        o = cache.attend(layer, step, q, lse=lse)
+        cache.weigh(layer, step, q, lse, weights)   # fp32 [L][n_seqs][H][slots of the table]
+    token, log_p = sample(logits, u, temperature=0.7, top_p=0.9)
+
+and, once sequences grow past their budget::
+
+    kept, kept_lens = cache.choose(step, weights, budget, first=4, recent=256)
+    cache.compact(step, kept, kept_lens, weights=weights)
+    kv_lens.copy_(kept_lens)      # appends take positions= from here on
 
 Calls go to ``stream``, or to torch's current stream on the cache's device.
 Where that is not the stream that a tensor was allocated on, the caller orders
@@ -32,6 +41,22 @@ from . import binding as B
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda i: torch.cuda.current_stream(i).cuda_stream)
 _DTYPE = {torch.bfloat16: B.CR_DTYPE_BF16, torch.float32: B.CR_DTYPE_F32}
+
+
+def _on_device(device: torch.device, stream: Optional[torch.cuda.Stream], call) -> None:
+    """call(stream handle) with the device and the call's stream as torch's current
+    ones: the library launches on the current device, and a workspace or result
+    allocated here belongs to the stream that uses it."""
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError("the stream must be on the device of the call's tensors")
+        with torch.cuda.stream(stream):
+            call(stream.cuda_stream)
+    elif torch.cuda.current_device() == device.index:
+        call(_raw_stream(device.index))
+    else:
+        with torch.cuda.device(device):
+            call(_raw_stream(device.index))
 
 
 class Sequences:
@@ -104,19 +129,7 @@ class PagedCache:
         return t.data_ptr()
 
     def _on(self, stream: Optional[torch.cuda.Stream], call) -> None:
-        """call(stream handle) with the cache's device and the call's stream as
-        torch's current ones: the library launches on the current device, and a
-        workspace or result allocated here belongs to the stream that uses it."""
-        if stream is not None:
-            if stream.device != self.device:
-                raise ValueError("the stream must be on the cache's device")
-            with torch.cuda.stream(stream):
-                call(stream.cuda_stream)
-        elif torch.cuda.current_device() == self.device.index:
-            call(_raw_stream(self.device.index))
-        else:
-            with torch.cuda.device(self.device):
-                call(_raw_stream(self.device.index))
+        _on_device(self.device, stream, call)
 
     def append(self, layer: int, seqs: Sequences, k: torch.Tensor, v: torch.Tensor,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -163,6 +176,23 @@ class PagedCache:
             seqs.workspace_bytes[n_heads, shared_len] = n
         return n
 
+    def _options(self, n: int, heads: int, scale: float, softcap: float, slopes, lo, hi,
+                 lse) -> B.cr_attend_options:
+        o = B.cr_attend_options(scale, softcap)
+        if slopes is not None:
+            sl = np.ascontiguousarray(slopes, dtype=np.float32)
+            if sl.shape != (heads,):
+                raise ValueError("slopes needs one entry per query head")
+            o.slopes = sl.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
+        o.lo, o.hi = self._index(lo, n, "lo"), self._index(hi, n, "hi")
+        if lse is not None:
+            if lse.dtype is not torch.float32 or lse.shape != (n, heads) or \
+                    not lse.is_contiguous() or lse.device != self.device:
+                raise TypeError(f"lse must be a contiguous fp32 [{n}, {heads}] tensor on the "
+                                "cache's device")
+            o.lse = lse.data_ptr()
+        return o
+
     def attend(self, layer: int, seqs: Sequences, q: torch.Tensor,
                out: Optional[torch.Tensor] = None, scale: float = 0.0, softcap: float = 0.0,
                slopes: Optional[Sequence[float]] = None, lo: Optional[torch.Tensor] = None,
@@ -175,20 +205,8 @@ class PagedCache:
         and lse (fp32 [n_tokens, n_heads]) are device tensors."""
         n, heads = self._tokens(seqs), q.shape[1]
         qr = self._rows(q, n, heads, "q")
-        o = B.cr_attend_options(scale, softcap)
-        if slopes is not None:
-            sl = np.ascontiguousarray(slopes, dtype=np.float32)
-            if sl.shape != (heads,):
-                raise ValueError("slopes needs one entry per query head")
-            o.slopes = sl.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
-        o.lo, o.hi = self._index(lo, n, "lo"), self._index(hi, n, "hi")
+        o = self._options(n, heads, scale, softcap, slopes, lo, hi, lse)
         o.shared_len = shared_len
-        if lse is not None:
-            if lse.dtype is not torch.float32 or lse.shape != (n, heads) or \
-                    not lse.is_contiguous() or lse.device != self.device:
-                raise TypeError(f"lse must be a contiguous fp32 [{n}, {heads}] tensor on the "
-                                "cache's device")
-            o.lse = lse.data_ptr()
         need = self._workspace_bytes(seqs, heads, shared_len)
         if workspace is not None and (workspace.device != self.device or
                                       not workspace.is_contiguous()):
@@ -209,3 +227,167 @@ class PagedCache:
 
         self._on(stream, call)
         return result
+
+    def _weights(self, seqs: Sequences, w: torch.Tensor) -> B.cr_key_weights:
+        if w.dtype is not torch.float32 or w.device != self.device:
+            raise TypeError("weights must be fp32 on the cache's device")
+        L, S, H, slots = w.shape
+        table = seqs.block_table.shape
+        if L != self.layout.n_layers or S != table[0] or H != self.n_kv_heads or \
+                slots != table[1] * self.block_size:
+            raise ValueError(f"weights: shape {tuple(w.shape)}, expected (n_layers, n_seqs, "
+                             "n_kv_heads, slots of the table)")
+        st = w.stride()
+        if slots > 1 and st[3] != 1:
+            raise ValueError("weights: the last dimension must be contiguous")
+        return B.cr_key_weights(w.data_ptr(), st[0] if L > 1 else 0, st[1] if S > 1 else 0,
+                                st[2] if H > 1 else 0)
+
+    def new_weights(self, seqs: Sequences) -> torch.Tensor:
+        """Weights for :meth:`weigh`, all 0."""
+        self._tokens(seqs)
+        S, blocks = seqs.block_table.shape
+        return torch.zeros(self.layout.n_layers, S, self.n_kv_heads, blocks * self.block_size,
+                           dtype=torch.float32, device=self.pool.device)
+
+    def weigh(self, layer: int, seqs: Sequences, q: torch.Tensor, lse: torch.Tensor,
+              weights: torch.Tensor, scale: float = 0.0, softcap: float = 0.0,
+              slopes: Optional[Sequence[float]] = None, lo: Optional[torch.Tensor] = None,
+              hi: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Adds the probabilities that the queries give each slot to weights (cr_weigh_keys):
+        fp32 [n_layers, n_seqs, n_kv_heads, slots of the table], of which the layer's part is
+        updated.  q, lse and the options are those of the call of :meth:`attend`.  workspace:
+        device scratch as cr_weigh_workspace_bytes says (None: a new one where it takes any)."""
+        n, heads = self._tokens(seqs), q.shape[1]
+        qr = self._rows(q, n, heads, "q")
+        o = self._options(n, heads, scale, softcap, slopes, lo, hi, lse)
+        w = self._weights(seqs, weights)
+        need = seqs.workspace_bytes.get((heads, "weigh"))
+        if need is None:
+            need = B.cr_weigh_workspace_bytes(self.layout, seqs.struct, heads)
+            seqs.workspace_bytes[heads, "weigh"] = need
+        if workspace is not None and (workspace.device != self.device or
+                                      not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous tensor on the cache's device")
+
+        def call(handle):
+            ws = workspace
+            if ws is None and need:
+                ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            B.cr_weigh_keys(self.pool.data_ptr(), self.layout, layer, seqs.struct, qr, heads, o, w,
+                            None if ws is None else ws.data_ptr(),
+                            0 if ws is None else ws.numel() * ws.element_size(), handle)
+
+        self._on(stream, call)
+        return weights
+
+    def _list(self, t: torch.Tensor, shape: tuple, name: str) -> int:
+        if t.dtype is not torch.int32 or t.device != self.device or t.shape != shape or \
+                not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous int32 {list(shape)} tensor on the "
+                            "cache's device")
+        return t.data_ptr()
+
+    def choose(self, seqs: Sequences, weights: torch.Tensor, budget: int, first: int = 0,
+               recent: int = 0, budgets: Optional[torch.Tensor] = None,
+               kept: Optional[torch.Tensor] = None, kept_lens: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None):
+        """The slots that stay of every layer, sequence and KV head (cr_choose_slots): kept
+        int32 [n_layers, n_seqs, n_kv_heads, budget] and kept_lens int32 [n_seqs] (None: new
+        tensors).  budgets: device int32, a sequence's own budget.  Returns (kept, kept_lens)."""
+        self._tokens(seqs)
+        w = self._weights(seqs, weights)
+        S = seqs.kv_lens.shape[0]
+        shape = (self.layout.n_layers, S, self.n_kv_heads, budget)
+        c = B.cr_choice(budget, first, recent, self._index(budgets, S, "budgets"))
+        if kept is not None:
+            self._list(kept, shape, "kept")
+        if kept_lens is not None:
+            self._index(kept_lens, S, "kept_lens")
+
+        def call(handle):
+            nonlocal kept, kept_lens
+            if kept is None:
+                kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+            if kept_lens is None:
+                kept_lens = torch.empty(S, dtype=torch.int32, device=self.device)
+            B.cr_choose_slots(self.layout, seqs.struct, w, c, kept.data_ptr(),
+                              kept_lens.data_ptr(), handle)
+
+        self._on(stream, call)
+        return kept, kept_lens
+
+    def compact(self, seqs: Sequences, kept: torch.Tensor, kept_lens: torch.Tensor,
+                weights: Optional[torch.Tensor] = None,
+                block_table: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Moves the slots that stay to the front, with their weights (cr_compact_kv): in place,
+        or into the blocks of block_table (device int32 [n_seqs][blocks]).  seqs has the lengths
+        before; kept_lens are those after."""
+        self._tokens(seqs)
+        S = seqs.kv_lens.shape[0]
+        if kept.dim() != 4:
+            raise TypeError("kept must be [n_layers, n_seqs, n_kv_heads, budget]")
+        budget = kept.shape[3]
+        k = self._list(kept, (self.layout.n_layers, S, self.n_kv_heads, budget), "kept")
+        lens = self._index(kept_lens, S, "kept_lens")
+        w = None if weights is None else self._weights(seqs, weights)
+        out, blocks = None, 0
+        if block_table is not None:
+            if block_table.dim() != 2:
+                raise TypeError("block_table must be a 2-d tensor")
+            blocks = block_table.shape[1]
+            out = self._list(block_table, (S, blocks), "block_table")
+        self._on(stream, lambda handle: B.cr_compact_kv(
+            self.pool.data_ptr(), self.layout, seqs.struct, k, budget, lens, out, blocks, w, handle))
+
+
+_SETTINGS = (("temperature", "temperatures", torch.float32), ("top_p", "top_ps", torch.float32),
+             ("min_p", "min_ps", torch.float32), ("top_k", "top_ks", torch.int32))
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+           tokens: Optional[torch.Tensor] = None, log_probs: Optional[torch.Tensor] = None,
+           stream: Optional[torch.cuda.Stream] = None):
+    """A token from every row of logits [n_rows, vocab] (bf16 or fp32, rows any distance apart)
+    by temperature, top-k, top-p and min-p and the random numbers u (fp32 [n_rows]), as cr_sample
+    says; each setting is a number for all rows or a device tensor with one per row (fp32, top_k
+    int32).  tokens int32 and log_probs fp32 [n_rows]: None = new tensors.  Returns (tokens,
+    log_probs)."""
+    if logits.dim() != 2 or logits.dtype not in _DTYPE or not logits.is_cuda:
+        raise TypeError("logits must be a bf16 or fp32 [n_rows, vocab] tensor in device memory")
+    n, vocab = logits.shape
+    dev = logits.device
+    st = logits.stride()
+    if vocab > 1 and st[1] != 1:
+        raise ValueError("logits: the last dimension must be contiguous")
+
+    def rows(t, dtype, name):
+        if t.dtype is not dtype or t.device != dev or t.shape != (n,) or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous {dtype} [{n}] tensor on the logits' device")
+        return t.data_ptr()
+
+    o = B.cr_sampling()
+    for value, (one, many, dtype) in zip((temperature, top_p, min_p, top_k), _SETTINGS):
+        if isinstance(value, torch.Tensor):
+            setattr(o, many, rows(value, dtype, one))
+        else:
+            setattr(o, one, value)
+    x = B.cr_logits(logits.data_ptr(), _DTYPE[logits.dtype], n, vocab, st[0] if n > 1 else 0)
+    numbers = rows(u, torch.float32, "u")
+    if tokens is not None:
+        rows(tokens, torch.int32, "tokens")
+    if log_probs is not None:
+        rows(log_probs, torch.float32, "log_probs")
+
+    def call(handle):
+        nonlocal tokens, log_probs
+        if tokens is None:
+            tokens = torch.empty(n, dtype=torch.int32, device=dev)
+        if log_probs is None:
+            log_probs = torch.empty(n, dtype=torch.float32, device=dev)
+        B.cr_sample(x, o, numbers, tokens.data_ptr(), log_probs.data_ptr(), handle)
+
+    _on_device(dev, stream, call)
+    return tokens, log_probs
