@@ -714,7 +714,7 @@ CR_API cr_status cr_compact_kv(void* kv, const cr_kv_layout* layout, const cr_se
  * that stay sum to more than u times their sum.
  *  logits:    device, n_rows rows of vocab logits, stride_row elements apart
  *             (>= 0); dtype CR_DTYPE_BF16 or CR_DTYPE_F32; aligned to its
- *             elements.  vocab at most 2^20.
+ *             elements.  vocab at most 2^19.
  *  options:   for all rows, or per row (device, n_rows) where the pointer is not
  *             NULL.  temperature <= 0 or NaN: the first token.  top_k <= 0 or >=
  *             vocab: no limit.  top_p >= 1: no limit; <= 0 or NaN: the first

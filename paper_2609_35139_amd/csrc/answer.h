@@ -67,7 +67,7 @@ struct CompactArgs {
 hipError_t compact(const CompactArgs& a, hipStream_t s);
 
 // ---- a token for every row of logits.
-constexpr int kMostVocab = 1 << 20;
+constexpr int kMostVocab = 1 << 19;
 struct SampleArgs {
   const void* logits;
   int64_t stride;

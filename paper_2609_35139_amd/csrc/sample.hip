@@ -21,7 +21,9 @@ namespace cr {
 
 constexpr int kSampleThreads = 512, kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleBins = 2048;
-constexpr int kSampleList = 2048;     // tokens that are sorted
+constexpr int kSampleList = 2048;     // tokens that are looked at one by one
+constexpr int kMostTopK = 256;        // top-k that a list is made for at once
+constexpr int kSampleShort = 256;     // of a list that is compared each with each
 
 typedef unsigned long long u64;
 
@@ -33,31 +35,47 @@ __device__ __forceinline__ float value_of(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// exp(d / T) 2^shift for d = x - x_0 <= 0, by t = 256 log2(e) d / T = n + r:
-// 2^(n / 256) from a table and the exponent, e^(r log 2 / 256) by its series up to
-// the fourth power (relative error 4e-17).
+// exp((x - x_0) / T) 2^shift.  With c = 64 log2(e) / T, x c - x_0 c = n + r - f: n whole,
+// |r| <= 1/2, f what x_0 c is off a whole number, the same for all tokens.  2^(n / 64)
+// comes from a table (with 2^(-f / 64) in it) and the exponent, 2^(r / 64) by its series
+// up to the fourth power (relative error 4e-14, below a step for all but the largest).
+// Products inside the fused operations are exact, so nothing is lost however far x and x_0
+// are from 0.  Ten fp64 operations, at half the rate of fp32 ones: a row of 151,936
+// logits takes a CU about 40 us.
+constexpr int kExpTable = 64;
 struct Weigher {
-  const double* table;   // 2^(j / 256) 2^shift
-  double top, c;         // 256 log2(e) / T
-  __device__ __forceinline__ double scaled(float x) const {
-    const double t = ((double)x - top) * c;
-    if (!(t >= -64. * 256.)) return 0.;
-    const double kMagic = 6755399441055744.;                 // 1.5 2^52
-    const double m = t + kMagic;
-    const int n = (int)(__double_as_longlong(m) & 0xffffffff);
-    const double y = (t - (m - kMagic)) * 0.0027076061740622863;   // log(2) / 256
-    double e = __builtin_fma(y, 1. / 24., 1. / 6.);
-    e = __builtin_fma(e, y, 0.5);
-    e = __builtin_fma(e, y, 1.);
-    e = __builtin_fma(e, y, 1.);
-    const long long b = __double_as_longlong(table[n & 255]) + ((long long)(n >> 8) << 52);
-    return __longlong_as_double(b) * e;
+  const double* table;   // 2^((j - f) / 64) 2^shift
+  double c, whole;       // whole: 1.5 2^52 less the whole number next to x_0 c
+  float lowest;          // what lies below weighs less than 2^-20 steps
+  __device__ __forceinline__ u64 operator()(float x) const {
+    x = x > lowest ? x : lowest;                      // (NaN too)
+    const double m = __builtin_fma((double)x, c, whole);
+    // (the float next to the lowest may lie further down; what it weighs is still no step)
+    const int n = max((int)(__double_as_longlong(m) & 0xffffffff), -80 * kExpTable);
+    const double r = __builtin_fma((double)x, c, whole - m);
+    constexpr double y = 0.69314718055994530942 / kExpTable;
+    double e = __builtin_fma(r, y * y * y * y / 24., y * y * y / 6.);
+    e = __builtin_fma(e, r, y * y / 2.);
+    e = __builtin_fma(e, r, y);
+    e = __builtin_fma(e, r, 1.);
+    const long long b = __double_as_longlong(table[n & (kExpTable - 1)]) +
+                        ((long long)(n & ~(kExpTable - 1)) << 46);
+    // in whole steps: added to 2^52, the bits are kOffset + the weight
+    return (u64)__double_as_longlong(__builtin_fma(__longlong_as_double(b), e, 4503599627370496.)) -
+           kOffset;
   }
-  __device__ __forceinline__ static u64 whole(double v) {      // v < 2^52, rounded
-    return (u64)__double_as_longlong(v + 4503599627370496.) & ((1ull << 52) - 1);
-  }
-  __device__ __forceinline__ u64 operator()(float x) const { return whole(scaled(x)); }
+  static constexpr u64 kOffset = 0x4330000000000000ull;
 };
+// The smallest logit whose p is at least min_p, which is that of (x - x_0) / T >=
+// log(min_p): so min_p is a bound of the logits themselves.
+__device__ __forceinline__ float least_logit(float min_p, double top, double temperature) {
+  const double t = temperature * log((double)min_p);
+  auto holds = [&](float x) { return (double)x - top >= t; };
+  float x = fmaxf((float)(top + t), -3.402823466e38f);
+  for (int i = 0; i < 4 && !holds(x); ++i) x = nextafterf(x, INFINITY);
+  for (int i = 0; i < 4 && holds(nextafterf(x, -INFINITY)); ++i) x = nextafterf(x, -INFINITY);
+  return fminf(x, (float)top);
+}
 
 // Where the tokens that stay end: those above v, and of those equal to v the ones
 // up to index `last`.
@@ -65,221 +83,337 @@ struct Cut {
   float v = -INFINITY;
   int last = -1;
   __device__ __forceinline__ bool keeps(float x, int i) const {
-    return x > v || (x == v && i <= last);
+    return (x > v) | ((x == v) & (i <= last));     // (no branches)
   }
 };
 
 struct SampleShared {
-  u64 mass[kSampleBins];
+  u64 mass[kSampleBins];                // or sums of the row's chunks
   uint32_t count[kSampleBins];
-  u64 list[kSampleList], weight[kSampleList];
-  u64 sums[kMostVocab / 256];       // of every wave's pieces of the row
-  double table[256];
+  u64 list[kSampleList], few[kSampleList], weight[kSampleShort];
+  double table[kExpTable];
   u64 scan[kSampleWaves];
   u64 word[4];
-  uint32_t n_list;
+  uint32_t n_list, n_few;
   float range[2 * kSampleWaves];
 };
 
+// A row is read in chunks of U vectors for each lane of a wave, wave w taking chunks
+// w, w + 8, ...: several where a pass only compares (its loads are what it waits
+// for), one where it forms weights.  What is done for a logit stands in the code once
+// or for one vector: a workgroup runs through most of this code once, and a line of
+// it that is not in the instruction cache takes about a microsecond (everything
+// unrolled over eight vectors: 180 KB, and 45 us for a pass that finds 360 tokens,
+// 9 now).
+constexpr int kRead = 4, kReadMost = 8;
+
 template <typename T>
 struct Sampler {
-  static constexpr int NT = kSampleThreads, VEC = 4;
+  static constexpr int NT = kSampleThreads, WAVES = kSampleWaves, VEC = 16 / sizeof(T);
+  template <int U> static constexpr int CHUNK = 64 * VEC * U;
   SampleShared& sh;
   const T* row;
   int vocab;
-  bool vectors;          // the row begins on four logits
-  bool infinite;         // the largest logit is infinite: it and its equals alone count
   Weigher weigh;
   int tid, lane, wave;
 
-  __device__ __forceinline__ int pieces() const { return (vocab + NT * VEC - 1) / (NT * VEC); }
-  __device__ __forceinline__ void load(int j, int thread, float (&x)[VEC]) const {
-    const int i = (j * NT + thread) * VEC;
-    if (vectors && i + VEC <= vocab) {
-      if constexpr (sizeof(T) == 2) {
-        const uint2 w = *reinterpret_cast<const uint2*>(row + i);
-        x[0] = __uint_as_float(w.x << 16);
-        x[1] = __uint_as_float(w.x & 0xffff0000u);
-        x[2] = __uint_as_float(w.y << 16);
-        x[3] = __uint_as_float(w.y & 0xffff0000u);
-      } else {
-        const float4 w = *reinterpret_cast<const float4*>(row + i);
-        x[0] = w.x;
-        x[1] = w.y;
-        x[2] = w.z;
-        x[3] = w.w;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = i + e < vocab ? to_f32(row[i + e]) : -INFINITY;
-    }
+  template <int U>
+  __device__ __forceinline__ int chunks() const { return (vocab + CHUNK<U> - 1) / CHUNK<U>; }
+  __device__ __forceinline__ static void elements(const uint4& w, float (&x)[VEC]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      if (!(x[e] > -INFINITY)) x[e] = -INFINITY;
-      if (infinite) x[e] = x[e] == INFINITY ? 0.f : -INFINITY;
+      if constexpr (sizeof(T) == 2)
+        x[e] = __uint_as_float(e % 2 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+      else
+        x[e] = __uint_as_float(u[e]);
     }
   }
-  // f(x, index) for this thread's logits above -inf
-  template <typename F>
-  __device__ __forceinline__ void each(F&& f) const {
-    const int n = pieces();
-#pragma unroll 1
-    for (int j = 0; j < n; ++j) {
-      float x[VEC];
-      load(j, tid, x);
+  // index of the first element of the lane's vector u of chunk c: vectors that pass
+  // the end of the row are read from its last elements, those of them that another
+  // vector holds as -inf
+  template <int U>
+  __device__ __forceinline__ int first_of(int c, int u) const {
+    return min(c * CHUNK<U> + (u * 64 + lane) * VEC, vocab - VEC);
+  }
+  template <int U>
+  __device__ __forceinline__ void load(int c, uint4 (&w)[U]) const {
+    if (vocab >= VEC) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (x[e] > -INFINITY) f(x[e], (j * NT + tid) * VEC + e);
+      for (int u = 0; u < U; ++u)
+        __builtin_memcpy(&w[u], row + first_of<U>(c, u), 16);     // (rows begin anywhere)
+      return;
     }
+    // a row shorter than a vector, element by element
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const int i = first_of<U>(c, u) + e;
+        if (i < 0) continue;
+        if constexpr (sizeof(T) == 2)
+          v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[i] << (e % 2 * 16);
+        else
+          v[e] = reinterpret_cast<const uint32_t*>(row)[i];
+      }
+      w[u] = uint4{v[0], v[1], v[2], v[3]};
+    }
+  }
+  // ... and -inf in the places of elements that another vector holds
+  template <int U>
+  __device__ __forceinline__ void clear(int c, uint4 (&w)[U]) const {
+    if ((c + 1) * CHUNK<U> <= vocab) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+      const int gone = c * CHUNK<U> + (u * 64 + lane) * VEC - first_of<U>(c, u);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        if (e >= gone) continue;
+        if constexpr (sizeof(T) == 2)
+          v[e / 2] = e % 2 ? (v[e / 2] & 0xffffu) | 0xff800000u : (v[e / 2] & 0xffff0000u) | 0xff80u;
+        else
+          v[e] = 0xff800000u;
+      }
+      w[u] = uint4{v[0], v[1], v[2], v[3]};
+    }
+  }
+  // f(chunk, its vectors) for this wave's chunks, the next one on its way meanwhile
+  template <int U, typename F>
+  __device__ __forceinline__ void each_chunk(F&& f) const {
+    const int n = chunks<U>();
+    if (wave >= n) return;
+    uint4 w[U], next[U];
+    load<U>(wave, w);
+#pragma unroll 1
+    for (int c = wave; c < n; c += WAVES) {
+      load<U>(min(c + WAVES, n - 1), next);
+      clear<U>(c, w);
+      f(c, w);
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = next[u];
+    }
+  }
+  // f(x, index) for the logits in [lo, hi] that `within` keeps: a bit for each of a
+  // lane's logits, then the lanes' bits one after the other.
+  template <typename F>
+  __device__ __forceinline__ void each_of(float lo, float hi, const Cut& within, F&& f) const {
+    each_chunk<kRead>([&](int c, const uint4 (&w)[kRead]) {
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < kRead; ++u) {
+        float x[VEC];
+        elements(w[u], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) any |= x[e] >= lo;
+      }
+      if (!__any(any)) return;
+      uint32_t bits = 0;
+#pragma unroll
+      for (int u = 0; u < kRead; ++u) {
+        float x[VEC];
+        elements(w[u], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          bits |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << (u * VEC + e);
+      }
+#pragma unroll 1
+      while (__any(bits != 0)) {
+        const int b = bits ? __ffs(bits) - 1 : 0;
+        uint32_t v = 0;
+#pragma unroll
+        for (int d = 0; d < kRead * 4; ++d) {
+          const uint32_t o = d % 4 == 0 ? w[d / 4].x : d % 4 == 1 ? w[d / 4].y : d % 4 == 2 ? w[d / 4].z : w[d / 4].w;
+          v = b * (int)sizeof(T) / 4 == d ? o : v;
+        }
+        if constexpr (sizeof(T) == 2) v = b % 2 ? v & 0xffff0000u : v << 16;
+        const float x = __uint_as_float(v);
+        const int i = first_of<kRead>(c, b / VEC) + b % VEC;
+        if (bits && within.keeps(x, i)) f(x, i);
+        bits &= bits - 1;
+      }
+    });
+  }
+  // the weights of a vector, all of them at once (each is a chain of dependent
+  // instructions)
+  __device__ __forceinline__ void form(const float (&x)[VEC], u64 (&q)[VEC]) const {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) q[e] = weigh(x[e]);
+  }
+  // all bits, or none (selected by bits, a value is loaded whether it is needed or not,
+  // and loads do not wait for each other's conditions)
+  __device__ __forceinline__ static u64 when(bool c) { return 0 - (u64)c; }
+  // (v of the lane that the data-parallel control names; 0 where there is none)
+  template <int CTRL, int ROWS = 0xf>
+  __device__ __forceinline__ static u64 lane_of(u64 v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)hi << 32 | lo;
+  }
+  // sum over the lanes up to this one within 16, then within the wave
+  __device__ __forceinline__ static u64 row_upto(u64 v) {
+    v += lane_of<0x111>(v);               // row_shr:1, 2, 4, 8
+    v += lane_of<0x112>(v);
+    v += lane_of<0x114>(v);
+    v += lane_of<0x118>(v);
+    return v;
+  }
+  __device__ __forceinline__ static u64 wave_upto(u64 v) {
+    v = row_upto(v);
+    v += lane_of<0x142, 0xa>(v);          // row_bcast:15 into rows 1 and 3
+    v += lane_of<0x143, 0xc>(v);          // row_bcast:31 into rows 2 and 3
+    return v;
+  }
+  __device__ __forceinline__ static u64 at_lane(u64 v, int l) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, l);
   }
   // sum of v over the threads before this one, and over all
-  __device__ __forceinline__ u64 before(u64 v, u64* total) {
-    u64 x = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const u64 y = __shfl_up(x, o);
-      if (lane >= o) x += y;
-    }
+  __device__ __forceinline__ u64 before(u64 v, u64* total) const {
+    static_assert(WAVES <= 16, "a row of lanes");
+    const u64 upto = wave_upto(v);
     __syncthreads();
-    if (lane == 63) sh.scan[wave] = x;
+    if (lane == 63) sh.scan[wave] = upto;
     __syncthreads();
-    u64 b = x - v, t = 0;
-    for (int i = 0; i < kSampleWaves; ++i) {
-      if (i < wave) b += sh.scan[i];
-      t += sh.scan[i];
-    }
-    *total = t;
-    return b;
+    const u64 w = row_upto(lane < WAVES ? sh.scan[lane] : 0);
+    *total = at_lane(w, WAVES - 1);
+    return upto - v + (wave > 0 ? at_lane(w, wave - 1) : 0);
   }
-  __device__ __forceinline__ u64 all(u64 v) {
+  __device__ __forceinline__ u64 all(u64 v) const {
     u64 t;
     before(v, &t);
     return t;
-  }
-  // the n entries of the list in descending order
-  __device__ __forceinline__ void sort(u64* list, int n) {
-    int size = 2;
-    while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += NT) list[i] = 0;
-    for (int k = 2; k <= size; k *= 2)
-      for (int d = k / 2; d > 0; d /= 2) {
-        __syncthreads();
-        for (int p = tid; p < size / 2; p += NT) {
-          const int i = ((p & ~(d - 1)) << 1) | (p & (d - 1));
-          const u64 a = list[i], b = list[i + d];
-          if ((a < b) == ((i & k) == 0)) { list[i] = b; list[i + d] = a; }
-        }
-      }
-    __syncthreads();
   }
   __device__ __forceinline__ static u64 entry(float x, int i) {
     return (u64)order_of(x) << 32 | (0xffffffffu - (uint32_t)i);
   }
   __device__ __forceinline__ static float entry_value(u64 e) { return value_of((uint32_t)(e >> 32)); }
   __device__ __forceinline__ static int entry_index(u64 e) { return (int)(0xffffffffu - (uint32_t)e); }
-  // tokens that f accepts, in the list; more than it holds are only counted
+  // the tokens in [lo, hi] that `within` keeps and f accepts, in the list; more than it
+  // holds are only counted
   template <typename F>
-  __device__ __forceinline__ uint32_t collect(F&& f) {
+  __device__ __forceinline__ uint32_t collect(float lo, float hi, const Cut& within, F&& f) const {
     __syncthreads();
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    each([&](float x, int i) {
-      if (!f(x, i)) return;
+    each_of(lo, hi, within, [&](float x, int i) {
+      if (!f(x)) return;
       const uint32_t at = atomicAdd(&sh.n_list, 1u);
       if (at < (uint32_t)kSampleList) sh.list[at] = entry(x, i);
     });
     __syncthreads();
     return sh.n_list;
   }
-
-  // ---- the cut behind which less than `need` (of tokens, or of weight) stands
-  // before a token, among those that `within` keeps.  The values' range is cut into
-  // bins, the bin that holds the cut becomes the range, until its tokens fit the
-  // list or are all equal.
+  // ---- bins: of values from hi down, in `count` and (weights) `mass`
   // (in 64 bits: no difference of two logits overflows or vanishes)
   __device__ __forceinline__ static int bin_of(float x, float hi, double scale) {
     return min(kSampleBins - 1, (int)(((double)hi - (double)x) * scale));
   }
-  __device__ Cut cut(bool by_weight, u64 need, float lo, float hi, const Cut& within) {
-    u64 above = 0;
-    for (;;) {
-      const double scale = hi > lo ? (double)(kSampleBins - 1) / ((double)hi - (double)lo) : 0.;
-      for (int i = tid; i < kSampleBins; i += NT) { sh.mass[i] = 0; sh.count[i] = 0; }
-      __syncthreads();
-      each([&](float x, int i) {
-        if (!(x >= lo && x <= hi && within.keeps(x, i))) return;
-        const int b = bin_of(x, hi, scale);
-        atomicAdd(&sh.count[b], 1u);
-        if (by_weight) atomicAdd(&sh.mass[b], weigh(x));
-      });
-      __syncthreads();
-      constexpr int PER = kSampleBins / NT;
-      u64 mine = 0;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) mine += by_weight ? sh.mass[tid * PER + i] : sh.count[tid * PER + i];
-      u64 total;
-      u64 at = above + before(mine, &total);
-      if (at < need && at + mine >= need) {
-        for (int i = 0; i < PER; ++i) {
-          const u64 c = by_weight ? sh.mass[tid * PER + i] : sh.count[tid * PER + i];
-          if (at + c >= need) {
-            sh.word[0] = tid * PER + i;
-            sh.word[1] = at;
-            break;
-          }
-          at += c;
-        }
-      } else if (tid == 0 && above + total < need) {      // all of them stay
-        sh.word[0] = kSampleBins;
-      }
-      __syncthreads();
-      const int bin = (int)sh.word[0];
-      if (bin >= kSampleBins) return within;
-      above = sh.word[1];
-      auto inside = [&](float x, int i) {
-        return x >= lo && x <= hi && within.keeps(x, i) && bin_of(x, hi, scale) == bin;
-      };
-      const uint32_t n = sh.count[bin];
-      __syncthreads();
-      if (n <= (uint32_t)kSampleList) {
-        collect(inside);
-        sort(sh.list, (int)n);
-        u64 w[kSampleList / NT], sum = 0;
-#pragma unroll
-        for (int i = 0; i < kSampleList / NT; ++i) {
-          const int p = tid * (kSampleList / NT) + i;
-          w[i] = p >= (int)n ? 0 : by_weight ? weigh(entry_value(sh.list[p])) : 1;
-          sum += w[i];
-        }
-        u64 b = above + before(sum, &total);
-#pragma unroll
-        for (int i = 0; i < kSampleList / NT; ++i) {
-          const int p = tid * (kSampleList / NT) + i;
-          // the last one with less than `need` before it
-          if (p < (int)n && b < need && (b + w[i] >= need || p == (int)n - 1)) sh.word[2] = sh.list[p];
-          b += w[i];
-        }
-        __syncthreads();
-        const u64 e = sh.word[2];
-        __syncthreads();
-        return Cut{entry_value(e), entry_index(e)};
-      }
-      float least = INFINITY, most = -INFINITY;
-      each([&](float x, int i) {
-        if (inside(x, i)) { least = fminf(least, x); most = fmaxf(most, x); }
-      });
-      reduce_range(least, most);
-      if (least == most) {
-        // equal ones: the first of them, by index
-        const u64 w = by_weight ? weigh(most) : 1;
-        const u64 take = (need - above + w - 1) / w;
-        return Cut{most, index_of_equal(most, take, within)};
-      }
-      lo = least;
-      hi = most;
-    }
+  __device__ __forceinline__ static double scale_of(float lo, float hi) {
+    return hi > lo ? (double)(kSampleBins - 1) / ((double)hi - (double)lo) : 0.;
   }
-  __device__ __forceinline__ void reduce_range(float& least, float& most) {
+  // the values that bins from `first` to `last` may hold
+  __device__ __forceinline__ static float2 values_of(int first, int last, float lo, float hi, double scale) {
+    if (!(scale > 0.)) return float2{lo, hi};
+    return float2{fmaxf(lo, (float)((double)hi - (double)(last + 2) / scale)),
+                  first > 0 ? (float)((double)hi - (double)(first - 1) / scale) : hi};
+  }
+  __device__ __forceinline__ void clear_bins() const {
+    __syncthreads();
+    for (int i = tid; i < kSampleBins; i += NT) { sh.mass[i] = 0; sh.count[i] = 0; }
+    __syncthreads();
+  }
+  // The bin in which the running sum (of tokens, or of weight), from `above` on, reaches
+  // `need`; what stands before it; the tokens up to its end.  bin kSampleBins: none does.
+  struct Found { int bin; u64 above; uint32_t tokens; };
+  __device__ __forceinline__ Found find(bool by_weight, u64 need, u64 above) const {
+    constexpr int PER = kSampleBins / NT;
+    __syncthreads();
+    u64 c[PER], mine = 0, total;
+    uint32_t tokens = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t n = sh.count[tid * PER + i];
+      c[i] = by_weight ? sh.mass[tid * PER + i] : n;
+      mine += c[i];
+      tokens += n;
+    }
+    u64 at = above + before(mine, &total), all;
+    uint32_t upto = (uint32_t)before(tokens, &all);
+    if (tid == 0) sh.word[0] = kSampleBins;
+    __syncthreads();
+    if (at < need && at + mine >= need) {
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (found) continue;
+        upto += sh.count[tid * PER + i];
+        found = at + c[i] >= need;
+        if (found) sh.word[0] = tid * PER + i;
+        else at += c[i];
+      }
+      sh.word[1] = at;
+      sh.word[2] = upto;
+    }
+    __syncthreads();
+    return Found{(int)sh.word[0], sh.word[1], (uint32_t)sh.word[2]};
+  }
+  // Of the n entries of `few`, the one up to which, in descending order and from `above`
+  // on, the sum reaches `need` (the last one if none does).
+  __device__ __forceinline__ u64 pick(bool by_weight, int n, u64 need, u64 above) const {
+    __syncthreads();
+    // (their weights lie in `mass`: the bins have been looked at)
+    for (int p = tid; p < n; p += NT) sh.mass[p] = by_weight ? weigh(entry_value(sh.few[p])) : 1;
+    __syncthreads();
+    for (int p = tid; p < n; p += NT) {
+      const u64 e = sh.few[p];
+      u64 b = above;
+      bool last = true;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const u64 o = sh.few[i];
+        b += sh.mass[i] & when(o > e);
+        last &= o >= e;
+      }
+      const u64 w = sh.mass[p];
+      if (b < need && (b + w >= need || last)) sh.word[3] = e;
+    }
+    __syncthreads();
+    return sh.word[3];
+  }
+
+  // The bins of [lo, hi] of the tokens that `within` keeps; returns the weight of all of
+  // those, of any value, where by_weight.
+  __device__ __forceinline__ u64 bins(bool by_weight, float lo, float hi, const Cut& within) const {
+    const double scale = scale_of(lo, hi);
+    clear_bins();
+    u64 sum = 0;
+    each_chunk<1>([&](int c, const uint4 (&w)[1]) {
+      float x[VEC];
+      u64 q[VEC];
+      elements(w[0], x);
+      if (by_weight) {
+        form(x, q);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) q[e] = 0;
+      }
+      const int i = first_of<1>(c, 0);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const bool kept = within.keeps(x[e], i + e);
+        sum += q[e] & when(kept);
+        if (kept & (x[e] >= lo) & (x[e] <= hi)) {
+          const int b = bin_of(x[e], hi, scale);
+          atomicAdd(&sh.count[b], 1u);
+          if (by_weight) atomicAdd(&sh.mass[b], q[e]);
+        }
+      }
+    });
+    return all(sum);
+  }
+  __device__ __forceinline__ void reduce_range(float& least, float& most) const {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       least = fminf(least, __shfl_xor(least, o));
@@ -288,71 +422,66 @@ struct Sampler {
     __syncthreads();
     if (lane == 0) { sh.range[wave] = least; sh.range[kSampleWaves + wave] = most; }
     __syncthreads();
-    for (int i = 0; i < kSampleWaves; ++i) {
-      least = fminf(least, sh.range[i]);
-      most = fmaxf(most, sh.range[kSampleWaves + i]);
+    least = sh.range[lane % kSampleWaves];
+    most = sh.range[kSampleWaves + lane % kSampleWaves];
+#pragma unroll
+    for (int o = kSampleWaves / 2; o > 0; o >>= 1) {
+      least = fminf(least, __shfl_xor(least, o));
+      most = fmaxf(most, __shfl_xor(most, o));
     }
   }
 
-  // ---- pieces of the row in order: wave w's part of piece j is entry j * waves +
-  // w of sums.  The index of the token in which the running sum of f passes `target`
-  // (the first with more than `target` up to it), of f's values given the sums.
+  // ---- the row in order: the sum of f over every chunk, and the token up to which
+  // f first sums to more than `target`, given those sums.  f(logits of a vector, index
+  // of the first, their shares).
   template <typename F>
-  __device__ __forceinline__ u64 sum_pieces(F&& f) {
-    const int n = pieces();
+  __device__ __forceinline__ u64 sum_chunks(F&& f) const {
     __syncthreads();
     u64 mine = 0;
-#pragma unroll 1
-    for (int j = 0; j < n; ++j) {
+    each_chunk<1>([&](int c, const uint4 (&w)[1]) {
       float x[VEC];
-      load(j, tid, x);
-      u64 t = 0;
+      u64 q[VEC], t = 0;
+      elements(w[0], x);
+      f(x, first_of<1>(c, 0), q);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (x[e] > -INFINITY) t += f(x[e], (j * NT + tid) * VEC + e);
+      for (int e = 0; e < VEC; ++e) t += q[e];
       mine += t;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-      if (lane == 0) sh.sums[j * kSampleWaves + wave] = t;
-    }
+      t = wave_upto(t);
+      if (lane == 63) sh.mass[c] = t;
+    });
     return all(mine);
   }
   template <typename F>
-  __device__ __forceinline__ int locate(u64 target, F&& f) {
-    const int n = pieces() * kSampleWaves, per = (n + NT - 1) / NT;
+  __device__ __forceinline__ int locate(u64 target, F&& f) const {
+    static_assert(kMostVocab / (64 * VEC) <= kSampleBins || VEC < 8, "sums");
+    const int n = chunks<1>(), per = (n + NT - 1) / NT;
     u64 mine = 0, total;
-    for (int i = tid * per; i < min(n, tid * per + per); ++i) mine += sh.sums[i];
+    for (int i = tid * per; i < min(n, tid * per + per); ++i) mine += sh.mass[i];
     u64 at = before(mine, &total);
     if (at <= target && at + mine > target) {
       int i = tid * per;
-      while (at + sh.sums[i] <= target) at += sh.sums[i++];
+      while (at + sh.mass[i] <= target) at += sh.mass[i++];
       sh.word[0] = i;
       sh.word[1] = at;
     }
     __syncthreads();
-    const int p = (int)sh.word[0];
-    at = sh.word[1];
     if (wave == 0) {
-      const int j = p / kSampleWaves, thread = p % kSampleWaves * 64 + lane;
+      const int c = (int)sh.word[0], i = first_of<1>(c, 0);
+      uint4 w[1];
       float x[VEC];
-      load(j, thread, x);
-      u64 w[VEC], t = 0;
+      u64 q[VEC], t = 0;
+      load<1>(c, w);
+      clear<1>(c, w);
+      elements(w[0], x);
+      f(x, i, q);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) t += q[e];
+      const u64 incl = wave_upto(t);
+      u64 b = sh.word[1] + incl - t;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        w[e] = x[e] > -INFINITY ? f(x[e], (j * NT + thread) * VEC + e) : 0;
-        t += w[e];
-      }
-      u64 incl = t;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const u64 y = __shfl_up(incl, o);
-        if (lane >= o) incl += y;
-      }
-      u64 b = at + incl - t;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        if (b <= target && b + w[e] > target) sh.word[2] = (j * NT + thread) * VEC + e;
-        b += w[e];
+        if (b <= target && b + q[e] > target) sh.word[2] = i + e;
+        b += q[e];
       }
     }
     __syncthreads();
@@ -360,9 +489,13 @@ struct Sampler {
     __syncthreads();
     return r;
   }
-  __device__ __forceinline__ int index_of_equal(float v, u64 take, const Cut& within) {
-    auto one = [&](float x, int i) -> u64 { return x == v && within.keeps(x, i); };
-    sum_pieces(one);
+  // the take-th token, by index, of those equal to v that `within` keeps
+  __device__ __forceinline__ int index_of_equal(float v, u64 take, const Cut& within) const {
+    auto one = [&](const float (&x)[VEC], int i, u64 (&q)[VEC]) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) q[e] = x[e] == v && within.keeps(x[e], i + e);
+    };
+    sum_chunks(one);
     return locate(take - 1, one);
   }
   // less than this stands before a token that top-p lets stay
@@ -374,68 +507,130 @@ struct Sampler {
     return t > 0. ? min((u64)t, total - 1) : 0;
   }
 
-  // ---- everything on a list of the first n tokens (all that may stay).  total: the
-  // weight that top-p is a share of (0: that of the first k of the list).
-  __device__ void from_list(int n, u64 k, float top_p, double min_weight, u64 total, float u,
-                            int* token, u64* token_weight, u64* kept_weight) {
-    constexpr int PER = kSampleList / NT;
-    sort(sh.list, n);
-    if (k > 0 && k < (u64)n) n = (int)k;
-    u64 w[PER], sum = 0, all_of_list;
-    bool large[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int p = tid * PER + i;
-      const double v = p < n ? weigh.scaled(entry_value(sh.list[p])) : 0.;
-      w[i] = Weigher::whole(v);
-      large[i] = p < n && (p == 0 || v >= min_weight);
-      sum += w[i];
-    }
-    u64 b = before(sum, &all_of_list);
-    const u64 share = top_p < 1.f ? share_of(top_p, total ? total : all_of_list) : ~0ull;
-    uint32_t stay = 0;
-    u64 weight = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int p = tid * PER + i;
-      if (large[i] && (p == 0 || b < share)) {
-        ++stay;
-        weight += w[i];
+  // ---- everything on a list of the first n tokens (all that may stay).  of: the weight
+  // that top-p is a share of (0: that of the first k of the list).  Returns the entry
+  // drawn.
+  __device__ __forceinline__ u64 from_list(int n, u64 k, float top_p, float least, u64 of, float u,
+                                           u64* kept_weight) const {
+    return n <= kSampleShort ? from_short_list(n, k, top_p, least, of, u, kept_weight)
+                             : from_long_list(n, k, top_p, least, of, u, kept_weight);
+  }
+  // each entry compared with each
+  __device__ __forceinline__ u64 from_short_list(int n, u64 k, float top_p, float least, u64 of,
+                                                 float u, u64* kept_weight) const {
+    static_assert(kSampleList <= kSampleBins, "weights of `few`");
+    static_assert(kSampleShort <= NT, "an entry for each thread");
+    const bool mine = tid < n;
+    const u64 e = mine ? sh.list[tid] : 0;
+    u64 q = mine ? weigh(entry_value(e)) : 0;
+    if (mine) sh.weight[tid] = q;
+    __syncthreads();
+    u64 b = 0;
+    uint32_t rank = 0;
+    if (mine) {
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const bool better = sh.list[i] > e;
+        b += sh.weight[i] & when(better);
+        rank += better;
       }
-      b += w[i];
     }
-    const int kept = (int)all(stay);
-    const u64 kept_sum = all(weight);
-    // by index: the entries of those that stay, turned around
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int p = tid * PER + i;
-      if (p < kept) sh.weight[p] = (u64)(uint32_t)sh.list[p] << 32 | (uint32_t)p;
+    const bool within = mine && (k == 0 || rank < k);
+    if (of == 0) of = all(within ? q : 0);
+    const u64 share = top_p < 1.f ? share_of(top_p, of) : ~0ull;
+    const bool stays = within && (rank == 0 || (b < share && entry_value(e) >= least));
+    q = stays ? q : 0;
+    __syncthreads();
+    if (mine) sh.weight[tid] = q;
+    const u64 kept = all(q);
+    const u64 target = target_of(u, kept);
+    if (stays) {
+      u64 at = 0;                          // of lower indexes: larger lower halves
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) at += sh.weight[i] & when((uint32_t)sh.list[i] > (uint32_t)e);
+      if (at <= target && at + q > target) sh.word[3] = e;
     }
     __syncthreads();
-    sort(sh.weight, kept);                 // (descending in ~index: ascending in index)
-    u64 q[PER];
-    sum = 0;
+    *kept_weight = kept;
+    return sh.word[3];
+  }
+  // by bins of the values, then by bins of the indexes
+  __device__ __forceinline__ u64 from_long_list(int n, u64 k, float top_p, float least, u64 of,
+                                                float u, u64* kept_weight) const {
+    constexpr int PER = kSampleList / NT;
+    u64 e[PER], q[PER];
+    float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int p = tid * PER + i;
-      q[i] = p < kept ? weigh(entry_value(sh.list[(uint32_t)sh.weight[p]])) : 0;
-      sum += q[i];
+      e[i] = tid + i * NT < n ? sh.list[tid + i * NT] : 0;
+      const float x = entry_value(e[i]);
+      q[i] = e[i] ? weigh(x) : 0;
+      if (e[i]) { lo = fminf(lo, x); hi = fmaxf(hi, x); }
     }
-    u64 t;
-    u64 at = before(sum, &t);
-    const u64 target = target_of(u, kept_sum);
+    reduce_range(lo, hi);
+    const double scale = scale_of(lo, hi);
+    // the last entry that stays by `need`: those below it lose their weight
+    auto cut_at = [&](bool by_weight, u64 need) {
+      clear_bins();
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int p = tid * PER + i;
-      if (at <= target && at + q[i] > target) sh.word[3] = sh.list[(uint32_t)sh.weight[p]];
-      at += q[i];
+      for (int i = 0; i < PER; ++i)
+        if (e[i]) {
+          const int b = bin_of(entry_value(e[i]), hi, scale);
+          atomicAdd(&sh.count[b], 1u);
+          atomicAdd(&sh.mass[b], q[i]);
+        }
+      if (tid == 0) sh.n_few = 0;
+      const Found f = find(by_weight, need, 0);
+      if (f.bin >= kSampleBins) return;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (e[i] && bin_of(entry_value(e[i]), hi, scale) == f.bin) sh.few[atomicAdd(&sh.n_few, 1u)] = e[i];
+      __syncthreads();
+      const u64 last = pick(by_weight, (int)sh.n_few, need, f.above);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (e[i] < last) e[i] = q[i] = 0;
+    };
+    auto sum = [&] {
+      u64 t = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) t += q[i];
+      return all(t);
+    };
+    if (k > 0 && k < (u64)n) cut_at(false, k);
+    if (top_p < 1.f) cut_at(true, share_of(top_p, of ? of : sum()));
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (e[i] && entry_value(e[i]) < least) e[i] = q[i] = 0;
+    const u64 kept = sum();
+    // bins of 2^s indexes
+    const u64 target = target_of(u, kept);
+    int s = 0;
+    while (((vocab - 1) >> s) >= kSampleBins) ++s;
+    clear_bins();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (e[i]) atomicAdd(&sh.mass[entry_index(e[i]) >> s], q[i]);
+    if (tid == 0) sh.n_few = 0;
+    const Found f = find(true, target + 1, 0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (e[i] && (entry_index(e[i]) >> s) == f.bin) sh.few[atomicAdd(&sh.n_few, 1u)] = e[i];
+    __syncthreads();
+    // (of lower indexes: larger lower halves)
+    const int m = (int)sh.n_few;
+    for (int p = tid; p < m; p += NT) sh.mass[p] = weigh(entry_value(sh.few[p]));
+    __syncthreads();
+    for (int p = tid; p < m; p += NT) {
+      const u64 o = sh.few[p];
+      u64 at = f.above;
+#pragma unroll 8
+      for (int i = 0; i < m; ++i) at += sh.mass[i] & when((uint32_t)sh.few[i] > (uint32_t)o);
+      if (at <= target && at + sh.mass[p] > target) sh.word[3] = o;
     }
     __syncthreads();
-    const u64 e = sh.word[3];
-    *token = entry_index(e);
-    *token_weight = order_of(entry_value(e));
-    *kept_weight = kept_sum;
+    *kept_weight = kept;
+    return sh.word[3];
   }
 };
 
@@ -443,106 +638,207 @@ template <typename T>
 __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   __shared__ SampleShared sh;
   using S = Sampler<T>;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float temperature = a.temperatures ? a.temperatures[r] : a.temperature;
   const float top_p = a.top_ps ? a.top_ps[r] : a.top_p;
   const float min_p = a.min_ps ? a.min_ps[r] : a.min_p;
   const int k_in = a.top_ks ? a.top_ks[r] : a.top_k;
   const float u = a.u[r];
-  S s{sh, static_cast<const T*>(a.logits) + (int64_t)r * a.stride, a.vocab, false, false, Weigher{},
-      tid, lane, wave};
-  s.vectors = reinterpret_cast<uintptr_t>(s.row) % (4 * sizeof(T)) == 0;
+  S s{sh, static_cast<const T*>(a.logits) + (int64_t)r * a.stride, a.vocab, Weigher{}, tid, lane, wave};
   const int shift = a.vocab <= (1 << 18) ? 44 : 42;
-  if (tid < 256) sh.table[tid] = ldexp(exp2((double)tid / 256.), shift);
+  // (a NaN among the settings leaves the first token)
+  const bool greedy = !(temperature > 0.f) || k_in == 1 || !(top_p > 0.f) || !(min_p <= 1.f);
 
-  // ---- the largest and the smallest logit; this thread's largest
-  float most = -INFINITY, least = INFINITY;
-  int at = 0x7fffffff;
-  s.each([&](float x, int i) {
-    if (x > most) { most = x; at = i; }
-    least = fminf(least, x);
-  });
-  const float mine = most;
-  u64 best = most > -INFINITY ? S::entry(most, at) : 0;
+  // ---- the largest logit, of each thread (and the chunk where it first stands) and of
+  // all
+  float mine = -INFINITY;
+  int where = 0;
+  s.template each_chunk<kReadMost>([&](int c, const uint4 (&w)[kReadMost]) {
+    float most = mine;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const u64 y = __shfl_xor(best, o);
-    best = y > best ? y : best;
-  }
-  if (lane == 0) sh.list[wave] = best;
-  s.reduce_range(least, most);
-  for (int i = 0; i < kSampleWaves; ++i) best = sh.list[i] > best ? sh.list[i] : best;
-  __syncthreads();
+    for (int v = 0; v < kReadMost; ++v) {
+      float x[S::VEC];
+      S::elements(w[v], x);
+#pragma unroll
+      for (int e = 0; e < S::VEC; ++e) most = x[e] > most ? x[e] : most;
+    }
+    where = most > mine ? c : where;
+    mine = most;
+  });
+  float low = mine > -INFINITY ? mine : INFINITY, top = mine;
+  s.reduce_range(low, top);
   auto answer = [&](int token, float log_p) {
     if (tid != 0) return;
     a.tokens[r] = token;
     if (a.log_probs) a.log_probs[r] = log_p;
   };
-  if (best == 0) return answer(-1, -INFINITY);
-  // (a NaN among the settings leaves the first token)
-  if (!(temperature > 0.f) || k_in == 1 || !(top_p > 0.f) || !(min_p <= 1.f))
-    return answer(S::entry_index(best), 0.f);
-  s.infinite = most == INFINITY;
-  const float top = s.infinite ? 0.f : most;
-  if (s.infinite) least = 0.f;
-  s.weigh = Weigher{sh.table, (double)top, 256. * 1.4426950408889634074 / (double)temperature};
+  if (top == -INFINITY) return answer(-1, -INFINITY);
+  if (greedy) {
+    int first = 0x7fffffff;
+    if (mine == top) {
+      uint4 w[kReadMost];
+      s.template load<kReadMost>(where, w);
+      s.template clear<kReadMost>(where, w);
+#pragma unroll
+      for (int v = kReadMost - 1; v >= 0; --v) {
+        float x[S::VEC];
+        S::elements(w[v], x);
+#pragma unroll
+        for (int e = S::VEC - 1; e >= 0; --e)
+          if (x[e] == top) first = s.template first_of<kReadMost>(where, v) + e;
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o));
+    __syncthreads();
+    if (lane == 0) sh.count[wave] = (uint32_t)first;
+    __syncthreads();
+    for (int i = 0; i < kSampleWaves; ++i) first = min(first, (int)sh.count[i]);
+    return answer(first, 0.f);
+  }
   const u64 k = k_in <= 0 || k_in >= a.vocab ? 0 : (u64)k_in;
-  const double one = ldexp(1., shift), min_weight = min_p > 0.f ? (double)min_p * one : 0.;
+  const double c = kExpTable * 1.4426950408889634074 / (double)temperature, at_top = top * c;
+  if (top == INFINITY || !(fabs(at_top) < 0x1p48)) {
+    // infinite ones, or so far from 0 that any other logit is too far from them: all of
+    // the same weight
+    auto equal = [&](const float (&x)[S::VEC], int, u64 (&q)[S::VEC]) {
+#pragma unroll
+      for (int e = 0; e < S::VEC; ++e) q[e] = x[e] == top;
+    };
+    const u64 n = s.sum_chunks(equal);
+    u64 m = k > 0 && k < n ? k : n;
+    if (top_p < 1.f) m = S::share_of(top_p, m);
+    return answer(s.locate(S::target_of(u, m), equal), -logf((float)m));
+  }
+  const double one = ldexp(1., shift);
+  {
+    const double next = rint(at_top), off = (at_top - next) + __builtin_fma((double)top, c, -at_top);
+    if (tid < kExpTable) sh.table[tid] = exp2((tid - off) / kExpTable) * one;
+    s.weigh = Weigher{sh.table, c, 6755399441055744. - next,
+                      fmaxf((float)((double)top - 64. * kExpTable / c), -3.402823466e38f)};
+  }
   auto finish = [&](int token, float x, u64 total) {
     answer(token, (float)(((double)x - (double)top) / (double)temperature - log((double)total / one)));
   };
+  // no token below `least` can stay by min_p
+  constexpr float kLowest = -3.402823466e38f;
+  const float least = min_p > 0.f ? least_logit(min_p, top, temperature) : kLowest;
+  __syncthreads();                         // (the table)
 
-  // ---- few tokens can stay: a list
+  // ---- the tokens that may stay, where they are few enough for the list: all of them,
+  // those from the k-th largest of the threads' largest on (at least k tokens are not
+  // below it), those from `least` on
   int n_list = -1;
+  u64 of = 0;                              // the weight of all, where top-p needs it
+  Cut cut;                                 // where those that stay end
+  float bound = INFINITY;
   if (a.vocab <= kSampleList) {
-    n_list = (int)s.collect([](float, int) { return true; });
-  } else if (k > 0 && k <= 512 && !s.infinite) {
-    // the k-th largest of the threads' largest: at least k tokens are not below it.
-    // lo: a bound that k threads reach
-    uint32_t lo = 0, hi = order_of(most);
-    const uint32_t key = order_of(mine);
-    for (int i = 0; i < 20 && lo < hi; ++i) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      const u64 c = s.all(key >= mid && mine > -INFINITY);
-      if (c >= k) {
-        lo = mid;
-        if (c == k) break;
-      } else {
-        hi = mid - 1;
-      }
+    bound = kLowest;
+  } else if (k > 0 && k <= (u64)kMostTopK) {
+    const double scale = S::scale_of(low, top);
+    s.clear_bins();
+    const int bin = mine > -INFINITY ? S::bin_of(mine, top, scale) : kSampleBins;
+    if (bin < kSampleBins) atomicAdd(&sh.count[bin], 1u);
+    const auto f = s.find(false, k, 0);
+    if (f.bin < kSampleBins) {
+      float most = top;
+      bound = bin <= f.bin ? mine : top;
+      s.reduce_range(bound, most);
     }
-    const uint32_t n = s.collect([&](float x, int) { return order_of(x) >= lo; });
+  } else if (k == 0 && top_p >= 1.f && min_p > 0.f) {
+    bound = least;
+  }
+  if (bound < INFINITY) {
+    const uint32_t n = s.collect(bound, top, Cut{}, [](float) { return true; });
     if (n <= (uint32_t)kSampleList) n_list = (int)n;
   }
-  int token;
-  u64 value, total;
+  // ---- else where the first k end, then where top-p ends: by bins of the values, from a
+  // bound down to which they are likely to lie (about one in 50 tokens is not below the
+  // least of the threads' largest), or below which no token can stay (all of them together weigh less than 1 - top_p); the bin in which
+  // the end lies becomes the range, until its tokens fit the list or are all equal
+#pragma unroll 1
+  for (int stage = 0; stage < 2; ++stage) {
+    const bool by_weight = stage == 1;
+    if (n_list >= 0 || (by_weight ? !(top_p < 1.f) : k == 0)) continue;
+    const Cut within = cut;
+    float lo = fmaxf(kLowest, by_weight ? top + temperature * (logf((1.f - top_p) / (float)a.vocab) - 0.01f)
+                                        : k * 100 <= (u64)a.vocab ? low : low - (top - low));
+    float hi = top;
+    u64 need = k, above = 0;
+#pragma unroll 1
+    for (bool first = true;; first = false) {
+      const u64 sum = s.bins(by_weight, lo, hi, within);
+      if (by_weight && first) {
+        of = sum;
+        need = S::share_of(top_p, of);
+      }
+      const auto f = s.find(by_weight, need, above);
+      if (f.bin >= kSampleBins) {
+        if (by_weight || lo == kLowest) break;         // all of them stay
+        lo = kLowest;
+        continue;
+      }
+      const double scale = S::scale_of(lo, hi);
+      const bool whole = hi == top && f.tokens <= (uint32_t)kSampleList;   // all up to the end
+      const uint32_t n = sh.count[f.bin];
+      const float2 v = S::values_of(whole ? 0 : f.bin, f.bin, lo, hi, scale);
+      if (whole || n <= (uint32_t)kSampleList) {
+        const int from = whole ? 0 : f.bin;
+        const uint32_t got = s.collect(v.x, v.y, within, [&](float x) {
+          const int b = S::bin_of(x, hi, scale);
+          return b >= from && b <= f.bin && x >= lo && x <= hi;
+        });
+        if (whole) {
+          n_list = (int)got;
+          break;
+        }
+        for (int p = tid; p < (int)n; p += S::NT) sh.few[p] = sh.list[p];
+        const u64 e = s.pick(by_weight, (int)n, need, f.above);
+        cut = Cut{S::entry_value(e), S::entry_index(e)};
+        break;
+      }
+      float least_here = INFINITY, most_here = -INFINITY;
+      s.each_of(v.x, v.y, within, [&](float x, int) {
+        if (S::bin_of(x, hi, scale) == f.bin) {
+          least_here = fminf(least_here, x);
+          most_here = fmaxf(most_here, x);
+        }
+      });
+      s.reduce_range(least_here, most_here);
+      if (least_here == most_here) {
+        // equal ones: the first of them, by index
+        const u64 w = by_weight ? s.weigh(most_here) : 1;
+        cut = Cut{most_here, s.index_of_equal(most_here, (need - f.above + w - 1) / w, within)};
+        break;
+      }
+      lo = least_here;
+      hi = most_here;
+      above = f.above;
+    }
+  }
+  u64 total;
   if (n_list >= 0) {
-    s.from_list(n_list, k, top_p, min_weight, 0, u, &token, &value, &total);
-    return finish(token, value_of((uint32_t)value), total);
+    const u64 e = s.from_list(n_list, k, top_p, least, of, u, &total);
+    return finish(S::entry_index(e), S::entry_value(e), total);
   }
-  // ---- many: where they end, then their sums in order of the index
-  Cut cut;
-  if (k > 0) cut = s.cut(false, k, least, top, cut);
-  if (top_p < 1.f) {
-    u64 sum = 0;
-    s.each([&](float x, int i) { if (cut.keeps(x, i)) sum += s.weigh(x); });
-    const u64 of = s.all(sum);
-    // (no token below lo can stay: all of them together weigh less than 1 - top_p)
-    const float lo = top + temperature * (logf((1.f - top_p) / (float)a.vocab) - 0.01f);
-    cut = s.cut(true, S::share_of(top_p, of), fmaxf(least, lo), top, cut);
-  }
-  auto weight = [&](float x, int i) -> u64 {
-    if (!cut.keeps(x, i)) return 0;
-    const double v = s.weigh.scaled(x);
-    return v >= min_weight ? Weigher::whole(v) : 0;
+  // ---- many: their sums in order of the index
+  if (least > cut.v) cut = Cut{nextafterf(least, -INFINITY), -1};
+  auto weight = [&](const float (&x)[S::VEC], int i, u64 (&q)[S::VEC]) {
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < S::VEC; ++e) {
+      any |= cut.keeps(x[e], i + e);
+      q[e] = 0;
+    }
+    if (!__any(any)) return;
+    s.form(x, q);
+#pragma unroll
+    for (int e = 0; e < S::VEC; ++e) q[e] &= S::when(cut.keeps(x[e], i + e));
   };
-  total = s.sum_pieces(weight);
-  token = s.locate(S::target_of(u, total), weight);
-  if (tid == 0) {
-    float x = to_f32(s.row[token]);
-    if (s.infinite) x = 0.f;
-    finish(token, x, total);
-  }
+  total = s.sum_chunks(weight);
+  const int token = s.locate(S::target_of(u, total), weight);
+  if (tid == 0) finish(token, to_f32(s.row[token]), total);
 }
 
 template <typename T>
