@@ -29,8 +29,16 @@ struct WeighArgs {
   float cap_log2, scale_over_cap;
   int bias;
   float slopes_log2[kMaxQueryHeads];
-  int split;                        // the waves of a workgroup share its keys' rows
+  int kind;                         // kWeighToken, kWeighRows, kWeighWide
+  // kWeighWide: what each row brings, [n_kv][n_tokens * group] and a chunk more; where
+  // the tiles may be few, partial sums of `slots` units (else 0: no parts)
+  struct RowInfo* info;
+  float* partial;
+  int slots;
+  int near;                         // 32 queries lie within 2^31 bytes
 };
+enum { kWeighToken = 0, kWeighRows = 1, kWeighWide = 2 };
+constexpr int kWeighSlots = 768;
 struct WeighTable {
   int q[kTableSeqs + 1];
 };
@@ -38,6 +46,13 @@ struct WeighTable {
 constexpr int weigh_keys(int element_bytes, int head_dim) {
   const int row = element_bytes * head_dim;
   return row <= 256 && element_bytes == 2 ? 64 : row <= 512 ? 32 : 16;
+}
+constexpr int weigh_token_keys(int element_bytes, int head_dim) {
+  return weigh_keys(element_bytes, head_dim) > 32 ? 32 : weigh_keys(element_bytes, head_dim);
+}
+// Tiles that the table has room for.
+inline int64_t weigh_tiles(const WeighArgs& a, int keys) {
+  return (int64_t)a.seqs.n_seqs * ((a.seqs.max_len + keys - 1) / keys);
 }
 template <typename T>
 hipError_t weigh(const WeighArgs& a, const WeighTable& tab, hipStream_t s);

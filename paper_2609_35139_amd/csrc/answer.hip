@@ -5,6 +5,7 @@
 
 #include "../../include/cacherepair.h"
 #include "profile.h"
+#include "rules.h"
 #include "serve_checks.h"
 
 namespace {
@@ -49,10 +50,29 @@ cr_status check_slots(const cr_kv_layout* l, const cr_sequences* q) {
 cr_status check_weigh(const cr_kv_layout* l, const cr_sequences* q, int n_heads, Batch* b) {
   return check_attend(l, q, n_heads, 0, b);
 }
-uint64_t weigh_workspace(const cr_sequences* q, const Batch& b) {
+// Which kernel a call takes, and its workspace.
+struct WeighPlan {
+  int kind = kWeighToken, slots = 0;
+  uint64_t table = 0, info = 0, partial = 0, total = 0;
+};
+WeighPlan weigh_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& b, int n_heads) {
+  WeighPlan p;
+  if (!b.n_tokens) return p;
+  const int group = n_heads / l->n_kv_heads;
+  p.kind = b.most * group <= 16 ? kWeighToken : b.most * group <= 256 ? kWeighRows : kWeighWide;
   Arena a;
-  if (b.n_tokens && b.off && q->n_seqs > kTableSeqs) a.take(((uint64_t)q->n_seqs + 1) * 4);
-  return a.off;
+  if (b.off && q->n_seqs > kTableSeqs) p.table = a.take(((uint64_t)q->n_seqs + 1) * 4);
+  if (p.kind == kWeighWide) {
+    p.info = a.take(((uint64_t)b.n_tokens * n_heads + 64) * 32);
+    const int keys = 2 * weigh_keys((int)esize(l->dtype), l->head_dim);
+    if ((int64_t)q->n_seqs * ceil_div((int64_t)q->max_blocks * q->block_size, keys) * l->n_kv_heads * 2 <=
+        kWeighSlots) {
+      p.slots = kWeighSlots;
+      p.partial = a.take((uint64_t)kWeighSlots * keys * 4);
+    }
+  }
+  p.total = a.off;
+  return p;
 }
 
 }  // namespace
@@ -65,7 +85,7 @@ cr_status cr_weigh_workspace_bytes(const cr_kv_layout* layout, const cr_sequence
   Batch b;
   const cr_status st = check_weigh(layout, seqs, n_heads, &b);
   if (st != CR_OK) return st;
-  *bytes = weigh_workspace(seqs, b);
+  *bytes = weigh_plan(layout, seqs, b, n_heads).total;
   return CR_OK;
 }
 
@@ -87,10 +107,10 @@ cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32_t laye
   if ((st = check_weights(weights, layout->n_layers, layout->n_kv_heads, seqs)) != CR_OK) return st;
   if (b.n_tokens == 0) return CR_OK;
   if (!o.lse) return CR_ERR_NULL;
-  const uint64_t need = weigh_workspace(seqs, b);
-  if (need) {
+  const WeighPlan p = weigh_plan(layout, seqs, b, n_heads);
+  if (p.total) {
     if (!workspace) return CR_ERR_NULL;
-    if (workspace_bytes < need || !aligned(workspace, ALIGN)) return CR_ERR_WORKSPACE;
+    if (workspace_bytes < p.total || !aligned(workspace, ALIGN)) return CR_ERR_WORKSPACE;
   }
   st = check_device();
   if (st != CR_OK) return st;
@@ -111,7 +131,13 @@ cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32_t laye
   a.lo = o.lo;
   a.hi = o.hi;
   set_scores(a, o, n_heads);
-  a.split = b.most * a.group > 16;
+  char* ws = static_cast<char*>(workspace);
+  a.kind = p.kind;
+  a.slots = p.slots;
+  const int64_t reach = 32 * q->stride_token + 256 * q->stride_head + 256;
+  a.near = q->stride_token < (1 << 24) && q->stride_head < (1 << 20) && reach * 4 < (int64_t)1 << 31;
+  a.info = reinterpret_cast<RowInfo*>(ws + p.info);
+  a.partial = reinterpret_cast<float*>(ws + p.partial);
   WeighTable tab{};
   a.ragged = b.off != nullptr;
   if (!a.ragged) {
@@ -119,7 +145,7 @@ cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32_t laye
   } else if (seqs->n_seqs <= kTableSeqs) {
     std::copy(b.off, b.off + seqs->n_seqs + 1, tab.q);
   } else {
-    int* dev = static_cast<int*>(workspace);
+    int* dev = reinterpret_cast<int*>(ws + p.table);
     CR_TRY(timed("weigh_table", s, [&] { return copy_table(b.off, seqs->n_seqs + 1, dev, s); }));
     a.q_off = dev;
   }

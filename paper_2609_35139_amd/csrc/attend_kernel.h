@@ -278,14 +278,6 @@ __device__ __forceinline__ float row_sum(float x) {
   return halves_sum(__uint_as_float(v[0]) + __uint_as_float(v[1]));
 }
 
-// This lane's number, from no register that has to live.  (opaque: not merged
-// with an earlier one)
-__device__ __forceinline__ int lane_again() {
-  int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-  asm volatile("" : "+v"(l));
-  return l;
-}
-
 // ------------------------------------------------------------------ kernel
 // RG * KG waves: KG groups of RG waves walk alternate tiles of KT keys, each
 // with its own ring of STAGES tiles; the RG waves of a group own 16 * NQ rows

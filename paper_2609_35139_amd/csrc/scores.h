@@ -57,4 +57,12 @@ template <> __device__ __forceinline__ float tanh_of<bf16>(float x) {
   return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
 }
 
+// This lane's number, from no register that has to live.  (opaque: not merged
+// with an earlier one)
+__device__ __forceinline__ int lane_again() {
+  int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(l));
+  return l;
+}
+
 }  // namespace cr
