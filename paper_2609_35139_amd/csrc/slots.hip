@@ -213,92 +213,163 @@ hipError_t choose(const ChooseArgs& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ compact
-// A workgroup moves one component (keys, values) of one (layer, sequence, head),
-// or its weights: 64 slots at a time, all read before any is written.  In place
-// that is enough: the list ascends, so kept[i] >= i and what a step writes lies
-// before all that later steps read.
-constexpr int kMoveRows = 64;
+// A workgroup moves one component (keys, values) of one (layer, sequence, head): MOVE
+// slots at a time, all read before any is written.  In place that is enough: the list
+// ascends, so kept[i] >= i and what a step writes lies before all that later steps
+// read.  So the next step's rows are on their way before this one's are written, and
+// its addresses are looked up while this one's rows are on their way.
+//
+// A workgroup's part of a row has 2^LOG 16-byte chunks, a thread moves chunk tid % 2^LOG
+// of U rows (rows that are no power of two: threads past the row idle).  Bound by
+// memory where there are enough workgroups; few of them, in place, share the rows'
+// columns, down to a cache line (36 layers of 2 heads, 2,048 of 4,096 slots of 256
+// bytes: 52 us with whole rows, XX with halves), out of place the steps.
+template <int LOG>
+struct MoveCfg {
+  static constexpr int NT = 256, PER_ROW = 1 << LOG, RPP = NT / PER_ROW;   // rows per pass
+  static constexpr int U = RPP > 32 ? NT / RPP : 8, MOVE = RPP * U;
+  static_assert(MOVE <= NT, "a thread looks a row up");
+};
 
+// Slot j of a sequence: bytes from its pool, or -1.
+__device__ __forceinline__ int64_t slot_bytes(const CompactArgs& a, const int* table, int j) {
+  const int id = table[j >> a.seqs.shift];
+  if (id < 0 || id >= a.seqs.n_blocks) return -1;
+  return ((int64_t)id * a.seqs.block + (int64_t)(j & ((1 << a.seqs.shift) - 1)) * a.seqs.token) *
+         a.element_bytes;
+}
+
+// The weights of one (layer, sequence, head), moved alike, and 0 behind them.
+__device__ __forceinline__ void move_weights(const CompactArgs& a) {
+  const int tid = threadIdx.x;
+  const int head = blockIdx.x % a.n_kv, ls = blockIdx.x / a.n_kv;
+  const int s = ls % a.seqs.n_seqs, layer = ls / a.seqs.n_seqs;
+  const int n = min(max(a.seqs.lens[s], 0), a.seqs.max_len);
+  const int m = min(max(a.kept_lens[s], 0), a.budget), end = min(m, a.seqs.max_len);
+  const int* kept = a.kept + (int64_t)blockIdx.x * a.budget;
+  float* w = a.weights.data + (int64_t)layer * a.weights.layer + (int64_t)s * a.weights.seq +
+             (int64_t)head * a.weights.head;
+  constexpr int U = 8;
+  for (int i0 = 0; i0 < max(n, end); i0 += 256 * U) {
+    float x[U];
+    bool write[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * 256 + tid;
+      x[u] = 0.f;
+      write[u] = i < n;                          // behind those that stay: nothing yet
+      if (i < end) {
+        const int j = kept[i];
+        write[u] = j >= 0 && j < n;              // (no slot: it keeps what it holds)
+        if (write[u]) x[u] = w[j];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]));
+    __syncthreads();                             // everything of this step is read
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (write[u]) w[i0 + u * 256 + tid] = x[u];
+  }
+}
+
+template <int LOG>
 __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
-  __shared__ int64_t src[kMoveRows], dst[kMoveRows];
+  using C = MoveCfg<LOG>;
+  __shared__ int64_t src[2][C::MOVE], dst[2][C::MOVE];
   const int tid = threadIdx.x;
   const int head = blockIdx.x % a.n_kv, ls = blockIdx.x / a.n_kv;
   const int s = ls % a.seqs.n_seqs, layer = ls / a.seqs.n_seqs;
   const int comp = blockIdx.y;
+  if (comp == 2) {
+    if (blockIdx.z == 0) move_weights(a);
+    return;
+  }
   const int n = min(max(a.seqs.lens[s], 0), a.seqs.max_len);
   const int m = min(max(a.kept_lens[s], 0), a.budget);
   const int* kept = a.kept + (int64_t)blockIdx.x * a.budget;
-  if (comp == 2) {
-    float* w = a.weights.data + (int64_t)layer * a.weights.layer + (int64_t)s * a.weights.seq +
-               (int64_t)head * a.weights.head;
-    const int end = min(m, a.seqs.max_len);
-    for (int i0 = 0; i0 < max(n, end); i0 += 256) {
-      const int i = i0 + tid;
-      float x = 0.f;
-      bool write = i < n;                        // behind those that stay: nothing yet
-      if (i < end) {
-        const int j = kept[i];
-        write = j >= 0 && j < n;                 // (no slot: it keeps what it holds)
-        if (write) x = w[j];
-      }
-      __syncthreads();
-      if (write) w[i] = x;
-    }
-    return;
-  }
   const int* table = a.seqs.table + (int64_t)s * a.seqs.max_blocks;
   const int* out = a.table_out ? a.table_out + (int64_t)s * a.max_blocks_out : table;
-  const int shift = a.seqs.shift, mask = (1 << shift) - 1;
-  const int most = min(m, a.max_blocks_out << shift);
+  const int most = min(m, a.max_blocks_out << a.seqs.shift);
   char* base = a.kv + ((int64_t)layer * a.layer + (int64_t)comp * a.kv_step +
                        (int64_t)head * a.seqs.head) * a.element_bytes;
-  const int per_row = a.row_bytes / 16, work = kMoveRows * per_row;
-  for (int i0 = 0; i0 < most; i0 += kMoveRows) {
-    __syncthreads();                             // the last step's addresses are idle
-    if (tid < kMoveRows) {
-      int64_t from = -1, to = -1;
-      const int i = i0 + tid;
-      if (i < most) {
-        const int j = kept[i];
-        if (j >= 0 && j < n && (j != i || a.table_out)) {
-          const int f = table[j >> shift], t = out[i >> shift];
-          if (f >= 0 && f < a.seqs.n_blocks && t >= 0 && t < a.seqs.n_blocks) {
-            from = ((int64_t)f * a.seqs.block + (int64_t)(j & mask) * a.seqs.token) * a.element_bytes;
-            to = ((int64_t)t * a.seqs.block + (int64_t)(i & mask) * a.seqs.token) * a.element_bytes;
-          }
-        }
+  const int columns = a.table_out ? 1 : gridDim.z, shares = a.table_out ? gridDim.z : 1;
+  const int chunk = (tid & (C::PER_ROW - 1)) + (columns > 1 ? blockIdx.z * C::PER_ROW : 0), r0 = tid >> LOG;
+  const bool active = chunk * 16 < a.row_bytes;
+  const int stride = C::MOVE * shares;           // (out of place the steps depend on nothing)
+  auto look_up = [&](int i0, int st) {
+    if (tid >= C::MOVE) return;
+    int64_t from = -1, to = -1;
+    const int i = i0 + tid;
+    if (i < most) {
+      const int j = kept[i];
+      if (j >= 0 && j < n && (j != i || a.table_out)) {
+        from = slot_bytes(a, table, j);
+        to = slot_bytes(a, out, i);
       }
-      src[tid] = from;
-      dst[tid] = to;
     }
-    __syncthreads();
-    constexpr int MOST = kMoveRows * 64 / 256;   // rows of up to 1 KB
-    uint4 x[MOST];
+    src[st][tid] = to < 0 ? -1 : from;
+    dst[st][tid] = to;
+  };
+  uint4 x[C::U];
+  auto read = [&](int st) {
 #pragma unroll
-    for (int u = 0; u < MOST; ++u) {
-      const int at = u * 256 + tid;
-      const int r = at / per_row;
-      if (at < work && src[r] >= 0)
-        x[u] = *reinterpret_cast<const uint4*>(base + src[r] + (at - r * per_row) * 16);
+    for (int u = 0; u < C::U; ++u) {
+      const int64_t from = src[st][r0 + u * C::RPP];
+      if (active && from >= 0) x[u] = *reinterpret_cast<const uint4*>(base + from + chunk * 16);
     }
+  };
+  int i0 = shares > 1 ? blockIdx.z * C::MOVE : 0, st = 0;
+  if (i0 >= most) return;
+  look_up(i0, 0);
+  __syncthreads();
+  read(0);
+  for (; i0 < most; i0 += stride, st ^= 1) {
+    look_up(i0 + stride, st ^ 1);
+    // (the rows have to be here, not on their way, when the others write)
 #pragma unroll
-    for (int u = 0; u < MOST; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
-    __syncthreads();                             // everything is read
+    for (int u = 0; u < C::U; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+    __syncthreads();                             // everything of this step is read
+    uint4 y[C::U];
 #pragma unroll
-    for (int u = 0; u < MOST; ++u) {
-      const int at = u * 256 + tid;
-      const int r = at / per_row;
-      if (at < work && src[r] >= 0)
-        *reinterpret_cast<uint4*>(base + dst[r] + (at - r * per_row) * 16) = x[u];
+    for (int u = 0; u < C::U; ++u) y[u] = x[u];
+    if (i0 + stride < most) read(st ^ 1);
+#pragma unroll
+    for (int u = 0; u < C::U; ++u) {
+      const int r = r0 + u * C::RPP;
+      if (active && src[st][r] >= 0) *reinterpret_cast<uint4*>(base + dst[st][r] + chunk * 16) = y[u];
     }
+    __syncthreads();                             // this step's addresses are idle
   }
 }
 
-hipError_t compact(const CompactArgs& a, hipStream_t s) {
+template <int LOG>
+hipError_t compact_as(const CompactArgs& a, int columns, hipStream_t s) {
   const int64_t rows = (int64_t)a.n_layers * a.seqs.n_seqs * a.n_kv;
-  const dim3 grid((unsigned)rows, a.weights.data ? 3 : 2);
-  CR_LAUNCH(compact_kernel, grid, dim3(256), 0, s, a);
+  const int64_t steps = (a.budget + MoveCfg<LOG>::MOVE - 1) / MoveCfg<LOG>::MOVE;
+  // out of place: about eight workgroups to a CU
+  const int64_t z = a.table_out ? std::max<int64_t>(1, std::min(steps, 2048 / (2 * rows))) : columns;
+  const dim3 grid((unsigned)rows, a.weights.data ? 3 : 2, (unsigned)z);
+  CR_LAUNCH((compact_kernel<LOG>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+hipError_t compact(const CompactArgs& a, hipStream_t s) {
+  const int chunks = a.row_bytes / 16;           // 4 (bf16 heads of 32) to 64 (fp32 of 256)
+  int log = 2, columns = 1;
+  while ((1 << log) < chunks) ++log;
+  const int64_t groups = 2 * (int64_t)a.n_layers * a.seqs.n_seqs * a.n_kv;
+  while (!a.table_out && log > 3 && groups * columns < 512) {
+    --log;
+    columns *= 2;
+  }
+  switch (log) {
+    case 2: return compact_as<2>(a, columns, s);
+    case 3: return compact_as<3>(a, columns, s);
+    case 4: return compact_as<4>(a, columns, s);
+    case 5: return compact_as<5>(a, columns, s);
+    default: return compact_as<6>(a, columns, s);
+  }
 }
 
 }  // namespace cr
