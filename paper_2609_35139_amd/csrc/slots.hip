@@ -31,17 +31,25 @@ __device__ __forceinline__ uint32_t lanes_before(uint32_t v, int lane, uint32_t*
 
 constexpr int kChooseBins = 2048;
 
-// A workgroup chooses for one (layer, sequence, head).  The smallest weight that
-// stays is found by counting: the weights' range is cut into at most 2048 bins,
-// the bin that holds the last one to stay becomes the range, at most three times
-// for 32 bits.  EPT: 4-slot groups that a thread keeps in registers; 0: as many
-// as there are, read again from the caches in every pass.
+// A workgroup chooses for one (layer, sequence, head), each wave in a run of slots of
+// its own.  The smallest weight that stays is found by counting: the weights' range is
+// cut into at most 2048 bins and the bin that holds the last one to stay becomes the
+// range, until its weights are few enough to compare each with each, or all equal.
+// EPT: vectors of four slots that a thread keeps in registers; 0: as many as there are,
+// read again from the caches in every pass.
 template <int NT, int EPT>
 __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   constexpr int WAVES = NT / 64;
-  __shared__ uint32_t hist[kChooseBins];
-  __shared__ uint32_t scratch[WAVES * 2 + 8];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr uint32_t FEW = 256;
+  // (every bin COPIES times, for a lane each: lanes that count in the same one wait for
+  // each other)
+  constexpr int COPIES = NT == 256 ? 2 : 4;
+  typedef uint32_t Counts __attribute__((ext_vector_type(COPIES)));
+  __shared__ Counts hist[kChooseBins];
+  __shared__ uint32_t few[FEW];
+  __shared__ uint32_t scratch[WAVES * 2], found[3];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.x % a.n_kv, ls = blockIdx.x / a.n_kv;
   const int s = ls % a.n_seqs, layer = ls / a.n_seqs;
   const int n = min(max(a.lens[s], 0), a.max_len);
@@ -59,50 +67,64 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   const float* w = a.weights.data + (int64_t)layer * a.weights.layer + (int64_t)s * a.weights.seq +
                    (int64_t)head * a.weights.head;
   const bool vectors = reinterpret_cast<uintptr_t>(w) % 16 == 0;
-  const int groups = (hi + 4 * NT - 1) / (4 * NT);   // 4 NT slots each, from slot 0
+  const int run = (n + 256 * WAVES - 1) / (256 * WAVES);   // vectors of a lane, 256 slots each
+  auto slot_of = [&](int j) { return ((wave * run + j) * 64 + lane) * 4; };
   uint4 keep[EPT ? EPT : 1];
+  // (a slot that is not to be chosen from has key 0, below that of every weight)
   auto load = [&](int j) {
-    const int i = (j * NT + tid) * 4;
+    const int i = slot_of(j), i0 = i - lane * 4;
     uint4 k{0, 0, 0, 0};
-    if (i < hi && i + 4 > lo) {
-      float4 x;
-      if (vectors && i + 4 <= a.max_len) {       // (may pass hi, not the row's end)
-        x = *reinterpret_cast<const float4*>(w + i);
-      } else {
-        x.x = w[i];
-        x.y = i + 1 < a.max_len ? w[i + 1] : 0.f;
-        x.z = i + 2 < a.max_len ? w[i + 2] : 0.f;
-        x.w = i + 3 < a.max_len ? w[i + 3] : 0.f;
-      }
+    if (i0 >= lo && i0 + 256 <= hi && vectors) {
+      const float4 x = *reinterpret_cast<const float4*>(w + i);
       k = uint4{weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w)};
+    } else if (i0 < hi && i0 + 256 > lo) {
+      k.x = i >= lo && i < hi ? weight_key(w[i]) : 0u;
+      k.y = i + 1 >= lo && i + 1 < hi ? weight_key(w[i + 1]) : 0u;
+      k.z = i + 2 >= lo && i + 2 < hi ? weight_key(w[i + 2]) : 0u;
+      k.w = i + 3 >= lo && i + 3 < hi ? weight_key(w[i + 3]) : 0u;
     }
     return k;
   };
   if constexpr (EPT > 0) {
 #pragma unroll
     for (int j = 0; j < EPT; ++j)
-      if (j < groups) keep[j] = load(j);
+      if (j < run) keep[j] = load(j);
   }
-  // f(key, slot) for this thread's slots to choose from
-  auto each = [&](auto&& f) {
-    auto four = [&](const uint4& k, int j) {
-      const int i = (j * NT + tid) * 4;
-      const uint32_t v[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (i + e >= lo && i + e < hi) f(v[e], i + e);
-    };
+  // f(vector of keys, its first slot), vector by vector of this thread
+  auto each_vector = [&](auto&& f) {
     if constexpr (EPT > 0) {
 #pragma unroll
       for (int j = 0; j < EPT; ++j)
-        if (j < groups) four(keep[j], j);
+        if (j < run) f(keep[j], slot_of(j));
     } else {
-      for (int j = 0; j < groups; ++j) four(load(j), j);
+      constexpr int U = 4;                        // (the next ones on their way meanwhile)
+      uint4 k[U], next[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = load(min(u, run - 1));
+#pragma unroll 1
+      for (int j = 0; j < run; j += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) k[u] = next[u];
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = load(min(j + U + u, run - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (j + u < run) f(k[u], slot_of(j + u));
+      }
     }
   };
-  // the range of the keys
+  // f(key) for this thread's slots
+  auto each = [&](auto&& f) {
+    each_vector([&](const uint4& k, int) {
+      f(k.x);
+      f(k.y);
+      f(k.z);
+      f(k.w);
+    });
+  };
+  // the range of the keys (0 is no key: it becomes the largest number)
   uint32_t kmin = ~0u, kmax = 0;
-  each([&](uint32_t k, int) { kmin = min(kmin, k); kmax = max(kmax, k); });
+  each([&](uint32_t k) { kmin = min(kmin, k - 1u); kmax = max(kmax, k); });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     kmin = min(kmin, (uint32_t)__shfl_xor(kmin, o));
@@ -114,98 +136,139 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     kmin = min(kmin, scratch[i]);
     kmax = max(kmax, scratch[WAVES + i]);
   }
-  // the key of the last one to stay, and how many of that key stay
+  kmin += 1u;
+  auto count_of = [&](int bin) {
+    const Counts c = hist[bin];
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) t += c[i];
+    return t;
+  };
+  // the key of the last one to stay (kmin in the end), and how many of that key stay
   uint32_t left = need;
   while (kmin < kmax) {
     const uint32_t span = kmax - kmin;
     const int bits = 32 - __clz(span), sh = bits > 11 ? bits - 11 : 0;
-    for (int i = tid; i < kChooseBins; i += NT) hist[i] = 0;
+    for (int i = tid; i < kChooseBins; i += NT) hist[i] = Counts{};
+    if (tid == 0) found[2] = 0;
     __syncthreads();
-    each([&](uint32_t k, int) {
-      if (k >= kmin && k <= kmax) atomicAdd(&hist[(k - kmin) >> sh], 1u);
+    each([&](uint32_t k) {
+      if (k - kmin <= span)
+        atomicAdd(reinterpret_cast<uint32_t*>(hist) + ((k - kmin) >> sh) * COPIES + lane % COPIES, 1u);
     });
     __syncthreads();
     // bins from the highest down: the first whose running count reaches `left`
-    constexpr int PER = kChooseBins / NT > 0 ? kChooseBins / NT : 1;
+    constexpr int PER = kChooseBins / NT;
     uint32_t c[PER], mine = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = kChooseBins - 1 - (tid * PER + i);
-      c[i] = b >= 0 ? hist[b] : 0;
-      mine += c[i];
-    }
+    for (int i = 0; i < PER; ++i) mine += c[i] = count_of(kChooseBins - 1 - (tid * PER + i));
     uint32_t total;
     uint32_t before = lanes_before(mine, lane, &total);
     if (lane == 0) scratch[wave] = total;
     __syncthreads();
     for (int i = 0; i < wave; ++i) before += scratch[i];
     if (before < left && before + mine >= left) {   // one thread
-      int i = 0;
-      while (before + c[i] < left) before += c[i++];
-      scratch[WAVES] = kChooseBins - 1 - (tid * PER + i);
-      scratch[WAVES + 1] = left - before;
+      bool done = false;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (done) continue;
+        done = before + c[i] >= left;
+        if (done) {
+          found[0] = kChooseBins - 1 - (tid * PER + i);
+          found[1] = left - before;
+        } else {
+          before += c[i];
+        }
+      }
     }
     __syncthreads();
-    const uint32_t bin = scratch[WAVES];
-    left = scratch[WAVES + 1];
-    const uint32_t to_bin = bin << sh;
+    const uint32_t to_bin = found[0] << sh, count = count_of(found[0]);
+    left = found[1];
     kmax = kmin + to_bin + min(span - to_bin, (1u << sh) - 1u);
     kmin += to_bin;
+    if (count <= FEW && kmin < kmax) {
+      each([&](uint32_t k) {
+        if (k - kmin <= kmax - kmin) few[atomicAdd(&found[2], 1u)] = k;
+      });
+      __syncthreads();
+      if (tid < (int)count) {
+        const uint32_t k = few[tid];
+        uint32_t above = 0, equal = 0;
+#pragma unroll 8
+        for (uint32_t i = 0; i < count; ++i) {
+          above += few[i] > k;
+          equal += few[i] == k;
+        }
+        if (above < left && above + equal >= left) {   // (equal ones write the same)
+          found[0] = k;
+          found[1] = left - above;
+        }
+      }
+      __syncthreads();
+      kmin = kmax = found[0];
+      left = found[1];
+    }
     __syncthreads();
   }
   // ---- the list, in order of the slots: a slot's place is the number of those
-  // before it that stay whatever happens, and of the equal ones up to `left`
-  uint32_t all_before = 0, equal_before = 0;
-  const int last = (n + 4 * NT - 1) / (4 * NT);
-  auto place = [&](const uint4& k, int j) {
-    const int i = (j * NT + tid) * 4;
+  // before it that stay whatever happens, and of the equal ones up to `left`.  Counted
+  // for each wave's run, then written run by run.
+  // the lanes whose slot e of a vector stays whatever happens, or is an equal one
+  struct Marks { uint64_t sure[4], equal[4]; };
+  auto marks_of = [&](const uint4& k, int i) {
     const uint32_t v[4] = {k.x, k.y, k.z, k.w};
-    uint32_t sure = 0, equal = 0;
+    Marks r;
+    const bool inside = i - lane * 4 >= lo && i - lane * 4 + 256 <= hi;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int at = i + e;
-      const bool in = at >= lo && at < hi;
-      if (at < n && (!in || v[e] > kmin)) sure |= 1u << e;
-      if (in && v[e] == kmin) equal |= 1u << e;
+      r.sure[e] = __ballot(v[e] > kmin);
+      r.equal[e] = __ballot(v[e] == kmin);
+      if (!inside) r.sure[e] |= __ballot(v[e] == 0 && i + e < n);
     }
-    uint32_t total;
-    const uint32_t packed = lanes_before(__popc(sure) | __popc(equal) << 16, lane, &total);
-    if (lane == 0) scratch[wave] = total;
-    __syncthreads();
-    uint32_t sure_at = all_before + (packed & 0xffff), equal_at = equal_before + (packed >> 16);
-    for (int x = 0; x < WAVES; ++x) {
-      const uint32_t t = scratch[x];
-      if (x < wave) { sure_at += t & 0xffff; equal_at += t >> 16; }
-      all_before += t & 0xffff;
-      equal_before += t >> 16;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool is_equal = (equal >> e) & 1;
-      if ((sure >> e) & 1 || (is_equal && equal_at < left)) out[sure_at + min(equal_at, left)] = i + e;
-      sure_at += (sure >> e) & 1;
-      equal_at += is_equal;
-    }
+    return r;
   };
-  if constexpr (EPT > 0) {
+  uint32_t sure_at = 0, equal_at = 0;
+  each_vector([&](const uint4& k, int i) {
+    const Marks r = marks_of(k, i);
 #pragma unroll
-    for (int j = 0; j < EPT; ++j)
-      if (j < last) place(j < groups ? keep[j] : uint4{0, 0, 0, 0}, j);
-  } else {
-    for (int j = 0; j < last; ++j) place(j < groups ? load(j) : uint4{0, 0, 0, 0}, j);
-  }
+    for (int e = 0; e < 4; ++e) {
+      sure_at += __popcll(r.sure[e]);
+      equal_at += __popcll(r.equal[e]);
+    }
+  });
+  if (lane == 0) { scratch[wave] = sure_at; scratch[WAVES + wave] = equal_at; }
+  __syncthreads();
+  sure_at = equal_at = 0;
+  for (int i = 0; i < wave; ++i) { sure_at += scratch[i]; equal_at += scratch[WAVES + i]; }
+  each_vector([&](const uint4& k, int i) {
+    const Marks r = marks_of(k, i);
+    // those of the lanes before this one, of all four slots
+    uint32_t at = sure_at, eq = equal_at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      at = __builtin_amdgcn_mbcnt_hi((uint32_t)(r.sure[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)r.sure[e], at));
+      eq = __builtin_amdgcn_mbcnt_hi((uint32_t)(r.equal[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)r.equal[e], eq));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool is_sure = (r.sure[e] >> lane) & 1, is_equal = (r.equal[e] >> lane) & 1;
+      if (is_sure | (is_equal & (eq < left))) out[at + min(eq, left)] = i + e;
+      at += is_sure;
+      eq += is_equal;
+      sure_at += __popcll(r.sure[e]);
+      equal_at += __popcll(r.equal[e]);
+    }
+  });
 }
 
 hipError_t choose(const ChooseArgs& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.n_layers * a.n_seqs * a.n_kv;
-  const dim3 grid((unsigned)rows);
+  const dim3 grid((unsigned)((int64_t)a.n_layers * a.n_seqs * a.n_kv));
   if (a.max_len <= 4096) {
     CR_LAUNCH((choose_kernel<256, 4>), grid, dim3(256), 0, s, a);
-  } else if (a.max_len <= 16384) {
-    CR_LAUNCH((choose_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
-  } else if (a.max_len <= 65536) {
-    CR_LAUNCH((choose_kernel<1024, 16>), grid, dim3(1024), 0, s, a);
+  } else if (a.max_len <= 8192) {
+    CR_LAUNCH((choose_kernel<256, 8>), grid, dim3(256), 0, s, a);
+  } else if (a.max_len <= 32768) {
+    CR_LAUNCH((choose_kernel<512, 16>), grid, dim3(512), 0, s, a);
   } else {
     CR_LAUNCH((choose_kernel<1024, 0>), grid, dim3(1024), 0, s, a);
   }
