@@ -26,6 +26,7 @@ constexpr int kMostTopK = 256;        // top-k that a list is made for at once
 constexpr int kSampleShort = 256;     // of a list that is compared each with each
 
 typedef unsigned long long u64;
+typedef u64 Pair __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t order_of(float x) {      // whole numbers in the order of x
   const uint32_t b = __float_as_uint(x + 0.f);               // (-0 is 0)
@@ -90,7 +91,7 @@ struct Cut {
 struct SampleShared {
   u64 mass[kSampleBins];                // or sums of the row's chunks
   uint32_t count[kSampleBins];
-  u64 list[kSampleList], few[kSampleList], weight[kSampleShort];
+  alignas(16) u64 list[kSampleList], few[kSampleList], weight[kSampleShort];
   double table[kExpTable];
   u64 scan[kSampleWaves];
   u64 word[4];
@@ -524,15 +525,16 @@ struct Sampler {
     const u64 e = mine ? sh.list[tid] : 0;
     u64 q = mine ? weigh(entry_value(e)) : 0;
     if (mine) sh.weight[tid] = q;
+    if (tid == n && n % 2) sh.list[n] = sh.weight[n] = 0;
     __syncthreads();
     u64 b = 0;
     uint32_t rank = 0;
     if (mine) {
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const bool better = sh.list[i] > e;
-        b += sh.weight[i] & when(better);
-        rank += better;
+#pragma unroll 4
+      for (int i = 0; i < n; i += 2) {           // (an entry of 0 behind an odd number)
+        const Pair o = *reinterpret_cast<const Pair*>(sh.list + i), w = *reinterpret_cast<const Pair*>(sh.weight + i);
+        b += (w[0] & when(o[0] > e)) + (w[1] & when(o[1] > e));
+        rank += (o[0] > e) + (o[1] > e);
       }
     }
     const bool within = mine && (k == 0 || rank < k);
@@ -546,8 +548,11 @@ struct Sampler {
     const u64 target = target_of(u, kept);
     if (stays) {
       u64 at = 0;                          // of lower indexes: larger lower halves
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) at += sh.weight[i] & when((uint32_t)sh.list[i] > (uint32_t)e);
+#pragma unroll 4
+      for (int i = 0; i < n; i += 2) {
+        const Pair o = *reinterpret_cast<const Pair*>(sh.list + i), w = *reinterpret_cast<const Pair*>(sh.weight + i);
+        at += (w[0] & when((uint32_t)o[0] > (uint32_t)e)) + (w[1] & when((uint32_t)o[1] > (uint32_t)e));
+      }
       if (at <= target && at + q > target) sh.word[3] = e;
     }
     __syncthreads();

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   constexpr int COPIES = NT == 256 ? 2 : 4;
   typedef uint32_t Counts __attribute__((ext_vector_type(COPIES)));
   __shared__ Counts hist[kChooseBins];
-  __shared__ uint32_t few[FEW];
+  __shared__ __align__(16) uint32_t few[FEW];
   __shared__ uint32_t scratch[WAVES * 2], found[3];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -150,6 +150,7 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     const uint32_t span = kmax - kmin;
     const int bits = 32 - __clz(span), sh = bits > 11 ? bits - 11 : 0;
     for (int i = tid; i < kChooseBins; i += NT) hist[i] = Counts{};
+    if (tid < (int)FEW) few[tid] = 0;               // (0 is no key)
     if (tid == 0) found[2] = 0;
     __syncthreads();
     each([&](uint32_t k) {
@@ -187,17 +188,25 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
     kmax = kmin + to_bin + min(span - to_bin, (1u << sh) - 1u);
     kmin += to_bin;
     if (count <= FEW && kmin < kmax) {
-      each([&](uint32_t k) {
-        if (k - kmin <= kmax - kmin) few[atomicAdd(&found[2], 1u)] = k;
+      const uint32_t range = kmax - kmin;
+      each_vector([&](const uint4& k, int) {
+        const bool any = (k.x - kmin <= range) | (k.y - kmin <= range) | (k.z - kmin <= range) |
+                         (k.w - kmin <= range);
+        if (!__any(any)) return;
+        const uint32_t v[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v[e] - kmin <= range) few[atomicAdd(&found[2], 1u)] = v[e];
       });
       __syncthreads();
       if (tid < (int)count) {
         const uint32_t k = few[tid];
         uint32_t above = 0, equal = 0;
-#pragma unroll 8
-        for (uint32_t i = 0; i < count; ++i) {
-          above += few[i] > k;
-          equal += few[i] == k;
+#pragma unroll 4
+        for (uint32_t i = 0; i < count; i += 4) {
+          const uint4 o = *reinterpret_cast<const uint4*>(few + i);
+          above += (o.x > k) + (o.y > k) + (o.z > k) + (o.w > k);
+          equal += (o.x == k) + (o.y == k) + (o.z == k) + (o.w == k);
         }
         if (above < left && above + equal >= left) {   // (equal ones write the same)
           found[0] = k;
