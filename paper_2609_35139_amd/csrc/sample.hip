@@ -714,7 +714,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     const u64 n = s.sum_chunks(equal);
     u64 m = k > 0 && k < n ? k : n;
     if (top_p < 1.f) m = S::share_of(top_p, m);
-    return answer(s.locate(S::target_of(u, m), equal), -logf((float)m));
+    return answer(s.locate(S::target_of(u, m), equal), -(float)log((double)m));
   }
   const double one = ldexp(1., shift);
   {
