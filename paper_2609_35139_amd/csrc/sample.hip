@@ -42,28 +42,28 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 // up to the fourth power (relative error 4e-14, below a step for all but the largest).
 // Products inside the fused operations are exact, so nothing is lost however far x and x_0
 // are from 0.  Ten fp64 operations, at half the rate of fp32 ones: a row of 151,936
-// logits takes a CU about 40 us.
+// logits takes a CU 46 us, by the operations: neither the chains of eight logits side by
+// side, a stage at a time, nor a table for each bank change that.
 constexpr int kExpTable = 64;
 struct Weigher {
   const double* table;   // 2^((j - f) / 64) 2^shift
   double c, whole;       // whole: 1.5 2^52 less the whole number next to x_0 c
   float lowest;          // what lies below weighs less than 2^-20 steps
-  __device__ __forceinline__ u64 operator()(float x) const {
-    x = x > lowest ? x : lowest;                      // (NaN too)
-    const double m = __builtin_fma((double)x, c, whole);
+  __device__ __forceinline__ u64 operator()(float logit) const {
+    const double x = (double)(logit > lowest ? logit : lowest);      // (NaN too)
+    const double m = __builtin_fma(x, c, whole);
     // (the float next to the lowest may lie further down; what it weighs is still no step)
     const int n = max((int)(__double_as_longlong(m) & 0xffffffff), -80 * kExpTable);
-    const double r = __builtin_fma((double)x, c, whole - m);
+    const long long b =
+        __double_as_longlong(table[n & (kExpTable - 1)]) + ((long long)(n & ~(kExpTable - 1)) << 46);
+    const double r = __builtin_fma(x, c, whole - m);
     constexpr double y = 0.69314718055994530942 / kExpTable;
     double e = __builtin_fma(r, y * y * y * y / 24., y * y * y / 6.);
     e = __builtin_fma(e, r, y * y / 2.);
     e = __builtin_fma(e, r, y);
     e = __builtin_fma(e, r, 1.);
-    const long long b = __double_as_longlong(table[n & (kExpTable - 1)]) +
-                        ((long long)(n & ~(kExpTable - 1)) << 46);
     // in whole steps: added to 2^52, the bits are kOffset + the weight
-    return (u64)__double_as_longlong(__builtin_fma(__longlong_as_double(b), e, 4503599627370496.)) -
-           kOffset;
+    return (u64)__double_as_longlong(__builtin_fma(__longlong_as_double(b), e, 4503599627370496.)) - kOffset;
   }
   static constexpr u64 kOffset = 0x4330000000000000ull;
 };
@@ -100,13 +100,13 @@ struct SampleShared {
 };
 
 // A row is read in chunks of U vectors for each lane of a wave, wave w taking chunks
-// w, w + 8, ...: several where a pass only compares (its loads are what it waits
-// for), one where it forms weights.  What is done for a logit stands in the code once
-// or for one vector: a workgroup runs through most of this code once, and a line of
-// it that is not in the instruction cache takes about a microsecond (everything
-// unrolled over eight vectors: 180 KB, and 45 us for a pass that finds 360 tokens,
-// 9 now).
-constexpr int kRead = 4, kReadMost = 8;
+// w, w + 8, ...: eight where a pass only compares (its loads are what it waits for: 7 us
+// for 151,936 logits), four where it forms weights.  What is done for a logit stands in
+// the code once, for a vector or for four: a workgroup runs through most of this code
+// once, and a line of it that is not in the instruction cache takes about a microsecond
+// (everything unrolled over eight vectors: 180 KB, and 45 us for a pass that finds 360
+// tokens; 9 to 13 now).
+constexpr int kRead = 4, kReadMost = 2 * kRead;
 
 template <typename T>
 struct Sampler {
@@ -196,51 +196,81 @@ struct Sampler {
       for (int u = 0; u < U; ++u) w[u] = next[u];
     }
   }
+  // f(vector number, its logits, the first one's index) for this wave's vectors, 64 lanes'
+  // at a time: the code stands once, the loads are as far ahead as in each_chunk.
+  template <typename F>
+  __device__ __forceinline__ void each_vector(F&& f) const {
+    each_chunk<kRead>([&](int c, uint4 (&w)[kRead]) {
+#pragma unroll 1
+      for (int u = 0; u < kRead; ++u) {
+        float x[VEC];
+        elements(w[0], x);
+        f(c * kRead + u, x, first_of<kRead>(c, u));
+#pragma unroll
+        for (int i = 0; i + 1 < kRead; ++i) w[i] = w[i + 1];
+      }
+    });
+  }
+  // A bit for each of a vector's logits that the cut keeps, and all bits where bit e is set
+  __device__ __forceinline__ static uint32_t kept_bits(const float (&x)[VEC], int i, const Cut& cut) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) bits |= (uint32_t)(x[e] > cut.v) << e;
+    if (cut.last >= 0) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) bits |= (uint32_t)((x[e] == cut.v) & (i + e <= cut.last)) << e;
+    }
+    return bits;
+  }
+  __device__ __forceinline__ static u64 when_bit(uint32_t bits, int e) {
+    return (u64)(int64_t)((int32_t)(bits << (31 - e)) >> 31);
+  }
   // f(x, index) for the logits in [lo, hi] that `within` keeps: a bit for each of a
   // lane's logits, then the lanes' bits one after the other.
   template <typename F>
   __device__ __forceinline__ void each_of(float lo, float hi, const Cut& within, F&& f) const {
-    each_chunk<kRead>([&](int c, const uint4 (&w)[kRead]) {
-      bool any = false;
-#pragma unroll
-      for (int u = 0; u < kRead; ++u) {
-        float x[VEC];
-        elements(w[u], x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) any |= x[e] >= lo;
-      }
-      if (!__any(any)) return;
-      uint32_t bits = 0;
-#pragma unroll
-      for (int u = 0; u < kRead; ++u) {
-        float x[VEC];
-        elements(w[u], x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          bits |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << (u * VEC + e);
-      }
+    each_chunk<kReadMost>([&](int c, uint4 (&w)[kReadMost]) {
 #pragma unroll 1
-      while (__any(bits != 0)) {
-        const int b = bits ? __ffs(bits) - 1 : 0;
-        uint32_t v = 0;
+      for (int half = 0; half < kReadMost / kRead; ++half) {
+        bool any = false;
 #pragma unroll
-        for (int d = 0; d < kRead * 4; ++d) {
-          const uint32_t o = d % 4 == 0 ? w[d / 4].x : d % 4 == 1 ? w[d / 4].y : d % 4 == 2 ? w[d / 4].z : w[d / 4].w;
-          v = b * (int)sizeof(T) / 4 == d ? o : v;
+        for (int u = 0; u < kRead; ++u) {
+          float x[VEC];
+          elements(w[u], x);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) any |= x[e] >= lo;
         }
-        if constexpr (sizeof(T) == 2) v = b % 2 ? v & 0xffff0000u : v << 16;
-        const float x = __uint_as_float(v);
-        const int i = first_of<kRead>(c, b / VEC) + b % VEC;
-        if (bits && within.keeps(x, i)) f(x, i);
-        bits &= bits - 1;
+        if (__any(any)) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int u = 0; u < kRead; ++u) {
+            float x[VEC];
+            elements(w[u], x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+              bits |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << (u * VEC + e);
+          }
+#pragma unroll 1
+          while (__any(bits != 0)) {
+            const int b = bits ? __ffs(bits) - 1 : 0;
+            uint32_t v = 0;
+#pragma unroll
+            for (int d = 0; d < kRead * 4; ++d) {
+              const uint4& four = w[d / 4];
+              const uint32_t o = d % 4 == 0 ? four.x : d % 4 == 1 ? four.y : d % 4 == 2 ? four.z : four.w;
+              v = b * (int)sizeof(T) / 4 == d ? o : v;
+            }
+            if constexpr (sizeof(T) == 2) v = b % 2 ? v & 0xffff0000u : v << 16;
+            const float x = __uint_as_float(v);
+            const int i = first_of<kReadMost>(c, half * kRead + b / VEC) + b % VEC;
+            if (bits && within.keeps(x, i)) f(x, i);
+            bits &= bits - 1;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kRead; ++u) w[u] = w[u + kRead];
       }
     });
-  }
-  // the weights of a vector, all of them at once (each is a chain of dependent
-  // instructions)
-  __device__ __forceinline__ void form(const float (&x)[VEC], u64 (&q)[VEC]) const {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) q[e] = weigh(x[e]);
   }
   // all bits, or none (selected by bits, a value is loaded whether it is needed or not,
   // and loads do not wait for each other's conditions)
@@ -390,27 +420,26 @@ struct Sampler {
     const double scale = scale_of(lo, hi);
     clear_bins();
     u64 sum = 0;
-    each_chunk<1>([&](int c, const uint4 (&w)[1]) {
-      float x[VEC];
+    each_vector([&](int, const float (&x)[VEC], int i) {
       u64 q[VEC];
-      elements(w[0], x);
-      if (by_weight) {
-        form(x, q);
-      } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) q[e] = 0;
-      }
-      const int i = first_of<1>(c, 0);
+      for (int e = 0; e < VEC; ++e) q[e] = by_weight ? weigh(x[e]) : 0;
+      const uint32_t kept = kept_bits(x, i, within);
+      uint32_t in = 0;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const bool kept = within.keeps(x[e], i + e);
-        sum += q[e] & when(kept);
-        if (kept & (x[e] >= lo) & (x[e] <= hi)) {
+        sum += q[e] & when_bit(kept, e);
+        in |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << e;
+      }
+      in &= kept;
+      if (!__any(in != 0)) return;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if ((in >> e) & 1) {
           const int b = bin_of(x[e], hi, scale);
           atomicAdd(&sh.count[b], 1u);
           if (by_weight) atomicAdd(&sh.mass[b], q[e]);
         }
-      }
     });
     return all(sum);
   }
@@ -439,23 +468,21 @@ struct Sampler {
   __device__ __forceinline__ u64 sum_chunks(F&& f) const {
     __syncthreads();
     u64 mine = 0;
-    each_chunk<1>([&](int c, const uint4 (&w)[1]) {
-      float x[VEC];
+    each_vector([&](int v, const float (&x)[VEC], int i) {
       u64 q[VEC], t = 0;
-      elements(w[0], x);
-      f(x, first_of<1>(c, 0), q);
+      f(x, i, q);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) t += q[e];
       mine += t;
       t = wave_upto(t);
-      if (lane == 63) sh.mass[c] = t;
+      if (lane == 63) sh.mass[v] = t;
     });
     return all(mine);
   }
   template <typename F>
   __device__ __forceinline__ int locate(u64 target, F&& f) const {
-    static_assert(kMostVocab / (64 * VEC) <= kSampleBins || VEC < 8, "sums");
-    const int n = chunks<1>(), per = (n + NT - 1) / NT;
+    static_assert(kMostVocab / (64 * VEC) <= kSampleBins, "sums");
+    const int n = chunks<kRead>() * kRead, per = (n + NT - 1) / NT;
     u64 mine = 0, total;
     for (int i = tid * per; i < min(n, tid * per + per); ++i) mine += sh.mass[i];
     u64 at = before(mine, &total);
@@ -723,8 +750,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     s.weigh = Weigher{sh.table, c, 6755399441055744. - next,
                       fmaxf((float)((double)top - 64. * kExpTable / c), -3.402823466e38f)};
   }
+  // (the largest logit's own weight, which may be off by a step: alone, its log is 0)
   auto finish = [&](int token, float x, u64 total) {
-    answer(token, (float)(((double)x - (double)top) / (double)temperature - log((double)total / one)));
+    const double q = (double)s.weigh(top);
+    answer(token, (float)(((double)x - (double)top) / (double)temperature - log((double)total / q)));
   };
   // no token below `least` can stay by min_p
   constexpr float kLowest = -3.402823466e38f;
@@ -760,8 +789,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   }
   // ---- else where the first k end, then where top-p ends: by bins of the values, from a
   // bound down to which they are likely to lie (about one in 50 tokens is not below the
-  // least of the threads' largest), or below which no token can stay (all of them together weigh less than 1 - top_p); the bin in which
-  // the end lies becomes the range, until its tokens fit the list or are all equal
+  // least of the threads' largest), or below which no token can stay (all of them together
+  // weigh less than 1 - top_p); the bin in which the end lies becomes the range, until its
+  // tokens fit the list or are all equal
 #pragma unroll 1
   for (int stage = 0; stage < 2; ++stage) {
     const bool by_weight = stage == 1;
@@ -830,16 +860,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   // ---- many: their sums in order of the index
   if (least > cut.v) cut = Cut{nextafterf(least, -INFINITY), -1};
   auto weight = [&](const float (&x)[S::VEC], int i, u64 (&q)[S::VEC]) {
-    bool any = false;
+    const uint32_t kept = S::kept_bits(x, i, cut);
 #pragma unroll
-    for (int e = 0; e < S::VEC; ++e) {
-      any |= cut.keeps(x[e], i + e);
-      q[e] = 0;
-    }
-    if (!__any(any)) return;
-    s.form(x, q);
+    for (int e = 0; e < S::VEC; ++e) q[e] = 0;
+    if (!__any(kept != 0)) return;
 #pragma unroll
-    for (int e = 0; e < S::VEC; ++e) q[e] &= S::when(cut.keeps(x[e], i + e));
+    for (int e = 0; e < S::VEC; ++e) q[e] = s.weigh(x[e]) & S::when_bit(kept, e);
   };
   total = s.sum_chunks(weight);
   const int token = s.locate(S::target_of(u, total), weight);

@@ -295,7 +295,7 @@ hipError_t choose(const ChooseArgs& a, hipStream_t s) {
 // of U rows (rows that are no power of two: threads past the row idle).  Bound by
 // memory where there are enough workgroups; few of them, in place, share the rows'
 // columns, down to a cache line (36 layers of 2 heads, 2,048 of 4,096 slots of 256
-// bytes: 52 us with whole rows, XX with halves), out of place the steps.
+// bytes: 55 us with whole rows, 41 with halves), out of place the steps.
 template <int LOG>
 struct MoveCfg {
   static constexpr int NT = 256, PER_ROW = 1 << LOG, RPP = NT / PER_ROW;   // rows per pass

@@ -510,6 +510,19 @@ def test_sample_random_numbers_at_their_ends():
         assert np.array_equal(tokens.cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("V", [1, 700, 9000, 40000])
+def test_sample_of_one_token_that_stays(V):
+    """Alone, a token's probability is 1 and its log exactly 0, whatever the logits are."""
+    from paper_2609_35139_amd.serving import sample
+    x = _logits(64, V, "f32", V + 1)
+    x[torch.arange(64), x.argmax(1)] += 20
+    u = torch.rand(64, generator=torch.Generator().manual_seed(V))
+    for k in (dict(top_p=0.5, temperature=0.33), dict(top_p=0.5, top_k=V // 3), dict(min_p=0.9), dict(top_k=1)):
+        tokens, log_p = sample(x.cuda(), u.cuda(), **k)
+        assert torch.equal(tokens.cpu().long(), x.argmax(1))
+        assert torch.equal(log_p.cpu(), torch.zeros(64))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sample_rows_anywhere_and_outputs_given(dtype):
     """Rows that begin on any element, further apart than they are long; one row of all."""
