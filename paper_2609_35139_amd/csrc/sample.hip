@@ -14,6 +14,7 @@
 // add in the order that suits it, and what is off is the rounding of each p,
 // 2^-45, a few 2^-36 of a sum of 2^18 of them.
 #include <algorithm>
+#include <type_traits>
 
 #include "answer.h"
 
@@ -229,46 +230,40 @@ struct Sampler {
   // lane's logits, then the lanes' bits one after the other.
   template <typename F>
   __device__ __forceinline__ void each_of(float lo, float hi, const Cut& within, F&& f) const {
-    each_chunk<kReadMost>([&](int c, uint4 (&w)[kReadMost]) {
+    each_chunk<kRead>([&](int c, const uint4 (&w)[kRead]) {
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < kRead; ++u) {
+        float x[VEC];
+        elements(w[u], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) any |= x[e] >= lo;
+      }
+      if (!__any(any)) return;
+      uint32_t bits = 0;
+#pragma unroll
+      for (int u = 0; u < kRead; ++u) {
+        float x[VEC];
+        elements(w[u], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          bits |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << (u * VEC + e);
+      }
 #pragma unroll 1
-      for (int half = 0; half < kReadMost / kRead; ++half) {
-        bool any = false;
+      while (__any(bits != 0)) {
+        const int b = bits ? __ffs(bits) - 1 : 0;
+        uint32_t v = 0;
 #pragma unroll
-        for (int u = 0; u < kRead; ++u) {
-          float x[VEC];
-          elements(w[u], x);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) any |= x[e] >= lo;
+        for (int d = 0; d < kRead * 4; ++d) {
+          const uint4& four = w[d / 4];
+          const uint32_t o = d % 4 == 0 ? four.x : d % 4 == 1 ? four.y : d % 4 == 2 ? four.z : four.w;
+          v = b * (int)sizeof(T) / 4 == d ? o : v;
         }
-        if (__any(any)) {
-          uint32_t bits = 0;
-#pragma unroll
-          for (int u = 0; u < kRead; ++u) {
-            float x[VEC];
-            elements(w[u], x);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-              bits |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << (u * VEC + e);
-          }
-#pragma unroll 1
-          while (__any(bits != 0)) {
-            const int b = bits ? __ffs(bits) - 1 : 0;
-            uint32_t v = 0;
-#pragma unroll
-            for (int d = 0; d < kRead * 4; ++d) {
-              const uint4& four = w[d / 4];
-              const uint32_t o = d % 4 == 0 ? four.x : d % 4 == 1 ? four.y : d % 4 == 2 ? four.z : four.w;
-              v = b * (int)sizeof(T) / 4 == d ? o : v;
-            }
-            if constexpr (sizeof(T) == 2) v = b % 2 ? v & 0xffff0000u : v << 16;
-            const float x = __uint_as_float(v);
-            const int i = first_of<kReadMost>(c, half * kRead + b / VEC) + b % VEC;
-            if (bits && within.keeps(x, i)) f(x, i);
-            bits &= bits - 1;
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < kRead; ++u) w[u] = w[u + kRead];
+        if constexpr (sizeof(T) == 2) v = b % 2 ? v & 0xffff0000u : v << 16;
+        const float x = __uint_as_float(v);
+        const int i = first_of<kRead>(c, b / VEC) + b % VEC;
+        if (bits && within.keeps(x, i)) f(x, i);
+        bits &= bits - 1;
       }
     });
   }
@@ -415,32 +410,42 @@ struct Sampler {
   }
 
   // The bins of [lo, hi] of the tokens that `within` keeps; returns the weight of all of
-  // those, of any value, where by_weight.
-  __device__ __forceinline__ u64 bins(bool by_weight, float lo, float hi, const Cut& within) const {
+  // those, of any value, where by_weight.  Tokens that are few among the row's (and only
+  // counted) are looked for first: 23 us instead of 38 for one in 50 of 151,936, but 71
+  // for one in 3.
+  __device__ __forceinline__ u64 bins(bool by_weight, bool few, float lo, float hi, const Cut& within) const {
     const double scale = scale_of(lo, hi);
     clear_bins();
     u64 sum = 0;
-    each_vector([&](int, const float (&x)[VEC], int i) {
-      u64 q[VEC];
+    if (few && !by_weight) {
+      each_of(lo, hi, within, [&](float x, int) { atomicAdd(&sh.count[bin_of(x, hi, scale)], 1u); });
+      __syncthreads();
+      return 0;
+    }
+    auto dense = [&](auto weighed) {
+      each_chunk<1>([&](int c, const uint4 (&w)[1]) {
+        float x[VEC];
+        u64 q[VEC];
+        elements(w[0], x);
+        const int i = first_of<1>(c, 0);
+        if constexpr (weighed) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) q[e] = by_weight ? weigh(x[e]) : 0;
-      const uint32_t kept = kept_bits(x, i, within);
-      uint32_t in = 0;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        sum += q[e] & when_bit(kept, e);
-        in |= (uint32_t)((x[e] >= lo) & (x[e] <= hi)) << e;
-      }
-      in &= kept;
-      if (!__any(in != 0)) return;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if ((in >> e) & 1) {
-          const int b = bin_of(x[e], hi, scale);
-          atomicAdd(&sh.count[b], 1u);
-          if (by_weight) atomicAdd(&sh.mass[b], q[e]);
+          for (int e = 0; e < VEC; ++e) q[e] = weigh(x[e]);
         }
-    });
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const bool kept = within.keeps(x[e], i + e);
+          if constexpr (weighed) sum += q[e] & when(kept);
+          if (kept & (x[e] >= lo) & (x[e] <= hi)) {
+            const int b = bin_of(x[e], hi, scale);
+            atomicAdd(&sh.count[b], 1u);
+            if constexpr (weighed) atomicAdd(&sh.mass[b], q[e]);
+          }
+        }
+      });
+    };
+    if (by_weight) dense(std::true_type{});
+    else dense(std::false_type{});
     return all(sum);
   }
   __device__ __forceinline__ void reduce_range(float& least, float& most) const {
@@ -797,13 +802,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     const bool by_weight = stage == 1;
     if (n_list >= 0 || (by_weight ? !(top_p < 1.f) : k == 0)) continue;
     const Cut within = cut;
+    const bool few = k * 100 <= (u64)a.vocab;
     float lo = fmaxf(kLowest, by_weight ? top + temperature * (logf((1.f - top_p) / (float)a.vocab) - 0.01f)
-                                        : k * 100 <= (u64)a.vocab ? low : low - (top - low));
+                                        : few ? low : low - (top - low));
     float hi = top;
     u64 need = k, above = 0;
 #pragma unroll 1
     for (bool first = true;; first = false) {
-      const u64 sum = s.bins(by_weight, lo, hi, within);
+      const u64 sum = s.bins(by_weight, few, lo, hi, within);
       if (by_weight && first) {
         of = sum;
         need = S::share_of(top_p, of);
