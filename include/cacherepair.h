@@ -663,11 +663,11 @@ CR_API cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32
  *  budgets:   device, n_seqs, or NULL: a sequence's own budget, within [0, budget].
  *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget] int32: the slots
  *             that stay, ascending, then -1.
- *  kept_lens: device, n_seqs int32: m.
+ *  kept_lens: device, n_seqs int32: m.  Not kv_lens or budgets, nor any part of them.
  * n_layers and n_kv_heads are the layout's; nothing else of it is used.
- * Errors: CR_ERR_NULL, CR_ERR_DIMS (layers, heads, budget < 1, first or recent
- * < 0, a table of more than 2^30 slots, a batch that takes 2^32 threads),
- * CR_ERR_OFFSETS (n_seqs), CR_ERR_LAYOUT (table, weights), CR_ERR_DEVICE before
+ * Errors: CR_ERR_NULL, CR_ERR_DIMS (layers, heads, budget outside [1, 2^30], first
+ * or recent < 0, a table of more than 2^30 slots, a batch that takes 2^32 threads),
+ * CR_ERR_OFFSETS (n_seqs), CR_ERR_LAYOUT (table, weights, kept_lens), CR_ERR_DEVICE before
  * any enqueue; CR_ERR_LAUNCH.
  */
 typedef struct {
@@ -684,7 +684,7 @@ CR_API cr_status cr_choose_slots(const cr_kv_layout* layout, const cr_sequences*
  *   K, V, W[l, s, h, i] <- K, V, W[l, s, h, kept[l, s, h, i]],  i < kept_lens[s],
  * and sets the weights from there to the sequence's old end to 0.  kv_lens are
  * the lengths before; those after are kept_lens, which the caller makes the
- * batch's (and gives cr_append_kv positions from then on: a token's slot is no
+ * batch's afterwards, not a buffer that is both (and gives cr_append_kv positions from then on: a token's slot is no
  * longer its position).  Keys keep the rotation of the position that they had.
  *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget], as cr_choose_slots
  *             leaves it or the caller's own: ascending, each below its

@@ -12,7 +12,8 @@ from .binding import (  # noqa: F401
     CR_DTYPE_BF16, CR_DTYPE_F32, CrError, cr_append_kv, cr_attend, cr_attend_workspace_bytes,
     cr_choose_slots, cr_chunk_schedule, cr_compact_kv, cr_dims, cr_kv_layout, cr_prepare_weights,
     cr_prepared_bytes, cr_repair, cr_sample, cr_status_string, cr_version, cr_weigh_keys,
-    cr_weigh_workspace_bytes, cr_weights_layout, cr_workspace_bytes, cr_workspace_view, layer_major_layout, load,
+    cr_weigh_workspace_bytes, cr_weights_layout, cr_workspace_bytes, cr_workspace_view,
+    layer_major_layout, load,
     make_dims,
 )
 

@@ -12,7 +12,13 @@ namespace {
 
 using namespace cr;   // the helpers of validate.h, serve_checks.h and profile.h
 
-constexpr int64_t kMostSlots = (int64_t)1 << 30;   // of a sequence's weights
+constexpr int64_t kMostSlots = (int64_t)1 << 30;   // of a sequence's weights, or in its list
+
+// Lengths that a call writes, or reads beside kv_lens, in those it only reads.
+bool lens_overlap(const int32_t* a, const int32_t* b, int n) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && (x < y ? y - x : x - y) < (uintptr_t)n * 4;
+}
 
 // The weights' rows, one of the table's slots for each layer, sequence and head.
 cr_status check_weights(const cr_key_weights* w, int n_layers, int n_heads, const cr_sequences* q) {
@@ -161,7 +167,12 @@ cr_status cr_choose_slots(const cr_kv_layout* layout, const cr_sequences* seqs,
     return CR_ERR_NULL;
   cr_status st = check_slots(layout, seqs);
   if (st != CR_OK) return st;
-  if (choice->budget < 1 || choice->first < 0 || choice->recent < 0) return CR_ERR_DIMS;
+  if (choice->budget < 1 || choice->budget > kMostSlots || choice->first < 0 || choice->recent < 0)
+    return CR_ERR_DIMS;
+  // (a workgroup would read what another has written)
+  if (lens_overlap(kept_lens, seqs->kv_lens, seqs->n_seqs) ||
+      lens_overlap(kept_lens, choice->budgets, seqs->n_seqs))
+    return CR_ERR_LAYOUT;
   if ((st = check_weights(weights, layout->n_layers, layout->n_kv_heads, seqs)) != CR_OK) return st;
   if ((st = check_device()) != CR_OK) return st;
   ChooseArgs a{};
@@ -191,7 +202,9 @@ cr_status cr_compact_kv(void* kv, const cr_kv_layout* layout, const cr_sequences
   cr_status st = check_cache(layout);
   if (st != CR_OK) return st;
   if ((st = check_slots(layout, seqs)) != CR_OK) return st;
-  if (budget < 1) return CR_ERR_DIMS;
+  if (budget < 1 || budget > kMostSlots) return CR_ERR_DIMS;
+  // (with the lengths after for those before, every slot behind them would be dropped)
+  if (lens_overlap(kept_lens, seqs->kv_lens, seqs->n_seqs)) return CR_ERR_LAYOUT;
   if (table_out && (max_blocks_out < 1 || (int64_t)max_blocks_out * seqs->block_size > kMostSlots))
     return CR_ERR_LAYOUT;
   if ((st = check_blocks(layout, seqs)) != CR_OK) return st;

@@ -418,7 +418,7 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
 template <int LOG>
 hipError_t compact_as(const CompactArgs& a, int columns, hipStream_t s) {
   const int64_t rows = (int64_t)a.n_layers * a.seqs.n_seqs * a.n_kv;
-  const int64_t steps = (a.budget + MoveCfg<LOG>::MOVE - 1) / MoveCfg<LOG>::MOVE;
+  const int64_t steps = ((int64_t)a.budget + MoveCfg<LOG>::MOVE - 1) / MoveCfg<LOG>::MOVE;
   // out of place: about eight workgroups to a CU
   const int64_t z = a.table_out ? std::max<int64_t>(1, std::min(steps, 2048 / (2 * rows))) : columns;
   const dim3 grid((unsigned)rows, a.weights.data ? 3 : 2, (unsigned)z);

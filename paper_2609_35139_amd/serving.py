@@ -43,6 +43,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
 _DTYPE = {torch.bfloat16: B.CR_DTYPE_BF16, torch.float32: B.CR_DTYPE_F32}
 
 
+def _int32(v: int) -> int:
+    """The nearest number that 32 bits hold (ctypes drops the others' upper bits)."""
+    return max(-(1 << 31), min(v, (1 << 31) - 1))
+
+
 def _on_device(device: torch.device, stream: Optional[torch.cuda.Stream], call) -> None:
     """call(stream handle) with the device and the call's stream as torch's current
     ones: the library launches on the current device, and a workspace or result
@@ -300,7 +305,7 @@ class PagedCache:
         w = self._weights(seqs, weights)
         S = seqs.kv_lens.shape[0]
         shape = (self.layout.n_layers, S, self.n_kv_heads, budget)
-        c = B.cr_choice(budget, first, recent, self._index(budgets, S, "budgets"))
+        c = B.cr_choice(_int32(budget), _int32(first), _int32(recent), self._index(budgets, S, "budgets"))
         if kept is not None:
             self._list(kept, shape, "kept")
         if kept_lens is not None:
@@ -373,7 +378,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
         if isinstance(value, torch.Tensor):
             setattr(o, many, rows(value, dtype, one))
         else:
-            setattr(o, one, value)
+            setattr(o, one, _int32(value) if dtype is torch.int32 else value)
     x = B.cr_logits(logits.data_ptr(), _DTYPE[logits.dtype], n, vocab, st[0] if n > 1 else 0)
     numbers = rows(u, torch.float32, "u")
     if tokens is not None:

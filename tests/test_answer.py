@@ -35,11 +35,11 @@ def _weigh(lay, q, kv=0x10000, layer=1, qr=None, heads=4, w=None, options=True, 
     return e.value.name
 
 
-def _choose(lay, q, w=None, budget=8, first=1, recent=2, kept=0xa00000, lens=0xb00000):
+def _choose(lay, q, w=None, budget=8, first=1, recent=2, kept=0xa00000, lens=0xb00000, budgets=None):
     with pytest.raises(B.CrError) as e:
         B.cr_choose_slots(lay, q, w or _weights(lay.n_layers, q.n_seqs, lay.n_kv_heads,
                                                 max(q.max_blocks * q.block_size, 1)),
-                          B.cr_choice(budget, first, recent, None), kept, lens)
+                          B.cr_choice(budget, first, recent, budgets), kept, lens)
     return e.value.name
 
 
@@ -148,6 +148,34 @@ def test_bad_choices():
     assert _choose(lay, q, recent=-1) == "CR_ERR_DIMS"
     assert _choose(lay, q, kept=0) == "CR_ERR_NULL"
     assert _choose(lay, q, lens=0) == "CR_ERR_NULL"
+
+
+def test_lists_past_what_their_indexes_hold():
+    lay, q = _batch()
+    assert _choose(lay, q, budget=(1 << 30) + 1) == "CR_ERR_DIMS"
+    assert _compact(lay, q, budget=(1 << 31) - 1) == "CR_ERR_DIMS"
+
+
+def test_lengths_after_in_the_lengths_before():
+    """Sequences' workgroups would read lengths that another one has written; a compaction
+    would take the new lengths for the old ones."""
+    lay, q = _batch()
+    for at in (0, 4, -4):
+        assert _choose(lay, q, lens=q.kv_lens + at) == "CR_ERR_LAYOUT"
+        assert _compact(lay, q, lens=q.kv_lens + at) == "CR_ERR_LAYOUT"
+        assert _choose(lay, q, lens=0xd00000 + at, budgets=0xd00000) == "CR_ERR_LAYOUT"
+    if torch.cuda.is_available():
+        return
+    for at in (4 * q.n_seqs, -4 * q.n_seqs):                   # next to each other
+        assert _choose(lay, q, lens=q.kv_lens + at) == "CR_ERR_DEVICE"
+        assert _compact(lay, q, lens=q.kv_lens + at) == "CR_ERR_DEVICE"
+
+
+def test_settings_that_32_bits_do_not_hold():
+    """A limit of 2^32 + 1 tokens is not one of one token."""
+    from paper_2609_35139_amd.serving import _int32
+    assert [_int32(v) for v in (0, -3, 7, (1 << 32) + 1, -(1 << 40), (1 << 31) - 1)] == \
+        [0, -3, 7, (1 << 31) - 1, -(1 << 31), (1 << 31) - 1]
 
 
 def test_bad_compactions():
