@@ -56,7 +56,16 @@ cr_status check_slots(const cr_kv_layout* l, const cr_sequences* q) {
 cr_status check_weigh(const cr_kv_layout* l, const cr_sequences* q, int n_heads, Batch* b) {
   return check_attend(l, q, n_heads, 0, b);
 }
-// Which kernel a call takes, and its workspace.
+// Which kernel a call takes, and its workspace.  Rows of a sequence and KV head:
+//  - up to 16, what an instruction takes at once: a wave for each tile of keys (64
+//    sequences of 8,192 slots, 32 query and 8 KV heads of 128: 227 us; four waves to a
+//    tile's rows, three of them idle, 650);
+//  - up to 512, where the table has room for at most 768 tiles: four waves share a
+//    tile's rows (one sequence of 4,000 slots, the same heads: 9 us for 20 rows, 11 for
+//    128, 19 for 512, 32 for 1,024; through LDS 16, 18, 24, 32);
+//  - else the rows go through LDS for twice the keys (8,000 slots: 14, 17, 28, 41 us;
+//    without 19, 20, 34, 55), and where tiles are few, units share a tile's rows (4,000
+//    slots, 2,048 rows: 48 us; not shared 58).
 struct WeighPlan {
   int kind = kWeighToken, slots = 0;
   uint64_t table = 0, info = 0, partial = 0, total = 0;
@@ -65,16 +74,19 @@ WeighPlan weigh_plan(const cr_kv_layout* l, const cr_sequences* q, const Batch& 
   WeighPlan p;
   if (!b.n_tokens) return p;
   const int group = n_heads / l->n_kv_heads;
-  p.kind = b.most * group <= 16 ? kWeighToken : b.most * group <= 256 ? kWeighRows : kWeighWide;
+  const int keys = weigh_keys((int)esize(l->dtype), l->head_dim);
+  const int64_t slots = (int64_t)q->max_blocks * q->block_size;
+  const auto tiles = [&](int n) { return (int64_t)q->n_seqs * ceil_div(slots, n) * l->n_kv_heads; };
+  p.kind = b.most * group <= 16                                ? kWeighToken
+           : b.most * group <= 512 && tiles(keys) <= kWeighSlots ? kWeighRows
+                                                                 : kWeighWide;
   Arena a;
   if (b.off && q->n_seqs > kTableSeqs) p.table = a.take(((uint64_t)q->n_seqs + 1) * 4);
   if (p.kind == kWeighWide) {
     p.info = a.take(((uint64_t)b.n_tokens * n_heads + 64) * 32);
-    const int keys = 2 * weigh_keys((int)esize(l->dtype), l->head_dim);
-    if ((int64_t)q->n_seqs * ceil_div((int64_t)q->max_blocks * q->block_size, keys) * l->n_kv_heads * 2 <=
-        kWeighSlots) {
+    if (tiles(2 * keys) * 2 <= kWeighSlots) {
       p.slots = kWeighSlots;
-      p.partial = a.take((uint64_t)kWeighSlots * keys * 4);
+      p.partial = a.take((uint64_t)kWeighSlots * 2 * keys * 4);
     }
   }
   p.total = a.off;

@@ -176,6 +176,81 @@ def test_weigh_many_ragged_sequences():
     _weigh_case(Batch("bf16", 4, 1, 32, 4, q, lens, seed=1), 0)
 
 
+# rows that go through LDS: more than 512 in a sequence, or some over many tiles
+WIDE = {
+    "long": dict(dtype="bf16", heads=8, kv_heads=2, d=128, bs=16, q=[133, 0, 3], lens=[300, 4, 100]),
+    "long-odd": dict(dtype="bf16", heads=7, kv_heads=1, d=64, bs=8, q=[75, 1], lens=[170, 400]),
+    "long-f32": dict(dtype="f32", heads=9, kv_heads=1, d=96, bs=2, q=[60, 2], lens=[60, 300]),
+    "many": dict(dtype="bf16", heads=24, kv_heads=8, d=64, bs=32, q=[7, 0, 1, 6] * 10,
+                 lens=[150, 40, 1, 190] * 10),
+    "many-f32": dict(dtype="f32", heads=12, kv_heads=6, d=32, bs=16, q=[9, 1, 13] * 15,
+                     lens=[9, 130, 141] * 15),
+}
+
+
+@pytest.mark.parametrize("name", WIDE)
+@pytest.mark.parametrize("kind", ["causal", "intervals", "cap", "slopes", "all"])
+def test_weigh_rows_through_lds(name, kind):
+    b = Batch(L=1, seed=7 + len(name), fill=-6.0, **WIDE[name])
+    rng = np.random.default_rng(6)
+    o = {}
+    if kind in ("intervals", "all"):
+        lo = rng.integers(-5, 180, b.N)
+        o.update(lo=lo.tolist(), hi=(lo + rng.integers(-3, 200, b.N)).tolist())
+    if kind in ("cap", "all"):
+        o["softcap"] = 3.0
+    if kind in ("slopes", "all"):
+        o.update(slopes=[0.2 * 2.0 ** -(h % 8) for h in range(b.heads)], scale=0.15)
+    w, cache, seqs, q, lse, prior, k = _weigh_case(b, 0, **o)
+    from paper_2609_35139_amd import binding as B
+    assert B.cr_weigh_workspace_bytes(cache.layout, seqs.struct, b.heads) > 0
+    again = prior.cuda()
+    cache.weigh(0, seqs, q, lse, again, **k)
+    assert torch.equal(again, w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", range(32, 257, 32))
+def test_weigh_rows_through_lds_of_every_head_dim(dtype, d):
+    _weigh_case(Batch(dtype, 8, 1, d, 16, [70], [170], seed=d), 0)
+
+
+def test_weigh_rows_through_lds_do_not_look_at_hidden_keys():
+    b = Batch("bf16", 8, 1, 64, 16, [80], [150], seed=2, fill=NAN)
+    for j in range(40, 150):
+        blk, r = b.row(0, j)
+        b.pool[0, 0, blk, r] = [INF, -INF, NAN][j % 3]
+    w, cache, seqs, q, lse, prior, k = _weigh_case(b, 0, hi=[40] * 80)
+    blk, r = b.row(0, 3)
+    cache.pool[0, 0, blk, r] = NAN
+    w2 = prior.cuda()
+    cache.weigh(0, seqs, q, lse, w2, **k)
+    assert torch.isnan(w2).nonzero().tolist() == [[0, 0, 0, 3]]
+
+
+@pytest.mark.parametrize("lse_of_one", [NAN, INF])
+def test_weigh_rows_through_lds_without_a_sum(lse_of_one):
+    """Rows whose lse is -inf, NaN or +inf among more than 512."""
+    q = 140
+    b = Batch("bf16", 4, 1, 64, 16, [q, q], [q + 30, q + 50], seed=q)
+    _, lse, _, _ = attend_oracle(b, 0)
+    cache, seqs, qh, _, _ = b.cuda()
+    dead = lse.float().cuda()
+    dead[:q] = -INF
+    w = cache.new_weights(seqs)
+    cache.weigh(0, seqs, qh, dead, w)
+    assert torch.equal(w[0, 0], torch.zeros_like(w[0, 0])) and float(w[0, 1].sum()) > 0
+    whole = w.clone()
+    dead[0] = lse_of_one
+    w.zero_()
+    cache.weigh(0, seqs, qh, dead, w)
+    assert torch.equal(w[0, 1], whole[0, 1])
+    if lse_of_one == INF:
+        assert torch.equal(w, whole)
+    else:
+        assert torch.isnan(w[0, 0, :, :31]).all() and not torch.isnan(w[0, 0, :, 31:]).any()
+
+
 def test_weigh_parts_of_few_tiles():
     """One long prompt over a short cache: its rows are split and joined."""
     b = Batch("bf16", 16, 1, 64, 16, [120], [120], seed=6)
