@@ -105,7 +105,8 @@ struct SampleShared {
 
 // A row is read in chunks of U vectors for each lane of a wave, wave w taking chunks
 // w, w + 8, ...: eight where a pass only compares (its loads are what it waits for: 7 us
-// for 151,936 logits), four where it forms weights.  What is done for a logit stands in
+// for 151,936 logits), four where it sums weights, one where it bins them (four: 3% slower,
+// the bins' code is the longer).  What is done for a logit stands in
 // the code once, for a vector or for four: a workgroup runs through most of this code
 // once, and a line of it that is not in the instruction cache takes about a microsecond
 // (everything unrolled over eight vectors: 180 KB, and 45 us for a pass that finds 360
