@@ -47,7 +47,9 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
   typedef uint32_t Counts __attribute__((ext_vector_type(COPIES)));
   __shared__ Counts hist[kChooseBins];
   __shared__ __align__(16) uint32_t few[FEW];
-  __shared__ uint32_t scratch[WAVES * 2], found[3];
+  // (the list's counts have a place of their own: where all weights are equal, no barrier
+  // lies between the last look at the range in `scratch` and the first count)
+  __shared__ uint32_t scratch[WAVES * 2], counts[WAVES * 2], found[3];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.x % a.n_kv, ls = blockIdx.x / a.n_kv;
@@ -245,10 +247,10 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
       equal_at += __popcll(r.equal[e]);
     }
   });
-  if (lane == 0) { scratch[wave] = sure_at; scratch[WAVES + wave] = equal_at; }
+  if (lane == 0) { counts[wave] = sure_at; counts[WAVES + wave] = equal_at; }
   __syncthreads();
   sure_at = equal_at = 0;
-  for (int i = 0; i < wave; ++i) { sure_at += scratch[i]; equal_at += scratch[WAVES + i]; }
+  for (int i = 0; i < wave; ++i) { sure_at += counts[i]; equal_at += counts[WAVES + i]; }
   each_vector([&](const uint4& k, int i) {
     const Marks r = marks_of(k, i);
     // those of the lanes before this one, of all four slots
