@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "answer.h"
+#include "sample_weights.h"
 
 namespace cr {
 
@@ -29,7 +30,6 @@ constexpr int kMostTopK = 256;
 // 30 and 33; 200: 39 and 35)
 constexpr int kSampleShort = 160;
 
-typedef unsigned long long u64;
 typedef u64 Pair __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t order_of(float x) {      // whole numbers in the order of x
@@ -38,48 +38,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {      // whole numbers in
 }
 __device__ __forceinline__ float value_of(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
-
-// exp((x - x_0) / T) 2^shift.  With c = 64 log2(e) / T, x c - x_0 c = n + r - f: n whole,
-// |r| <= 1/2, f what x_0 c is off a whole number, the same for all tokens.  2^(n / 64)
-// comes from a table (with 2^(-f / 64) in it) and the exponent, 2^(r / 64) by its series
-// up to the fourth power (relative error 4e-14, below a step for all but the largest).
-// Products inside the fused operations are exact, so nothing is lost however far x and x_0
-// are from 0.  Ten fp64 operations, at half the rate of fp32 ones: a row of 151,936
-// logits takes a CU 46 us, by the operations: neither the chains of eight logits side by
-// side, a stage at a time, nor a table for each bank change that.
-constexpr int kExpTable = 64;
-struct Weigher {
-  const double* table;   // 2^((j - f) / 64) 2^shift
-  double c, whole;       // whole: 1.5 2^52 less the whole number next to x_0 c
-  float lowest;          // what lies below weighs less than 2^-20 steps
-  __device__ __forceinline__ u64 operator()(float logit) const {
-    const double x = (double)(logit > lowest ? logit : lowest);      // (NaN too)
-    const double m = __builtin_fma(x, c, whole);
-    // (the float next to the lowest may lie further down; what it weighs is still no step)
-    const int n = max((int)(__double_as_longlong(m) & 0xffffffff), -80 * kExpTable);
-    const long long b =
-        __double_as_longlong(table[n & (kExpTable - 1)]) + ((long long)(n & ~(kExpTable - 1)) << 46);
-    const double r = __builtin_fma(x, c, whole - m);
-    constexpr double y = 0.69314718055994530942 / kExpTable;
-    double e = __builtin_fma(r, y * y * y * y / 24., y * y * y / 6.);
-    e = __builtin_fma(e, r, y * y / 2.);
-    e = __builtin_fma(e, r, y);
-    e = __builtin_fma(e, r, 1.);
-    // in whole steps: added to 2^52, the bits are kOffset + the weight
-    return (u64)__double_as_longlong(__builtin_fma(__longlong_as_double(b), e, 4503599627370496.)) - kOffset;
-  }
-  static constexpr u64 kOffset = 0x4330000000000000ull;
-};
-// The smallest logit whose p is at least min_p, which is that of (x - x_0) / T >=
-// log(min_p): so min_p is a bound of the logits themselves.
-__device__ __forceinline__ float least_logit(float min_p, double top, double temperature) {
-  const double t = temperature * log((double)min_p);
-  auto holds = [&](float x) { return (double)x - top >= t; };
-  float x = fmaxf((float)(top + t), -3.402823466e38f);
-  for (int i = 0; i < 4 && !holds(x); ++i) x = nextafterf(x, INFINITY);
-  for (int i = 0; i < 4 && holds(nextafterf(x, -INFINITY)); ++i) x = nextafterf(x, -INFINITY);
-  return fminf(x, (float)top);
 }
 
 // Where the tokens that stay end: those above v, and of those equal to v the ones
@@ -753,19 +711,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     return answer(s.locate(S::target_of(u, m), equal), -(float)log((double)m));
   }
   const double one = ldexp(1., shift);
-  {
-    const double next = rint(at_top), off = (at_top - next) + __builtin_fma((double)top, c, -at_top);
-    if (tid < kExpTable) sh.table[tid] = exp2((tid - off) / kExpTable) * one;
-    s.weigh = Weigher{sh.table, c, 6755399441055744. - next,
-                      fmaxf((float)((double)top - 64. * kExpTable / c), -3.402823466e38f)};
-  }
+  if (tid < kExpTable) sh.table[tid] = Weigher::entry(tid, top, c, one);
+  s.weigh = Weigher::of(sh.table, top, c);
   // (the largest logit's own weight, which may be off by a step: alone, its log is 0)
   auto finish = [&](int token, float x, u64 total) {
     const double q = (double)s.weigh(top);
     answer(token, (float)(((double)x - (double)top) / (double)temperature - log((double)total / q)));
   };
   // no token below `least` can stay by min_p
-  constexpr float kLowest = -3.402823466e38f;
+  constexpr float kLowest = kLowestLogit;
   const float least = min_p > 0.f ? least_logit(min_p, top, temperature) : kLowest;
   __syncthreads();                         // (the table)
 
