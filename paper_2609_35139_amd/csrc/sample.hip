@@ -752,17 +752,18 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   }
   // ---- else where the first k end, then where top-p ends: by bins of the values, from a
   // bound down to which they are likely to lie (about one in 50 tokens is not below the
-  // least of the threads' largest), or below which no token can stay (all of them together
-  // weigh less than 1 - top_p); the bin in which the end lies becomes the range, until its
-  // tokens fit the list or are all equal
+  // least of the threads' largest), or below which hardly a token can stay (by their logits
+  // all of them together weigh less than 1 - top_p; what is held of each may be up to half
+  // a step more); if it lies lower it is looked for among all; the bin in which the end lies
+  // becomes the range, until its tokens fit the list or are all equal
 #pragma unroll 1
   for (int stage = 0; stage < 2; ++stage) {
     const bool by_weight = stage == 1;
     if (n_list >= 0 || (by_weight ? !(top_p < 1.f) : k == 0)) continue;
     const Cut within = cut;
     const bool few = k * 100 <= (u64)a.vocab;
-    float lo = fmaxf(kLowest, by_weight ? top + temperature * (logf((1.f - top_p) / (float)a.vocab) - 0.01f)
-                                        : few ? low : low - (top - low));
+    float lo = by_weight ? at_most(top + (double)temperature * (logf((1.f - top_p) / (float)a.vocab) - 0.01f))
+                         : fmaxf(kLowest, few ? low : low - (top - low));
     float hi = top;
     u64 need = k, above = 0;
 #pragma unroll 1
@@ -774,8 +775,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
       }
       const auto f = s.find(by_weight, need, above);
       if (f.bin >= kSampleBins) {
-        if (by_weight || lo == kLowest) break;         // all of them stay
-        lo = kLowest;
+        if (lo == kLowest) break;                      // all of them stay
+        lo = kLowest;                                  // the end lies below the bound
         continue;
       }
       const double scale = S::scale_of(lo, hi);

@@ -101,3 +101,18 @@ def test_sample_one_row_of_a_large_vocabulary_at_small_temperatures():
         for t in (1e-6, 1e-8, 1e-10):
             for k in (dict(), dict(top_k=50), dict(top_k=9000), dict(top_p=0.9)):
                 _sample_case(x, temperature=t, **k)
+
+
+def test_sample_top_p_whose_end_lies_below_its_bound():
+    """220,000 tokens, each just below the weight at which all of them together would be
+    1 - top_p, weigh 4.70 steps and are held as 5: more than 1 - top_p, so the end lies among them
+    and not above the bound.  By the weights themselves the first token alone stays; by those held,
+    it and the first 10,285 others of 5 2^-44 each.  Either way u, 2^-24 below 1, draws the first."""
+    V, p = 220000, 1 - 2.0 ** -24
+    bound = math.log(2.0 ** -24 / V) - 0.01
+    x = torch.full((2, V), bound - 0.003)
+    x[0, 0] = x[1, 0] = 0.0
+    step = math.exp(float(x[0, 1])) * 2.0 ** 44
+    assert 4.5 < step < 2.0 ** 20 / V                  # rounds upwards, past the share of each
+    x[1] += 8.0
+    _sample_case(x, torch.full((2,), p), top_p=p)
