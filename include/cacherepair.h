@@ -550,7 +550,8 @@ CR_API cr_status cr_append_kv(void* kv, const cr_kv_layout* layout, int32_t laye
  *  scale:      factor of q.k, > 0 (0 = 1 / sqrt(head_dim)).
  *  softcap:    0, or > 0: scores become softcap * tanh(score / softcap).
  *  slopes:     NULL, or host, n_heads entries: slopes[h] * |p - j| is taken off
- *              the score of the query in slot p and the key in slot j.
+ *              the score of the query in slot p and the key in slot j (slots, not
+ *              positions: after cr_compact_kv they differ).
  *  lo, hi:     device, n_tokens int32 each, or NULL: query t sees the keys in
  *              slots [lo[t], hi[t]) of its sequence (within the sequence's
  *              length and the table).  lo NULL = 0; hi NULL = causal, up to the query's own
@@ -639,8 +640,11 @@ typedef struct {
  *             arguments, 256-byte aligned; contents undefined after the call.
  *             Calls that may overlap in time need their own.
  * Scores, exponentials and sums are fp32, the sums in an order that depends on
- * sizes and lengths alone.  A key that is seen and not finite makes its own
- * slot's weight infinite or NaN; where lse is NaN, all that the row sees.
+ * sizes and lengths alone.  A key that is seen and not finite can make its own
+ * slot's weight infinite or NaN, and no other; where lse is NaN, all that the row
+ * sees are.  A probability is the exponential of the difference of two fp32 numbers:
+ * scores and lse of magnitude x leave it off by up to x 2^-20 of itself, so that from
+ * 2^20 on it says nothing (from 2^30 on it may be infinite or NaN).
  * n_tokens == 0 returns CR_OK with nothing enqueued.
  * Errors as cr_attend; CR_ERR_NULL also without options or lse, CR_ERR_LAYOUT
  * also for the weights' strides and alignment.
@@ -684,17 +688,24 @@ CR_API cr_status cr_choose_slots(const cr_kv_layout* layout, const cr_sequences*
  *   K, V, W[l, s, h, i] <- K, V, W[l, s, h, kept[l, s, h, i]],  i < kept_lens[s],
  * and sets the weights from there to the sequence's old end to 0.  kv_lens are
  * the lengths before; those after are kept_lens, which the caller makes the
- * batch's afterwards, not a buffer that is both (and gives cr_append_kv positions from then on: a token's slot is no
- * longer its position).  Keys keep the rotation of the position that they had.
+ * batch's afterwards, not a buffer that is both.
+ * From then on a token's slot is no longer its position.  Keys keep the rotation of
+ * the position that they had, so cr_append_kv is given positions; causal calls see
+ * all slots that stayed.  But slopes, lo and hi of cr_attend and cr_weigh_keys go by
+ * slots: a distance is that between the slots that are left, shorter than the one
+ * between the tokens, and differs from head to head where their lists do; an interval
+ * cuts the slots that are left.  A model with slopes or windows gets other scores
+ * than before the compaction.
  *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget], as cr_choose_slots
  *             leaves it or the caller's own: ascending, each below its
- *             sequence's length (an entry that is no such slot, or whose slot
- *             lies in no block, moves nothing).
+ *             sequence's length.  An entry that is no such slot moves nothing;
+ *             one whose slot, or the place for it, lies in no block moves its
+ *             weight alone.
  *  table_out: NULL = in place; a block that several sequences share must not be
  *             compacted in place.  Otherwise device, n_seqs rows of
  *             max_blocks_out block ids: the blocks to fill, none of which may
  *             be a block that is read; what they hold is left alone where
- *             nothing moves.  A slot past that table is dropped.
+ *             nothing moves.  Keys and values past that table are dropped.
  *  weights:   NULL = none.
  * Errors as cr_choose_slots, and CR_ERR_DTYPE; layout and blocks as
  * cr_append_kv.

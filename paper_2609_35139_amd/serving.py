@@ -21,6 +21,10 @@ and, once sequences grow past their budget::
     cache.compact(step, kept, kept_lens, weights=weights)
     kv_lens.copy_(kept_lens)      # appends take positions= from here on
 
+From a compaction on a token's slot is not its position: ``slopes``, ``lo`` and ``hi`` of
+:meth:`PagedCache.attend` and :meth:`PagedCache.weigh` go by the slots that are left, so a
+model with distance slopes or windows gets other scores than before it.
+
 Calls go to ``stream``, or to torch's current stream on the cache's device.
 Where that is not the stream that a tensor was allocated on, the caller orders
 the two and keeps the tensor (or calls its ``record_stream``) until the call
@@ -329,7 +333,8 @@ class PagedCache:
                 stream: Optional[torch.cuda.Stream] = None) -> None:
         """Moves the slots that stay to the front, with their weights (cr_compact_kv): in place,
         or into the blocks of block_table (device int32 [n_seqs][blocks]).  seqs has the lengths
-        before; kept_lens are those after."""
+        before; kept_lens are those after.  Slots are not positions from then on: appends take
+        positions=, slopes and intervals go by slots."""
         self._tokens(seqs)
         S = seqs.kv_lens.shape[0]
         if kept.dim() != 4:
