@@ -6,8 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from serving_helpers import TORCH
-from test_gpu_answer import _i32, _layout_cache, _sample_case
+from serving_helpers import TORCH, Batch
+from test_gpu_answer import _i32, _layout_cache, _sample_case, _weigh_case
 
 pytestmark = pytest.mark.gpu
 INF, NAN = math.inf, math.nan
@@ -19,6 +19,107 @@ def _cuda():
         pytest.skip("no GPU")
     from paper_2609_35139_amd import binding
     binding.load()
+
+
+# -------------------------------------------------------------------- weigh
+def _again(case, b, **o):
+    """The oracle's weights, and the same bits from a second call."""
+    w, cache, seqs, q, lse, prior, k = case
+    again = prior.cuda()
+    cache.weigh(0, seqs, q, lse, again, **k)
+    assert torch.equal(again, w)
+    return w, cache, seqs, q, lse, prior, k
+
+
+# single tokens: (a sequence's queries, slots), more tiles of keys than there are waves, so
+# that a wave has a run of tiles that passes from sequence to sequence
+RUNS = {"bf16": (32, dict(dtype="bf16", heads=32, kv_heads=16, d=64, bs=16)),
+        "f32": (32, dict(dtype="f32", heads=32, kv_heads=16, d=32, bs=8)),
+        "f32-wide": (16, dict(dtype="f32", heads=8, kv_heads=8, d=160, bs=64))}
+
+
+@pytest.mark.parametrize("name", RUNS)
+def test_weigh_single_tokens_of_more_tiles_than_waves(name):
+    keys, sizes = RUNS[name]                             # keys of a tile
+    rng = np.random.default_rng(len(name))
+    S, most = 64, 1024
+    lens = rng.integers(1, most + 1, S)
+    lens[rng.random(S) < 0.15] = 0
+    lens[5], lens[6], lens[S - 1] = most, 1, 33
+    q = np.minimum(rng.choice([0, 1, 1, 1, 2, 8], S), lens)
+    q[5] = 1
+    b = Batch(q=q.tolist(), lens=lens.tolist(), seed=2, **sizes)
+    assert sum(-(-n // keys) for n, m in zip(lens, q) if m) > 2 * 4 * -(-1024 // sizes["kv_heads"])
+    case = _again(_weigh_case(b, 0), b)
+    from paper_2609_35139_amd import binding as B
+    assert B.cr_weigh_workspace_bytes(case[1].layout, case[2].struct, b.heads) == 0
+    lo = rng.integers(0, 500, b.N)
+    _weigh_case(b, 0, lo=lo.tolist(), hi=(lo + rng.integers(0, 600, b.N)).tolist(), softcap=3.0,
+                slopes=[0.01] * b.heads)
+
+
+@pytest.mark.parametrize("kv_heads,dtype", [(1, "bf16"), (1, "f32"), (6, "bf16")])
+def test_weigh_many_ragged_sequences_with_a_prompt_through_lds(kv_heads, dtype):
+    """More sequences than travel with a launch (their offsets in the workspace, beside what the
+    rows bring and, for few tiles, the parts), a prompt of more than 512 rows for a KV head among
+    them, sequences without queries before, behind and last."""
+    rng = np.random.default_rng(3)
+    q = rng.integers(0, 4, 150)
+    lens = q + rng.integers(0, 60, 150)
+    q[7], lens[7] = 140, 150
+    q[[6, 8, 9, 148, 149]] = 0
+    group = 4
+    b = Batch(dtype, group * kv_heads, kv_heads, 32, 4, q.tolist(), lens.tolist(), seed=1)
+    case = _again(_weigh_case(b, 0), b)
+    from paper_2609_35139_amd import binding as B
+    need = B.cr_weigh_workspace_bytes(case[1].layout, case[2].struct, b.heads)
+    rows, keys = b.N * b.heads * 32, 128 if dtype == "bf16" else 64          # of a tile
+    few = 2 * 150 * kv_heads * -(-b.table.shape[1] * 4 // keys) <= 768       # tiles that share parts
+    assert few == (kv_heads == 1 and dtype == "bf16")
+    assert rows + 151 * 4 < need < rows + 8192 + 768 * 4 * keys * few
+    assert not few or need > rows + 768 * 4 * keys
+    lo = rng.integers(-5, 100, b.N)
+    _weigh_case(b, 0, lo=lo.tolist(), hi=(lo + rng.integers(-3, 90, b.N)).tolist(), softcap=2.5)
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [1000] * 16 + [1024, 0, 17]), ("f32", [500] * 16 + [512, 1])])
+def test_weigh_through_lds_of_more_units_than_workgroups(dtype, lens):
+    """More than 8,192 (tile, KV head) units: a workgroup takes several."""
+    q = [min(n, 17) for n in lens]
+    b = Batch(dtype, 64, 64, 32, 16, q, lens, seed=4)
+    keys = 128 if dtype == "bf16" else 64
+    assert sum(-(-n // keys) for n in lens) * 64 > 8192
+    case = _again(_weigh_case(b, 0), b)
+    from paper_2609_35139_amd import binding as B
+    assert B.cr_weigh_workspace_bytes(case[1].layout, case[2].struct, 64) > 0
+
+
+# rows of a KV head: one instruction's, read where they lie, through LDS (in steps where whole
+# queries make up a round of rows, else row by row); heads of a group 1, 4, 5
+FAR = [(1, 4, 64), (30, 4, 64), (140, 4, 64), (120, 5, 128), (600, 1, 32), (140, 4, 256)]
+
+
+@pytest.mark.parametrize("q,group,d", FAR)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weigh_queries_that_lie_apart(q, group, d, dtype):
+    """Queries with gaps between tokens and heads; heads further apart than the steps of the rows'
+    addresses take; tokens so; and as far as they do take."""
+    b = Batch(dtype, group, 1, d, 16, [q], [q + 70], seed=q + d)
+    w, cache, seqs, rows, lse, prior, k = _weigh_case(b, 0)
+    for token, head in ((group * (d + 16) + 40, d + 16), (d, (1 << 20) + 8), ((1 << 24) + 8, d),
+                        ((1 << 23) - 4096, d)):
+        n = (q - 1) * token + (group - 1) * head + d
+        print(f"strides {token} {head}, {n >> 20} Mi elements", flush=True)
+        store = torch.empty(n, dtype=TORCH[dtype], device="cuda")
+        if n < 1 << 24:
+            store.fill_(NAN)
+        apart = torch.as_strided(store, (q, group, d), (token, head, 1))
+        apart.copy_(rows)
+        again = prior.cuda()
+        cache.weigh(0, seqs, apart, lse, again)
+        assert torch.equal(again, w)
+        del store, apart
+        torch.cuda.empty_cache()
 
 
 # ------------------------------------------------------------------- choose
