@@ -35,7 +35,7 @@ struct WeighArgs {
   struct RowInfo* info;
   float* partial;
   int slots;
-  int near;                         // 32 queries lie within 2^31 bytes
+  int near;                         // the rows of a round of transfers lie within 2^31 bytes
 };
 enum { kWeighToken = 0, kWeighRows = 1, kWeighWide = 2 };
 constexpr int kWeighSlots = 768;

@@ -152,8 +152,9 @@ cr_status cr_weigh_keys(const void* kv, const cr_kv_layout* layout, int32_t laye
   char* ws = static_cast<char*>(workspace);
   a.kind = p.kind;
   a.slots = p.slots;
-  const int64_t reach = 32 * q->stride_token + 256 * q->stride_head + 256;
-  a.near = q->stride_token < (1 << 24) && q->stride_head < (1 << 20) && reach * 4 < (int64_t)1 << 31;
+  // (a round of rows spans 64 queries of one head each, or fewer of up to 64 heads)
+  a.near = q->stride_token < (1 << 23) && q->stride_head < (1 << 20) &&
+           (64 * (q->stride_token + q->stride_head) + 256) * 4 < (int64_t)1 << 31;
   a.info = reinterpret_cast<RowInfo*>(ws + p.info);
   a.partial = reinterpret_cast<float*>(ws + p.partial);
   WeighTable tab{};

@@ -422,14 +422,14 @@ __global__ __launch_bounds__(256, (WideCfg<T, D>::RESIDENT)) void weigh_wide_ker
     // Where a round's rows are whole queries, a lane's query and head of the group are the
     // same in every round, and the rest of its address is the same for all lanes.
     constexpr int STEP = 4 * C::RPW;                      // rows of a round
-    const int qt = (int)(a.q_token * (int64_t)sizeof(T)), qh = (int)(a.q_head * (int64_t)sizeof(T));
+    const uint32_t qt = (uint32_t)(a.q_token * (int64_t)sizeof(T)), qh = (uint32_t)(a.q_head * (int64_t)sizeof(T));
     const bool steps = RB <= 256 && STEP % a.group == 0 && a.near;
     uint32_t lane_at;
     {
       const int row = wave * C::RPW + lane_again() / C::CPR, i = row / a.group;
       int ch = (lane_again() % C::CPR) ^ row_swizzle<RB>(row);
       if (D * (int)sizeof(T) < RB && ch * 16 >= D * (int)sizeof(T)) ch = 0;   // (never read)
-      lane_at = (uint32_t)(i * qt + (row - i * a.group) * qh + ch * 16);
+      lane_at = (uint32_t)i * qt + (uint32_t)(row - i * a.group) * qh + ch * 16;   // (used where `near`)
     }
     auto issue = [&](int first, int st) {                 // rows from `first` on into stage st
       char* base = lds + st * C::STAGE;
