@@ -296,44 +296,41 @@ __global__ __launch_bounds__(256) void weigh_rows_kernel(WeighArgs a, WeighTable
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x % a.n_kv;
   const Tiles<KT> tiles(a, tab);
-  for (long long t = blockIdx.x / a.n_kv; t < tiles.total; t += gridDim.x / a.n_kv) {
-    const int2 at = tiles.find(t);
-    const int s = at.x, k0 = at.y * KT;
-    if (s < 0) return;
-    const Queries qs = queries_of(a, tab, s);
-    const int len = seq_len(a.seqs, s), n = min(len, a.seqs.max_len);
-    KeyTile<T, D, KT> keys;
-    keys.load(a, s, head, k0, n);
-    const bool bad = keys.bad();
-    float sum[KA * 4];
+  const int2 at = tiles.find(blockIdx.x / a.n_kv);     // (-1: fewer tiles than there is room for)
+  const int s = at.x, k0 = at.y * KT;
+  if (s < 0) return;
+  const Queries qs = queries_of(a, tab, s);
+  const int len = seq_len(a.seqs, s), n = min(len, a.seqs.max_len);
+  KeyTile<T, D, KT> keys;
+  keys.load(a, s, head, k0, n);
+  const bool bad = keys.bad();
+  float sum[KA * 4];
 #pragma unroll
-    for (int x = 0; x < KA * 4; ++x) sum[x] = 0.f;
-    const int n_rows = qs.nq * a.group;
-    int r0 = wave * 16;
-    if (!a.hi) r0 += max(0, k0 - (len - qs.nq)) * a.group / 16 * 16;   // causal: from query k0 on
-    for (; r0 < n_rows; r0 += 64) {
-      const int r = min(r0 + c16, n_rows - 1), i = r / a.group, gr = r - i * a.group;
-      RowInfo row = row_info(a, len, qs, head, i, gr);
-      if (r0 + c16 >= n_rows) row.hi = row.lo = 0;
-      if (!__any(row.lo < row.hi && row.lo < k0 + KT && row.hi > k0)) continue;
-      const T* qp = static_cast<const T*>(a.q) + (int64_t)(qs.tok0 + i) * a.q_token +
-                    (int64_t)(head * a.group + gr) * a.q_head;
-      frag qf[QF];
+  for (int x = 0; x < KA * 4; ++x) sum[x] = 0.f;
+  const int n_rows = qs.nq * a.group;
+  int r0 = wave * 16;
+  if (!a.hi) r0 += max(0, k0 - (len - qs.nq)) * a.group / 16 * 16;   // causal: from query k0 on
+  for (; r0 < n_rows; r0 += 64) {
+    const int r = min(r0 + c16, n_rows - 1), i = r / a.group, gr = r - i * a.group;
+    RowInfo row = row_info(a, len, qs, head, i, gr);
+    if (r0 + c16 >= n_rows) row.hi = row.lo = 0;
+    if (!__any(row.lo < row.hi && row.lo < k0 + KT && row.hi > k0)) continue;
+    const T* qp = static_cast<const T*>(a.q) + (int64_t)(qs.tok0 + i) * a.q_token +
+                  (int64_t)(head * a.group + gr) * a.q_head;
+    frag qf[QF];
 #pragma unroll
-      for (int kk = 0; kk < QF; ++kk) qf[kk] = load_frag<T, frag>(qp + kk * KSTEP + g * KPL);
-      const bool whole = !bad && __all(row.lo <= k0 && row.hi >= k0 + KT);
-      add_rows<T, D, KT>(a, a.cap_log2 > 0.f || a.bias, keys, k0, qf, row, whole, sum);
-    }
-    const float mine = sum_to_lane(sum, c16);
-    const int id = c16 % (KA * 4), key = (id >> 2) * 16 + 4 * g + (id & 3);
-    if (c16 < KA * 4) part[wave * KT + key] = mine;
-    __syncthreads();
-    const int j = threadIdx.x;
-    if (j < KT && k0 + j < n)
-      a.weights.data[(int64_t)s * a.weights.seq + (int64_t)head * a.weights.head + k0 + j] +=
-          (part[j] + part[KT + j]) + (part[2 * KT + j] + part[3 * KT + j]);
-    __syncthreads();
+    for (int kk = 0; kk < QF; ++kk) qf[kk] = load_frag<T, frag>(qp + kk * KSTEP + g * KPL);
+    const bool whole = !bad && __all(row.lo <= k0 && row.hi >= k0 + KT);
+    add_rows<T, D, KT>(a, a.cap_log2 > 0.f || a.bias, keys, k0, qf, row, whole, sum);
   }
+  const float mine = sum_to_lane(sum, c16);
+  const int id = c16 % (KA * 4), key = (id >> 2) * 16 + 4 * g + (id & 3);
+  if (c16 < KA * 4) part[wave * KT + key] = mine;
+  __syncthreads();
+  const int j = threadIdx.x;
+  if (j < KT && k0 + j < n)
+    a.weights.data[(int64_t)s * a.weights.seq + (int64_t)head * a.weights.head + k0 + j] +=
+        (part[j] + part[KT + j]) + (part[2 * KT + j] + part[3 * KT + j]);
 }
 
 // ---- many rows: queries and what their rows bring go through LDS, for 2 x KT keys of
@@ -533,8 +530,7 @@ hipError_t weigh_as(const WeighArgs& a, const WeighTable& tab, hipStream_t s) {
     const dim3 grid((unsigned)(a.n_kv * (groups < most ? groups : most)));
     CR_LAUNCH((weigh_token_kernel<T, D>), grid, dim3(256), 0, s, a, tab);
   } else if (a.kind == kWeighRows) {
-    const int64_t groups = weigh_tiles(a, weigh_keys(sizeof(T), D)), most = (4096 + a.n_kv - 1) / a.n_kv;
-    const dim3 grid((unsigned)(a.n_kv * (groups < most ? groups : most)));
+    const dim3 grid((unsigned)(weigh_tiles(a, weigh_keys(sizeof(T), D)) * a.n_kv));   // (at most kWeighSlots)
     CR_LAUNCH((weigh_rows_kernel<T, D>), grid, dim3(256), 0, s, a, tab);
   } else {
     constexpr int KEYS = WideCfg<T, D>::KEYS;
