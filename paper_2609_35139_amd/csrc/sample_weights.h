@@ -11,9 +11,11 @@ typedef unsigned long long u64;
 // comes from a table (with 2^(-f / 64) in it) and the exponent, 2^(r / 64) by its series
 // up to the fourth power (relative error 4e-14, below a step for all but the largest).
 // Products inside the fused operations are exact, so nothing is lost however far x and x_0
-// are from 0.  Ten fp64 operations, at half the rate of fp32 ones: a row of 151,936
-// logits takes a CU 46 us, by the operations: neither the chains of eight logits side by
-// side, a stage at a time, nor a table for each bank change that.
+// are from 0.  A pass that forms weights takes a CU 46 us for a row of 151,936 logits and
+// issues about 37 vector instructions for a logit, ten of them fp64 (counters of 256 rows
+// without a filter, less those of the first token alone).  At four cycles of a SIMD each
+// that is 37 us: bound by their number.  Neither the chains of eight logits side by side, a
+// stage at a time, nor a table for each bank changed it.
 constexpr int kExpTable = 64;
 constexpr float kLowestLogit = -3.402823466e38f;      // the type's lowest
 // The largest fp32 number that is not above x, but no less than the lowest.

@@ -274,11 +274,13 @@ __global__ __launch_bounds__(NT) void choose_kernel(ChooseArgs a) {
 
 hipError_t choose(const ChooseArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.n_layers * a.n_seqs * a.n_kv));
-  // 256 threads hold 8,192 slots in registers, 512 hold 32,768.  Where a CU has more than
-  // one workgroup, small ones fill it better (2,304 rows of 8,000 slots: 23 us, with 512
-  // threads 28), else large ones are done sooner (288 rows: 13 us, with 256 threads 16).
-  // Slots that are read again in every pass take twice as long (2,304 rows of 30,000:
-  // 121 us, from registers 63).
+  // 256 threads hold 8,192 slots in registers, 512 hold 32,768.  Where there are more than
+  // two workgroups for a CU, small ones fill it better (2,304 rows of 8,000 slots of which
+  // half stay: 44 us, with 512 threads 60; 520 rows 18.3 and 22.7), else large ones are done
+  // sooner (512 rows: 15 us, with 256 threads 17; 288 rows 14 and 16).  Slots that are read
+  // again in every pass take twice as long (2,304 rows of 30,000: 331 us, from registers
+  // 152).  The rule goes by the table, as the lengths are on the device: rows of 4,000 slots
+  // take 220 us in a table of 65,536 and 28 in one of 8,192.
   if (a.max_len <= 8192 && grid.x > 512) {
     CR_LAUNCH((choose_kernel<256, 8>), grid, dim3(256), 0, s, a);
   } else if (a.max_len <= 32768) {
@@ -300,7 +302,9 @@ hipError_t choose(const ChooseArgs& a, hipStream_t s) {
 // of U rows (rows that are no power of two: threads past the row idle).  Bound by
 // memory where there are enough workgroups; few of them, in place, share the rows'
 // columns, down to a cache line (36 layers of 2 heads, 2,048 of 4,096 slots of 256
-// bytes: 55 us with whole rows, 41 with halves), out of place the steps.
+// bytes: 55 us with whole rows, 41 with halves, several such caches in turn; 28 on one
+// of them again and again, whose 153 MB stay in the last-level cache), out of place the
+// steps.
 template <int LOG>
 struct MoveCfg {
   static constexpr int NT = 256, PER_ROW = 1 << LOG, RPP = NT / PER_ROW;   // rows per pass

@@ -224,8 +224,8 @@ __device__ __forceinline__ void add_rows(const WeighArgs& a, bool general, const
 
 // ---- up to 16 rows in every sequence (single tokens): each wave has tiles of its own, a
 // run of them, and keeps the rows while the sequence is the same.  Bound by the keys'
-// bytes: 64 sequences of up to 8,192 slots, 8 KV heads of 128: 84 us, 4.3 TB/s; tiles of
-// 64 keys leave fewer waves to a CU (99 us).
+// bytes: 64 sequences of 73 to 15,144 slots (170,000 in all), 8 KV heads of 128: 82 us,
+// 4.4 TB/s; tiles of 64 keys leave fewer waves to a CU (99 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void weigh_token_kernel(WeighArgs a, WeighTable tab) {
   using MM = Mma16<T>;
@@ -335,11 +335,15 @@ __global__ __launch_bounds__(256) void weigh_rows_kernel(WeighArgs a, WeighTable
 
 // ---- many rows: queries and what their rows bring go through LDS, for 2 x KT keys of
 // a workgroup; two waves hold the same keys and take every other half of a chunk's rows.
-// The chunk after the one that is worked on is on its way meanwhile.  Bound by the issue
-// of what is done for a score beside its products (a fused multiply-add, an exponential, a
-// fused multiply-add into the sum, and moves: about ten to a matrix instruction at a head
-// of 128): 8,192 queries over 12,288 slots, 32 query and 8 KV heads, 804 us, 684 TFLOP/s
-// (rows from memory, without LDS: 1,421 us).
+// The chunk after the one that is worked on is on its way meanwhile.  8,192 queries over
+// 12,288 slots, 32 query and 8 KV heads of 128: 805 us, 683 TFLOP/s (rows from memory,
+// without LDS: 1,421 us).  By the counters 7.4 vector instructions go with a matrix
+// instruction; the arithmetic of its scores (a fused multiply-add, an exponential, a fused
+// multiply-add into the sum) is 3 of them, the others decide who sees what, unpack the
+// rows' information and form addresses.  They fill some 45% of the issue, the matrix
+// instructions 28%, and waves wait 33% of their time: no limit is reached.  Capped scores
+// take 1,716 us, slopes 1,086, documents' intervals 1,066 (165 TFLOP/s of what is seen);
+// fp32, 2,048 queries over 4,096 slots of the same heads 735 us, 70 TFLOP/s.
 //
 // Rows of all sequences, KV head by KV head: info[head][tok0 * group + r].
 __global__ __launch_bounds__(256) void weigh_info_kernel(WeighArgs a, WeighTable tab) {

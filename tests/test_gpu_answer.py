@@ -32,10 +32,10 @@ WEIGH = {
     # single tokens: one row of a group, lengths from none to several tiles
     "tokens": dict(dtype="bf16", heads=16, kv_heads=2, d=128, bs=16, q=[1] * 6, lens=[1, 0, 17, 250, 33, 129]),
     "tokens-f32": dict(dtype="f32", heads=4, kv_heads=4, d=96, bs=1, q=[1, 0, 1], lens=[3, 5, 90]),
-    # up to 256 rows in a sequence
+    # up to 512 rows for a KV head, over few tiles
     "rows": dict(dtype="bf16", heads=6, kv_heads=3, d=64, bs=8, q=[0, 5, 1, 40], lens=[9, 5, 130, 141]),
     "rows-f32": dict(dtype="f32", heads=5, kv_heads=1, d=32, bs=4, q=[7, 30], lens=[7, 150]),
-    # more: through LDS, chunks that end inside, groups that do not divide a round's rows
+    # prompts of fewer rows than go through LDS, groups that do not divide a step's rows
     "prompt": dict(dtype="bf16", heads=8, kv_heads=2, d=128, bs=16, q=[90, 0, 3], lens=[200, 4, 100]),
     "prompt-odd": dict(dtype="bf16", heads=7, kv_heads=1, d=64, bs=8, q=[61], lens=[170]),
     "prompt-f32": dict(dtype="f32", heads=5, kv_heads=1, d=128, bs=2, q=[60, 2], lens=[60, 300]),
