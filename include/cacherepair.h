@@ -697,7 +697,8 @@ CR_API cr_status cr_choose_slots(const cr_kv_layout* layout, const cr_sequences*
  * cuts the slots that are left.  A model with slopes or windows gets other scores
  * than before the compaction.
  *  kept:      device, [n_layers][n_seqs][n_kv_heads][budget], as cr_choose_slots
- *             leaves it or the caller's own: ascending, each below its
+ *             leaves it or the caller's own: ascending, no slot twice and, in
+ *             place, none before its own place in the list, each below its
  *             sequence's length.  An entry that is no such slot moves nothing;
  *             one whose slot, or the place for it, lies in no block moves its
  *             weight alone.
